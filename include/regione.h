@@ -69,6 +69,8 @@ enum { REGIONE_METRIC_COSINE = 0, REGIONE_METRIC_L2 = 1 };
 enum { REGIONE_ROWS_EDITED_QUERIES = 0, REGIONE_ROWS_PAPER = 1 };
 /* which elements of a head form a rotary pair: (2i, 2i+1) or (i, i + D/2) */
 enum { REGIONE_ROPE_INTERLEAVED = 0, REGIONE_ROPE_HALF = 1 };
+/* what a grouped product applies to its sums: nothing, or gelu in its tanh form */
+enum { REGIONE_ACT_NONE = 0, REGIONE_ACT_GELU_TANH = 1 };
 
 /* Library version (major*10000 + minor*100 + patch) and status names. */
 int regione_version(void);
@@ -265,6 +267,71 @@ int regione_rikv_load_e4m3(const uint8_t* k_q, const uint8_t* v_q, const float* 
                            int B, int Nc_cap, int H, int D,
                            regione_bf16* k_cache, regione_bf16* v_cache,
                            int32_t* dev_status, void* stream);
+
+/*
+ * The 4-bit microscaled format, for the operands of regione_mxfp4_grouped_matmul and for the cache below.
+ * (The paper keeps everything in the model's precision; this format has no counterpart there.)  32
+ * consecutive elements of a row share one power-of-two scale, an element is a 4-bit E2M1 value (1 sign,
+ * 2 exponent, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives):
+ *     s = 2^k, k the smallest integer with max |x| / 2^k <= 6 over the 32 elements (k = 0 if all are zero;
+ *         k >= -127); stored as the byte k + 127 (E8M0)
+ *     code = nearest E2M1 value of x / s, ties to the even code; elements 2i and 2i + 1 of a row are the low
+ *         and the high half of byte i
+ *     value(code) * s is exact in bf16 (but for 2^128, to which maxima above 1.75 * 2^127 are rounded: infinite)
+ * regione_mxfp4_quantize: row j of request b is row idx[b, j] of x (idx NULL: row j; then cap <= src_rows),
+ * for j < n[b] (n NULL: for every j < cap).  regione_mxfp4_dequantize widens rows j < n[b] back.
+ * x dev bf16 [B, src_rows, K] ([B, cap, K] when widening); codes dev u8 [B, cap, K / 2]; scales dev u8
+ * [B, cap, K / 32]; idx dev int32 [B, cap]; n dev int32 [B].  K a multiple of 32.  x and codes 16-byte
+ * aligned.  Rows past n[b] are left untouched; a count outside [0, cap] is clamped, an index outside
+ * [0, src_rows) skipped, and REGIONE_DEV_BOUNDS recorded.  An infinite element becomes the largest value
+ * of its block's scale; NaN elements are not preserved.
+ */
+int regione_mxfp4_quantize(const regione_bf16* x, const int32_t* idx, const int32_t* n, int B, int64_t src_rows, int64_t cap,
+                           int64_t K, uint8_t* codes, uint8_t* scales, int32_t* dev_status, void* stream);
+int regione_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, const int32_t* n, int B, int64_t cap, int64_t K,
+                             regione_bf16* x, int32_t* dev_status, void* stream);
+
+/*
+ * 4-bit variant of the Region-Instruction KV cache (see regione_rikv_store and its 8-bit variant): the
+ * retained rows of K and V in the format above, a scale per 32 elements of a head, 17 / 64 of the bf16
+ * cache's bytes.
+ * k_full, v_full [B, N_full, H, D] bf16; keep_rows dev int32 [B, Nc_cap]; n_keep dev int32 [B];
+ * k_q, v_q dev u8 [B, Nc_cap, H, D / 2]; k_scale, v_scale dev u8 [B, Nc_cap, H, D / 32];
+ * k_cache, v_cache dev bf16 [B, Nc_cap, H, D].  Rows past n_keep[b] are left untouched by both.
+ * D must be 64 or 128.
+ */
+int regione_rikv_store_mxfp4(const regione_bf16* k_full, const regione_bf16* v_full, const int32_t* keep_rows,
+                             const int32_t* n_keep, int B, int N_full, int Nc_cap, int H, int D, uint8_t* k_q, uint8_t* v_q,
+                             uint8_t* k_scale, uint8_t* v_scale, int32_t* dev_status, void* stream);
+int regione_rikv_load_mxfp4(const uint8_t* k_q, const uint8_t* v_q, const uint8_t* k_scale, const uint8_t* v_scale,
+                            const int32_t* n_keep, int B, int Nc_cap, int H, int D, regione_bf16* k_cache,
+                            regione_bf16* v_cache, int32_t* dev_status, void* stream);
+
+/*
+ * Matrix products of ragged groups of rows.  (The paper takes the model's layers as given; what a region
+ * step asks of them is that the number of recomputed rows stays on the device, and that text and image rows
+ * have weights of their own.)  Group g is the rows [row_begin[g], row_end[g]) of x, its weight set
+ * i = g mod n_weights (1: one set for all; 2: text and image rows of every request in turn; groups: experts):
+ *     out[r, :] = act(x[r, :] W_i^T + bias_i)     sums in fp32, one rounding to bf16
+ * x dev bf16 [rows_cap, K], rows x_stride elements apart; w dev bf16 [n_weights, N, K]; bias dev bf16
+ * [n_weights, N] or NULL; row_begin, row_end dev int32 [groups]; out dev bf16 [rows_cap, N], rows out_stride
+ * elements apart.  Groups may be empty, rows may be in no group (theirs of out are left untouched), no row
+ * may be in two; a range that is not within [0, rows_cap] is cut to it and REGIONE_DEV_BOUNDS recorded.
+ * out may not overlap x or w.  K, N and the strides are multiples of 8, groups <= 1024, x, w, bias and out
+ * 16-byte aligned.  activation: REGIONE_ACT_NONE, or REGIONE_ACT_GELU_TANH,
+ * act(y) = y / 2 (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))).  One kernel launch; nothing is allocated.
+ *
+ * regione_mxfp4_grouped_matmul: the same with x and w in the 4-bit format (rows quantised along K): x_q
+ * [rows_cap, K / 2], x_scale [rows_cap, K / 32], w_q [n_weights, N, K / 2], w_scale [n_weights, N, K / 32],
+ * all contiguous and 16-byte aligned.  K is a multiple of 128.
+ */
+int regione_grouped_matmul(const regione_bf16* x, int64_t x_stride, const regione_bf16* w, const regione_bf16* bias,
+                           const int32_t* row_begin, const int32_t* row_end, int rows_cap, int groups, int n_weights, int K, int N,
+                           int activation, regione_bf16* out, int64_t out_stride, int32_t* dev_status, void* stream);
+int regione_mxfp4_grouped_matmul(const uint8_t* x_q, const uint8_t* x_scale, const uint8_t* w_q, const uint8_t* w_scale,
+                                 const regione_bf16* bias, const int32_t* row_begin, const int32_t* row_end, int rows_cap,
+                                 int groups, int n_weights, int K, int N, int activation, regione_bf16* out, int64_t out_stride,
+                                 int32_t* dev_status, void* stream);
 
 /*
  * Region attention with the Region-Instruction KV cache (Sec. 4, "Region-Aware

@@ -585,3 +585,51 @@ def stage_schedule(T=28, t_st=6, forced=(16,), t_sm=2):
     for i in range(bounds[-1], 0, -1):
         kinds.append((i, "full"))
     return kinds
+
+
+# ---- 4-bit microscaled format (E2M1 elements, a power-of-two scale per 32), and products of groups of rows -------------
+
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mxfp4_quantize(x):
+    """x [..., K] -> (codes uint8 [..., K / 2], scales uint8 [..., K / 32]).  The scale is found by search from the definition
+    (smallest k >= -127 with max |x| <= 6 * 2^k), the code by distance (ties to the even code)."""
+    x = np.asarray(x, np.float64)
+    t = x.reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
+    top = np.minimum(np.abs(t).max(-1), 255.0 * 2.0 ** 120)               # largest finite bf16
+    k = np.full(top.shape, 128)
+    while True:
+        lower = (top <= 6.0 * 2.0 ** (k - 1.0)) & (k > -127)
+        if not lower.any():
+            break
+        k = np.where(lower, k - 1, k)
+    k = np.where(top == 0, 0, k)
+    a = np.abs(t) / (2.0 ** k)[..., None]
+    d = np.abs(np.minimum(a, 6.0)[..., None] - E2M1)
+    best = d.min(-1, keepdims=True)
+    even_first = np.array([0, 2, 4, 6, 1, 3, 5, 7])
+    code = even_first[np.argmax((d == best)[..., even_first], -1)].astype(np.uint8)
+    code = (code | (np.signbit(t).astype(np.uint8) << 3)).reshape(x.shape)
+    return code[..., 0::2] | (code[..., 1::2] << 4), (k + 127).astype(np.uint8)
+
+
+def mxfp4_dequantize(codes, scales):
+    code = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], 2 * codes.shape[-1])
+    v = np.where(code & 8, -1.0, 1.0) * E2M1[code & 7]
+    return v * np.repeat(2.0 ** (scales.astype(np.float64) - 127.0), 32, axis=-1)
+
+
+def grouped_matmul(x, w, row_begin, row_end, out, bias=None, gelu=False):
+    """out[r] = act(x[r] W_i^T + b_i) for the rows of every group g, i = g mod len(w); other rows as in ``out``."""
+    out = np.array(out, np.float64)
+    for g, (b, e) in enumerate(zip(row_begin, row_end)):
+        i = g % len(w)
+        for r in range(int(b), int(e)):
+            y = np.asarray(w[i], np.float64) @ np.asarray(x[r], np.float64)
+            if bias is not None:
+                y = y + np.asarray(bias[i], np.float64)
+            if gelu:
+                y = 0.5 * y * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (y + 0.044715 * y ** 3)))
+            out[r] = y
+    return out

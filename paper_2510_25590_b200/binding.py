@@ -20,6 +20,7 @@ DEV_OK, DEV_TIMEOUT, DEV_BOUNDS = 0, 5, 6
 METRIC_COSINE, METRIC_L2 = 0, 1
 ROWS_EDITED_QUERIES, ROWS_PAPER = 0, 1
 ROPE_INTERLEAVED, ROPE_HALF = 0, 1
+ACT_NONE, ACT_GELU_TANH = 0, 1
 
 STEP_MOVES, STEP_ATTENTION = 1, 2
 
@@ -61,6 +62,12 @@ SIGNATURES = {
     "regione_rikv_store_e4m3": (c_int, [_P, _P, _P, _P, c_int, c_int, c_int, c_int, c_int, _P, _P, _P, _P, _P, _P]),
     "regione_rikv_load_e4m3": (c_int, [_P, _P, _P, _P, _P, c_int, c_int, c_int, c_int, _P, _P, _P, _P]),
     "regione_fresh_qkv": (c_int, [_P] * 5 + [c_int] * 6 + [_P, _P, c_float, _P, _P, c_int, _P, _P, _P, _P, _P]),
+    "regione_mxfp4_quantize": (c_int, [_P, _P, _P, c_int, c_int64, c_int64, c_int64, _P, _P, _P, _P]),
+    "regione_mxfp4_dequantize": (c_int, [_P, _P, _P, c_int, c_int64, c_int64, _P, _P, _P]),
+    "regione_rikv_store_mxfp4": (c_int, [_P, _P, _P, _P, c_int, c_int, c_int, c_int, c_int, _P, _P, _P, _P, _P, _P]),
+    "regione_rikv_load_mxfp4": (c_int, [_P, _P, _P, _P, _P, c_int, c_int, c_int, c_int, _P, _P, _P, _P]),
+    "regione_grouped_matmul": (c_int, [_P, c_int64, _P, _P, _P, _P] + [c_int] * 6 + [_P, c_int64, _P, _P]),
+    "regione_mxfp4_grouped_matmul": (c_int, [_P] * 7 + [c_int] * 6 + [_P, c_int64, _P, _P]),
     "regione_region_attention_workspace": (c_size_t, [c_int] * 6),
     "regione_region_attention": (c_int, [_P] * 8 + [c_int] * 6 + [c_float, _P, _P, c_size_t, _P, _P]),
     "regione_region_attention_scatter": (c_int, [_P] * 8 + [c_int] * 6 + [c_float, _P, c_int, _P, _P, c_size_t, _P, _P]),
@@ -316,6 +323,131 @@ def rikv_load_e4m3(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_sta
         _ptr(v_scale, torch.float32, "v_scale"), _ptr(n_keep, torch.int32), B, cap, H, D,
         _ptr(k_cache, bf, "k_cache"), _ptr(v_cache, bf, "v_cache"), _ptr(dev_status, torch.int32),
         _stream(stream)), "regione_rikv_load_e4m3")
+
+
+def _want(t, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise RegionEError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def mxfp4_quantize(x, codes, scales, idx=None, n=None, dev_status=None, stream=None):
+    """Rows of bf16 ``x`` [B, rows, K] to 4-bit microscaled ``codes`` [B, cap, K / 2] and ``scales`` [B, cap, K / 32]: row j of
+    request b is row idx[b, j] (without ``idx`` row j), j < n[b] (without ``n`` every one)."""
+    torch = _torch()
+    u8, i32 = torch.uint8, torch.int32
+    B, rows, K = x.shape
+    cap = codes.shape[1]
+    _want(codes, (B, cap, K // 2), "codes")
+    _want(scales, (B, cap, K // 32), "scales")
+    if idx is not None:
+        _want(idx, (B, cap), "idx")
+    if n is not None:
+        _want(n, (B,), "n")
+    _check(load().regione_mxfp4_quantize(
+        _ptr(x, torch.bfloat16, "x"), _ptr(idx, i32, "idx"), _ptr(n, i32, "n"), B, rows, cap, K, _ptr(codes, u8, "codes"),
+        _ptr(scales, u8, "scales"), _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_quantize")
+
+
+def mxfp4_dequantize(codes, scales, x, n=None, dev_status=None, stream=None):
+    """Widens rows j < n[b] of ``mxfp4_quantize`` back to bf16 ``x`` [B, cap, K] (exactly the quantised values)."""
+    torch = _torch()
+    u8, i32 = torch.uint8, torch.int32
+    B, cap, K = x.shape
+    _want(codes, (B, cap, K // 2), "codes")
+    _want(scales, (B, cap, K // 32), "scales")
+    if n is not None:
+        _want(n, (B,), "n")
+    _check(load().regione_mxfp4_dequantize(
+        _ptr(codes, u8, "codes"), _ptr(scales, u8, "scales"), _ptr(n, i32, "n"), B, cap, K, _ptr(x, torch.bfloat16, "x"),
+        _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_dequantize")
+
+
+def rikv_store_mxfp4(k_full, v_full, keep_rows, n_keep, k_q, v_q, k_scale, v_scale, dev_status=None, stream=None):
+    """``rikv_store`` into a 4-bit microscaled cache: codes [B, cap, H, D / 2], a scale per 32 elements [B, cap, H, D / 32]."""
+    torch = _torch()
+    bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
+    B, n_full, H, D = k_full.shape
+    cap = keep_rows.shape[1]
+    _want(v_full, k_full.shape, "v_full")
+    _want(keep_rows, (B, cap), "keep_rows")
+    _want(n_keep, (B,), "n_keep")
+    for t, d, name in ((k_q, 2, "k_q"), (v_q, 2, "v_q"), (k_scale, 32, "k_scale"), (v_scale, 32, "v_scale")):
+        _want(t, (B, cap, H, D // d), name)
+    _check(load().regione_rikv_store_mxfp4(
+        _ptr(k_full, bf, "k_full"), _ptr(v_full, bf, "v_full"), _ptr(keep_rows, i32, "keep_rows"), _ptr(n_keep, i32, "n_keep"),
+        B, n_full, cap, H, D, _ptr(k_q, u8, "k_q"), _ptr(v_q, u8, "v_q"), _ptr(k_scale, u8, "k_scale"),
+        _ptr(v_scale, u8, "v_scale"), _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_rikv_store_mxfp4")
+
+
+def rikv_load_mxfp4(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_status=None, stream=None):
+    """Widens a 4-bit cache back to bf16 (exactly the quantised values) for the attention."""
+    torch = _torch()
+    bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
+    B, cap, H, D = k_cache.shape
+    _want(v_cache, k_cache.shape, "v_cache")
+    _want(n_keep, (B,), "n_keep")
+    for t, d, name in ((k_q, 2, "k_q"), (v_q, 2, "v_q"), (k_scale, 32, "k_scale"), (v_scale, 32, "v_scale")):
+        _want(t, (B, cap, H, D // d), name)
+    _check(load().regione_rikv_load_mxfp4(
+        _ptr(k_q, u8, "k_q"), _ptr(v_q, u8, "v_q"), _ptr(k_scale, u8, "k_scale"), _ptr(v_scale, u8, "v_scale"),
+        _ptr(n_keep, i32, "n_keep"), B, cap, H, D, _ptr(k_cache, bf, "k_cache"), _ptr(v_cache, bf, "v_cache"),
+        _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_rikv_load_mxfp4")
+
+
+def _rows(t, name):
+    """Device address and row distance of a bf16 CUDA matrix whose rows may lie apart."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise RegionEError(f"{name} must be a CUDA tensor")
+    if t.dtype != torch.bfloat16:
+        raise RegionEError(f"{name} must have dtype {torch.bfloat16}, got {t.dtype}")
+    rows, cols = t.shape
+    stride = t.stride(0) if rows > 1 else max(cols, 1)
+    if cols > 1 and t.stride(1) != 1 or stride < cols:
+        raise RegionEError(f"the elements of a row of {name} must be contiguous and its rows apart")
+    return t.data_ptr(), stride
+
+
+def grouped_matmul(x, w, row_begin, row_end, out, bias=None, activation=ACT_NONE, dev_status=None, stream=None):
+    """out[r] = act(x[r] @ w[i].T + bias[i]) for the rows r of group g, row_begin[g] <= r < row_end[g], with its weight set
+    i = g % w.shape[0].  ``x`` [rows, K], ``out`` [rows, N] (rows may lie apart), ``w`` [sets, N, K], ``bias`` [sets, N], the
+    ranges on the device; rows of no group are left as they are."""
+    torch = _torch()
+    bf, i32 = torch.bfloat16, torch.int32
+    rows, K = x.shape
+    sets, N, _ = w.shape
+    _want(w, (sets, N, K), "w")
+    _want(out, (rows, N), "out")
+    _want(row_end, row_begin.shape, "row_end")
+    if bias is not None:
+        _want(bias, (sets, N), "bias")
+    (xp, xs), (op, os_) = _rows(x, "x"), _rows(out, "out")
+    _check(load().regione_grouped_matmul(
+        xp, xs, _ptr(w, bf, "w"), _ptr(bias, bf, "bias"), _ptr(row_begin, i32, "row_begin"), _ptr(row_end, i32, "row_end"), rows,
+        row_begin.numel(), sets, K, N, int(activation), op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)),
+        "regione_grouped_matmul")
+
+
+def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bias=None, activation=ACT_NONE, dev_status=None,
+                         stream=None):
+    """``grouped_matmul`` of rows and weights in the 4-bit format: codes [rows, K / 2] and [sets, N, K / 2], scales
+    [rows, K / 32] and [sets, N, K / 32]."""
+    torch = _torch()
+    bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
+    rows, K = x_q.shape[0], 2 * x_q.shape[1]
+    sets, N, _ = w_q.shape
+    _want(x_scale, (rows, K // 32), "x_scale")
+    _want(w_q, (sets, N, K // 2), "w_q")
+    _want(w_scale, (sets, N, K // 32), "w_scale")
+    _want(out, (rows, N), "out")
+    _want(row_end, row_begin.shape, "row_end")
+    if bias is not None:
+        _want(bias, (sets, N), "bias")
+    op, os_ = _rows(out, "out")
+    _check(load().regione_mxfp4_grouped_matmul(
+        _ptr(x_q, u8, "x_q"), _ptr(x_scale, u8, "x_scale"), _ptr(w_q, u8, "w_q"), _ptr(w_scale, u8, "w_scale"),
+        _ptr(bias, bf, "bias"), _ptr(row_begin, i32, "row_begin"), _ptr(row_end, i32, "row_end"), rows, row_begin.numel(), sets, K, N,
+        int(activation), op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_grouped_matmul")
 
 
 def fresh_qkv(q_src, k_src, v_src, idx, n, q_weight, k_weight, eps, cos_table, sin_table, rope_layout,

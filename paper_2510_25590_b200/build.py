@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libregione.so")
 SOURCES = ["api.cu", "partition.cu", "rowcopy.cu", "latent.cu", "gamma.cu", "kvquant.cu", "freshqkv.cu", "attention_simt.cu", "attention_tc.cu",
-           "step.cu"]
+           "step.cu", "mxfp4.cu", "grouped.cu"]
 HEADERS = ["attention_plan.cuh", "common.cuh", "rowcopy.cuh", "sm100_ptx.cuh"]
 
 

@@ -1,0 +1,696 @@
+// Matrix products of ragged groups of rows (regione_grouped_matmul, regione_mxfp4_grouped_matmul):
+//
+//     out[r, :] = act(x[r, :] W_i^T + b_i),    r in [row_begin[g], row_end[g]),  i = g mod n_weights
+//
+// The paper names no such operator: it takes the model's layers as given.  What its region step asks of them is here: the
+// recomputed rows of a request are few, their number is known on the device only (the partition wrote it), and text and image
+// rows of a block have weights of their own (Sec. 4 "Region-Aware Generation": which rows a region step recomputes).
+//
+// The features of W are the M side of the tensor-core product and the rows of x its N side: D^T = W x^T.  M is fixed by the
+// hardware (128 lanes of tensor memory a CTA), N is any multiple of 16 or 32 up to 256 named in the instruction, so a group
+// of 5 rows costs a tile of 16 or 32 and not one of 128 or 256.
+#include "common.cuh"
+#include "sm100_ptx.cuh"
+
+#include <algorithm>
+
+namespace regione {
+
+constexpr int kFeat = 128;                            // features a CTA
+constexpr int kChunkBytes = 128;                      // of K: 64 bf16 or 256 4-bit elements, one swizzle row
+constexpr int kTileBytes = 128 * kChunkBytes;         // 128 rows of either operand
+constexpr int kStageBytes = 2 * kTileBytes;           // features, rows
+constexpr int kMaxStages = 6;
+constexpr int kMaxGroups = 1024;
+constexpr int kScaleA = 1024, kScaleB = 2048;         // scales of a stage: [2 of 128 elements][1 or 2 of 128 rows][512 bytes]
+constexpr int kEpiWarps = 8;
+constexpr int kStagingBytes = 1024;                   // per epilogue warp: 16 rows of 32 features
+constexpr int kProducer = kEpiWarps, kIssuer = kEpiWarps + 1, kScaler = kEpiWarps + 2;
+constexpr int kScaleWarps = 4;
+constexpr long long kGroupedWait = 4000000000LL;      // cycles (about 2 s): bound of every wait
+constexpr int kMaps = 4;                              // boxes of 16, 32, 64 and 128 rows of x
+
+struct GroupedArgs {
+    const int32_t *row_begin, *row_end;
+    int groups, n_weights, rows_cap, K, N;
+    int chunks;                                       // of K
+    int stages;
+    int slices;                                       // of K, one per CTA of a cluster (the kernel without pairs)
+    int width;                                        // rows of a tile at most (the kernel without pairs)
+    const uint16_t* bias;                             // [n_weights, N] or NULL
+    int activation;
+    uint16_t* out;
+    long long out_stride;
+    const uint8_t *x_scale, *w_scale;                 // [rows_cap, K / 32], [n_weights, N, K / 32]
+    int32_t* dev_status;
+};
+struct GroupedMaps {
+    CUtensorMap w;                                    // (K, N, n_weights), box 128 bytes x 128 rows
+    CUtensorMap x[kMaps];                             // (K, rows), box 128 bytes x 16 << i rows
+};
+
+struct GroupedControl {
+    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+    uint32_t tmem;
+    int abort_flag;
+    int width, total;                                 // of the plan: rows of a tile at most, tiles
+    int cost[8];
+    int first[kMaxGroups + 1];                        // first tile of a group (in units of its feature tiles' row tiles)
+};
+
+// ---- instructions that the pair of CTAs and the scaled product need -------------------------------------------
+namespace {
+
+template <bool PAIR> __device__ __forceinline__ void tmem_alloc512(uint32_t slot) {
+    if constexpr (PAIR)
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(slot) : "memory");
+    else
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(slot) : "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void tmem_free512(uint32_t taddr) {
+    if constexpr (PAIR) {
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(taddr) : "memory");
+    } else {
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(taddr) : "memory");
+    }
+}
+
+template <bool PAIR, bool FP4>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    if constexpr (FP4 && PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    else if constexpr (FP4)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    else if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        ptx::mma_ss(d, a, b, idesc, accumulate);
+}
+
+// Scales of 128 rows and 128 elements (512 bytes: row r at (r % 32) * 16 + (r / 32) * 4) to 4 columns of tensor memory, in all four
+// lane groups; in a pair each CTA from its own shared memory to its own tensor memory.  Products issued behind it by the same
+// thread see them.
+template <bool PAIR> __device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+    if constexpr (PAIR)
+        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else
+        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+// All tcgen05 operations issued so far by this thread arrive on `bar`, in a pair on the barrier at that place in both CTAs.
+template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        ptx::mma_commit(bar);
+}
+
+// Tiled loads; in a pair `bar` may be the leader's.
+template <bool PAIR>
+__device__ __forceinline__ void load_w(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void load_x(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+
+// 16 lanes x 16 columns: thread l gets rows l / 4 and l / 4 + 8, columns 2 (l % 4) + {0, 1} and the same 8 further on.
+__device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr) : "memory");
+}
+// Four 8 x 8 matrices of 16-bit elements, transposed; lane l names the place of row l % 8 of matrix l / 8.
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                 ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+}  // namespace
+
+// ---- waits: bounded; a wait that runs out is recorded and makes the other roles of the CTA give up -----------------
+__device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status) {
+    const long long t0 = clock64();
+    while (!ptx::mbar_try_wait_cluster(bar, parity)) {
+        if (*abort_flag) return false;
+        if (clock64() - t0 > kGroupedWait) {
+            *abort_flag = 1;
+            record_status(dev_status, REGIONE_DEV_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, GroupedControl* ctl, int32_t* dev_status) {
+    return ptx::mbar_try_wait_cluster(bar, parity) || grouped_wait_slow(bar, parity, &ctl->abort_flag, dev_status);
+}
+
+// gelu(x) = x / 2 (1 + tanh(u)) = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3); the second form keeps its relative accuracy
+// where tanh(u) is near -1.
+__device__ __forceinline__ float gelu_tanh(float x) {
+    const float u = x * fmaf(0.044715f * 0.7978845608f, x * x, 0.7978845608f);
+    return __fdividef(x, 1.0f + fast_exp2(-2.8853900818f * u));
+}
+
+__device__ __forceinline__ int rows_of(const GroupedArgs& p, int g, int& begin) {
+    const int b = p.row_begin[g], e = p.row_end[g];
+    begin = min(max(b, 0), p.rows_cap);
+    return max(min(e, p.rows_cap) - begin, 0);
+}
+
+// Rows [first, first + live) of a group against a feature tile; `width` = columns of the product.
+struct GroupedTile {
+    int first, live, width, weights, feature;
+};
+
+// Tile t of the plan.  Tiles of a group run through eight feature tiles before they go on to the next rows, so that the tiles in
+// flight at one time share both operands.  PAIR: 256 features, widths in steps of 32.
+template <bool PAIR>
+__device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const GroupedControl* ctl, int t, int f_tiles) {
+    int lo = 0, hi = p.groups;                        // last group whose first tile is not behind t
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((long long)ctl->first[mid] * f_tiles <= t) lo = mid; else hi = mid;
+    }
+    int begin;
+    const int rows = rows_of(p, lo, begin), n = ctl->first[lo + 1] - ctl->first[lo];
+    int in = t - ctl->first[lo] * f_tiles;
+    const int block = in / (8 * n);
+    in -= block * 8 * n;
+    const int wide = min(8, f_tiles - block * 8), at = in / wide;
+    constexpr int kStep = PAIR ? 32 : 16;
+    const int width = ((rows + n - 1) / n + kStep - 1) / kStep * kStep;       // n even tiles
+    GroupedTile tile;
+    tile.first = begin + at * width;
+    tile.live = min(width, rows - at * width);
+    tile.width = width;
+    tile.weights = lo % p.n_weights;
+    tile.feature = (block * 8 + in - at * wide) * (PAIR ? 2 : 1) * kFeat;
+    return tile;
+}
+
+template <bool FP4, bool PAIR>
+__global__ void __launch_bounds__((kEpiWarps + 2 + (FP4 ? kScaleWarps : 0)) * 32, 1)
+grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__ GroupedArgs p) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    constexpr int kElems = FP4 ? 256 : 64;            // of K in a chunk
+    constexpr int kMaxWidth = PAIR ? (FP4 ? 224 : 256) : 128;
+    constexpr int kAcc1 = PAIR ? kMaxWidth : 0;       // column of the second accumulator
+    constexpr int kScaleCol = PAIR ? 448 : 128;       // columns of the scales: 2 x (8 of W, 16 of x)
+    const uint32_t smem = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
+    uint8_t* base = smem_raw + (smem - ptx::smem_addr(smem_raw));
+    uint8_t* scales = base + (size_t)p.stages * kStageBytes;
+    uint8_t* staging = scales + (FP4 ? (size_t)p.stages * (kScaleA + kScaleB) : 0);
+    GroupedControl* ctl = reinterpret_cast<GroupedControl*>(staging + kEpiWarps * kStagingBytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cluster = PAIR ? 2 : p.slices;
+    const int rank = cluster > 1 ? (int)(blockIdx.x % cluster) : 0;
+    const bool leader = !PAIR || rank == 0;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            ptx::mbar_init(ptx::smem_addr(&ctl->full[s]), 1 + (FP4 ? (PAIR ? 2 : 1) : 0));
+            ptx::mbar_init(ptx::smem_addr(&ctl->empty[s]), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            ptx::mbar_init(ptx::smem_addr(&ctl->acc_full[a]), 1);
+            ptx::mbar_init(ptx::smem_addr(&ctl->acc_empty[a]), kEpiWarps * (PAIR ? 2 : 1));
+        }
+        ptx::mbar_init(ptx::smem_addr(&ctl->drain), 1);
+        ctl->abort_flag = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == kIssuer) tmem_alloc512<PAIR>(ptx::smem_addr(&ctl->tmem));
+    if (warp == kProducer && lane == 0) ptx::prefetch_tensormap(&maps.w);
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    // ---- plan: from the groups' row counts, which only the device knows --------------------------------------------
+    const int f_tiles = (p.N + (PAIR ? 2 : 1) * kFeat - 1) / ((PAIR ? 2 : 1) * kFeat);
+    const int workers = PAIR ? gridDim.x / 2 : gridDim.x / cluster;
+    if constexpr (PAIR) {
+        // Widths of 32 .. 256 (224) rows: one warp adds up the tiles of one width.  A round of tiles takes as long as its width, plus
+        // what a tile costs whatever its width; the width with the cheapest rounds is taken, the larger of equals.
+        if (warp < kMaxWidth / 32) {
+            const int width = 32 * (warp + 1);
+            int n = 0;
+            for (int g = lane; g < p.groups; g += 32) {
+                int begin;
+                n += (rows_of(p, g, begin) + width - 1) / width;
+            }
+            n = __reduce_add_sync(0xffffffffu, n);
+            const long long rounds = ((long long)n * f_tiles + workers - 1) / workers;
+            if (lane == 0) ctl->cost[warp] = (int)min(rounds * (max(width, 64) + 16), 0x7fffffffLL);
+        }
+        __syncthreads();
+    }
+    if (warp == 0) {
+        int width = p.width;
+        if constexpr (PAIR) {
+            int best = kMaxWidth / 32 - 1;
+            for (int i = kMaxWidth / 32 - 2; i >= 0; --i)
+                if (ctl->cost[i] < ctl->cost[best]) best = i;
+            width = 32 * (best + 1);
+        }
+        int at = 0;
+        for (int g0 = 0; g0 < p.groups; g0 += 32) {
+            const int g = g0 + lane;
+            int n = 0;
+            if (g < p.groups) {
+                int begin;
+                const int rows = rows_of(p, g, begin);
+                n = (rows + width - 1) / width;
+                if (blockIdx.x == 0 && (p.row_begin[g] < 0 || p.row_end[g] > p.rows_cap || p.row_end[g] < p.row_begin[g]))
+                    record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+            }
+            int sum = n;
+            for (int d = 1; d < 32; d <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, sum, d);
+                if (lane >= d) sum += up;
+            }
+            if (g < p.groups) ctl->first[g] = at + sum - n;
+            at += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (lane == 0) {
+            ctl->first[p.groups] = at;
+            const long long total = (long long)at * f_tiles;
+            // (one tile per cluster without pairs: the grid covers every set of ranges that do not overlap)
+            if (!PAIR && total > workers && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+            ctl->total = (int)min(total, 0x7fffffffLL);
+        }
+    }
+    ptx::tc_fence_before_sync();
+    if (cluster > 1) ptx::cluster_sync(); else __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = ctl->tmem;
+    const int worker = blockIdx.x / cluster, total = ctl->total;
+    const int step = PAIR ? workers : 0x40000000;
+    // chunks of K that this CTA takes
+    const int c_begin = PAIR ? 0 : (int)((long long)p.chunks * rank / p.slices);
+    const int c_end = PAIR ? p.chunks : (int)((long long)p.chunks * (rank + 1) / p.slices);
+    auto bar_at = [&](const uint64_t* bar) {          // a barrier of the leader
+        const uint32_t a = ptx::smem_addr(bar);
+        return PAIR ? ptx::map_rank(a, 0) : a;
+    };
+
+    if (warp == kProducer) {
+        if (ptx::elect_one()) {
+            int s = 0, filled = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (long long t = worker; t < total && ok; t += step) {
+                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+                const int half = PAIR ? tile.width / 2 : tile.width;
+                int box = 0;
+                while ((16 << box) < half) ++box;
+                const CUtensorMap* x_map = &maps.x[box];
+                const uint32_t bytes = (kTileBytes + (16u << box) * kChunkBytes) * (PAIR ? 2 : 1);
+                const int feature = tile.feature + (PAIR ? rank * kFeat : 0), row = tile.first + (PAIR ? rank * half : 0);
+                for (int c = c_begin; c < c_end; ++c) {
+                    if (!grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
+                    if (leader) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&ctl->full[s]), bytes);
+                    const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * kStageBytes;
+                    load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
+                    load_x<PAIR>(dst + kTileBytes, x_map, bar, c * (FP4 ? kChunkBytes : kElems), row);
+                    ++filled;
+                    if (++s == p.stages) { s = 0; phase ^= 1; }
+                }
+            }
+            if (!ok && leader) {                      // copies in flight land before shared memory is given up
+                for (int i = min(filled, p.stages); i > 0; --i) {
+                    int q = s - i;
+                    uint32_t ph = phase;
+                    if (q < 0) { q += p.stages; ph ^= 1; }
+                    const long long t0 = clock64();
+                    while (!ptx::mbar_try_wait_cluster(ptx::smem_addr(&ctl->full[q]), ph) && clock64() - t0 < kGroupedWait / 8) {}
+                }
+            }
+        }
+    } else if (warp == kIssuer) {
+        if (leader && ptx::elect_one()) {
+            constexpr uint32_t hi = ptx::smem_desc_hi_sw128(1024);              // 8-row groups 1024 bytes apart
+            constexpr uint32_t hi_plain = (128u >> 4) | (1u << 14);             // scales: no swizzle, 8 rows of 16 bytes
+            int s = 0, it = 0, sf = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (long long t = worker; t < total && ok; t += step, ++it) {
+                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+                const int a = PAIR ? it & 1 : 0;
+                const uint32_t d = tmem + (a ? kAcc1 : 0);
+                if (it >= 2 && !grouped_wait(ptx::smem_addr(&ctl->acc_empty[a]), ((it >> 1) - 1) & 1, ctl, p.dev_status)) { ok = false; break; }
+                ptx::tc_fence_after_sync();
+                const uint32_t idesc = FP4 ? (1u << 7) | (1u << 10) | ((uint32_t)(tile.width >> 3) << 17) | (1u << 23) |
+                                                 ((PAIR ? 2u : 1u) << 27)
+                                           : ptx::idesc_bf16_f32(PAIR ? 256 : 128, tile.width, false);
+                uint32_t accumulate = 0;
+                for (int c = c_begin; c < c_end; ++c) {
+                    if (!grouped_wait(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
+                    ptx::tc_fence_after_sync();
+                    const uint32_t at = smem + s * kStageBytes;
+                    const uint32_t a_lo = ptx::smem_desc_lo(at, 16), b_lo = ptx::smem_desc_lo(at + kTileBytes, 16);
+                    uint32_t sfa = 0, sfb = 0;
+                    if constexpr (FP4) {
+                        sfa = tmem + kScaleCol + sf * 32;
+                        sfb = sfa + 8;
+                        sf ^= 1;
+                        const uint32_t sa = ptx::smem_addr(scales) + s * (kScaleA + kScaleB), sb = sa + kScaleA;
+                        for (int k = 0; k < 2; ++k) {
+                            copy_scales<PAIR>(sfa + 4 * k, ptx::smem_desc_join(ptx::smem_desc_lo(sa + k * 512, 16), hi_plain));
+                            copy_scales<PAIR>(sfb + 8 * k, ptx::smem_desc_join(ptx::smem_desc_lo(sb + k * 1024, 16), hi_plain));
+                            if (tile.width > 128)
+                                copy_scales<PAIR>(sfb + 8 * k + 4, ptx::smem_desc_join(ptx::smem_desc_lo(sb + k * 1024 + 512, 16), hi_plain));
+                        }
+                    }
+                    // 32 bytes of K to an instruction; what lies behind K is zero and left out
+                    const int left = (p.K - c * kElems + kElems / 4 - 1) / (kElems / 4);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k >= left) break;
+                        // (bits 4 and 29: which half of a scale word the two blocks of 32 have)
+                        const uint32_t id = FP4 && (k & 1) ? idesc | (2u << 4) | (2u << 29) : idesc;
+                        mma<PAIR, FP4>(d, ptx::smem_desc_join(a_lo + 2 * k, hi), ptx::smem_desc_join(b_lo + 2 * k, hi), id,
+                                       sfa + 4 * (k >> 1), sfb + 8 * (k >> 1), accumulate);
+                        accumulate = 1;
+                    }
+                    commit<PAIR>(ptx::smem_addr(&ctl->empty[s]));
+                    if (++s == p.stages) { s = 0; phase ^= 1; }
+                }
+                if (ok) commit<PAIR>(ptx::smem_addr(&ctl->acc_full[a]));
+            }
+            if (!ok) {                                // products in flight end before tensor memory is given up
+                commit<PAIR>(ptx::smem_addr(&ctl->drain));
+                const long long t0 = clock64();
+                while (!ptx::mbar_try_wait_cluster(ptx::smem_addr(&ctl->drain), 0) && clock64() - t0 < kGroupedWait / 8) {}
+            }
+        }
+    } else if (FP4 && warp >= kScaler) {
+        // Scales of every fourth chunk: 8 bytes a row from device memory to the place in shared memory that the copy to tensor
+        // memory reads.
+        const int k32 = p.K / 32;
+        int seq = 0;                                  // chunks so far
+        bool ok = true;
+        for (long long t = worker; t < total && ok; t += step) {
+            const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+            const int feature = tile.feature + (PAIR ? rank * kFeat : 0);
+            const uint8_t* w_base = p.w_scale + (size_t)tile.weights * p.N * k32;
+            for (int c = c_begin; c < c_end; ++c, ++seq) {
+                if ((seq & (kScaleWarps - 1)) != warp - kScaler) continue;
+                const int s = seq % p.stages;
+                const uint32_t phase = (seq / p.stages) & 1;
+                const bool two = (c + 1) * kElems <= p.K;                       // the chunk's second 128 elements are there
+                uint2 v[12];
+#pragma unroll
+                for (int i = 0; i < 12; ++i) {
+                    const int r = (i >> 2) * 128 - 128 + (lane >> 2) + 8 * (i & 3) + 32 * (lane & 3);   // row of W (below 0) or of x
+                    const uint8_t* src = nullptr;
+                    if (i < 4) {
+                        const int f = feature + r + 128;
+                        if (f < p.N) src = w_base + (size_t)f * k32;
+                    } else if (r < tile.width && tile.first + r < p.rows_cap) {
+                        src = p.x_scale + (size_t)(tile.first + r) * k32;
+                    }
+                    v[i] = make_uint2(0u, 0u);
+                    if (src != nullptr) {
+                        const uint32_t* q = reinterpret_cast<const uint32_t*>(src + (size_t)c * 8);
+                        v[i].x = __ldg(q);
+                        if (two) v[i].y = __ldg(q + 1);
+                    }
+                }
+                ok = __all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status));
+                if (!ok) break;
+                uint32_t* sa = reinterpret_cast<uint32_t*>(scales + (size_t)s * (kScaleA + kScaleB));
+                uint32_t* sb = sa + kScaleA / 4;
+#pragma unroll
+                for (int i = 0; i < 12; ++i) {
+                    uint32_t* dst = i < 4 ? sa + 32 * i + lane : sb + ((i >> 2) - 1) * 128 + 32 * (i & 3) + lane;
+                    dst[0] = v[i].x;
+                    dst[i < 4 ? 128 : 256] = v[i].y;
+                }
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive_cluster(bar_at(&ctl->full[s]));
+            }
+        }
+    } else if (warp < kEpiWarps) {
+        const int sub = warp & 3, part = warp >> 2;
+        const uint32_t stage = ptx::smem_addr(staging) + warp * kStagingBytes;
+        int it = 0;
+        for (long long t = worker; t < total; t += step, ++it) {
+            const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+            const int a = PAIR ? it & 1 : 0;
+            const int feature = tile.feature + (PAIR ? rank * kFeat : 0) + 32 * sub;
+            float bias[4] = {0.f, 0.f, 0.f, 0.f};     // of features lane / 4 + {0, 8, 16, 24}
+            if (p.bias != nullptr && (PAIR || p.slices == 1))
+                for (int i = 0; i < 4; ++i) {
+                    const int f = feature + (lane >> 2) + 8 * i;
+                    if (f < p.N) bias[i] = __uint_as_float((uint32_t)p.bias[(size_t)tile.weights * p.N + f] << 16);
+                }
+            if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->acc_full[a]), (PAIR ? it >> 1 : 0) & 1, ctl, p.dev_status)))
+                break;
+            ptx::tc_fence_after_sync();
+            const uint32_t acc = tmem + (a ? kAcc1 : 0) + ((uint32_t)(32 * sub) << 16);
+            if (!PAIR && p.slices > 1) {
+                // this slice's sums as [row][128 features] fp32 over the stages, which nothing reads any more
+                float* sums = reinterpret_cast<float*>(base);
+                for (int c = part * 16; c < tile.live; c += 32) {
+                    uint32_t r[16];
+                    ptx::tmem_ld16(acc + c, r);
+                    ptx::tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sums[(c + i) * kFeat + 32 * sub + lane] = __uint_as_float(r[i]);
+                }
+            } else {
+                for (int c = part * 16; c < tile.live; c += 32) {
+                    uint32_t r[16];
+                    tmem_ld_16x256b_x2(acc + c, r);
+                    tmem_ld_16x256b_x2(acc + (16u << 16) + c, r + 8);
+                    ptx::tmem_wait_ld();
+                    float y[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        y[i] = __uint_as_float(r[i]) + bias[(i >> 3) * 2 + ((i >> 1) & 1)];
+                        if (p.activation == REGIONE_ACT_GELU_TANH) y[i] = gelu_tanh(y[i]);
+                    }
+                    // row of the tile t at 64 t, its 16-byte pieces (8 features) turned by t / 2 so that eight rows meet eight banks
+                    const int row = (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1, turn = (row >> 1) & 3;
+                    stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
+                                      pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+                    stmatrix_x4_trans(stage + row * 64 + (((piece + 2) ^ turn) << 4), pack_bf16x2(y[8], y[9]),
+                                      pack_bf16x2(y[10], y[11]), pack_bf16x2(y[12], y[13]), pack_bf16x2(y[14], y[15]));
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int q = (lane >> 2) + 8 * i, j = lane & 3;
+                        const uint4 v = *reinterpret_cast<const uint4*>(staging + warp * kStagingBytes + q * 64 + ((j ^ ((q >> 1) & 3)) << 4));
+                        if (c + q < tile.live && feature + 8 * j < p.N)
+                            *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + c + q) * p.out_stride + feature + 8 * j) = v;
+                    }
+                    __syncwarp();
+                }
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (PAIR && lane == 0) ptx::mbar_arrive_cluster(bar_at(&ctl->acc_empty[a]));
+        }
+    }
+
+    // ---- the slices of a tile meet --------------------------------------------------------------------------------------
+    __syncwarp();
+    if (!PAIR && p.slices > 1) {
+        ptx::cluster_sync();
+        if (warp < kEpiWarps && worker < total && !ctl->abort_flag) {
+            const GroupedTile tile = tile_at<PAIR>(p, ctl, worker, f_tiles);
+            // pieces of 8 features of a row, dealt over the cluster's threads; slices are added in their order
+            for (int u = threadIdx.x * p.slices + rank; u < tile.live * (kFeat / 8); u += kEpiWarps * 32 * p.slices) {
+                const int q = u / (kFeat / 8), j = u % (kFeat / 8), f = tile.feature + 8 * j;
+                if (f >= p.N) continue;
+                float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                const uint32_t at = smem + (q * kFeat + 8 * j) * 4;
+                for (int s = 0; s < p.slices; ++s) {
+                    const uint32_t from = ptx::map_rank(at, s);
+                    const float4 lo = ptx::ld_cluster_f4(from), hi = ptx::ld_cluster_f4(from + 16);
+                    y[0] += lo.x; y[1] += lo.y; y[2] += lo.z; y[3] += lo.w;
+                    y[4] += hi.x; y[5] += hi.y; y[6] += hi.z; y[7] += hi.w;
+                }
+                if (p.bias != nullptr) {
+                    const uint4 b = ldg128(p.bias + (size_t)tile.weights * p.N + f);
+                    y[0] += bf16_lo(b.x); y[1] += bf16_hi(b.x); y[2] += bf16_lo(b.y); y[3] += bf16_hi(b.y);
+                    y[4] += bf16_lo(b.z); y[5] += bf16_hi(b.z); y[6] += bf16_lo(b.w); y[7] += bf16_hi(b.w);
+                }
+                if (p.activation == REGIONE_ACT_GELU_TANH)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = gelu_tanh(y[e]);
+                uint4 o;
+                o.x = pack_bf16x2(y[0], y[1]); o.y = pack_bf16x2(y[2], y[3]);
+                o.z = pack_bf16x2(y[4], y[5]); o.w = pack_bf16x2(y[6], y[7]);
+                *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + q) * p.out_stride + f) = o;
+            }
+        }
+    }
+    ptx::tc_fence_before_sync();
+    if (cluster > 1) ptx::cluster_sync(); else __syncthreads();
+    ptx::tc_fence_after_sync();
+    if (warp == kIssuer) tmem_free512<PAIR>(tmem);
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------------------
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeFn grouped_encode_fn() {
+    static EncodeFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<EncodeFn>(f);
+    }();
+    return fn;
+}
+
+// Rows of K elements (4-bit ones as K / 2 bytes), `sets` of them, in boxes of 128 bytes by `box` rows.
+static bool grouped_map(CUtensorMap* map, bool fp4, int rank, const void* at, long long K, long long rows, long long sets,
+                        long long row_bytes, int box) {
+    EncodeFn fn = grouped_encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)(fp4 ? K / 2 : K), (cuuint64_t)rows, (cuuint64_t)sets};
+    const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)(row_bytes * rows)};
+    const cuuint32_t boxes[3] = {(cuuint32_t)(fp4 ? kChunkBytes : kChunkBytes / 2), (cuuint32_t)box, 1u}, ones[3] = {1u, 1u, 1u};
+    return fn(map, fp4 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(at), dims,
+              strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool FP4> static constexpr size_t grouped_smem(int stages) {
+    return 1024 + (size_t)stages * (kStageBytes + (FP4 ? kScaleA + kScaleB : 0)) + kEpiWarps * kStagingBytes + sizeof(GroupedControl);
+}
+
+template <bool FP4, bool PAIR> static bool grouped_configure(int dev) {
+    static int configured[kMaxDevices] = {};
+    if (__atomic_load_n(&configured[dev], __ATOMIC_ACQUIRE)) return true;
+    if (cudaFuncSetAttribute(grouped_kernel<FP4, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)grouped_smem<FP4>(kMaxStages)) !=
+        cudaSuccess)
+        return false;
+    __atomic_store_n(&configured[dev], 1, __ATOMIC_RELEASE);
+    return true;
+}
+
+template <bool FP4, bool PAIR>
+static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, unsigned blocks, int cluster, cudaStream_t st) {
+    const int dev = current_device();
+    if (dev < 0 || !grouped_configure<FP4, PAIR>(dev)) return REGIONE_CUDA_ERROR;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3((kEpiWarps + 2 + (FP4 ? kScaleWarps : 0)) * 32);
+    cfg.dynamicSmemBytes = grouped_smem<FP4>(p.stages);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return launch_status(launch_counted(&cfg, grouped_kernel<FP4, PAIR>, maps, p));
+}
+
+template <bool FP4>
+static int grouped_run(const void* x, long long x_row_bytes, const void* w, GroupedArgs p, cudaStream_t st) {
+    constexpr int kElems = FP4 ? 256 : 64;
+    const int sms = sm_count();
+    p.chunks = (p.K + kElems - 1) / kElems;
+    // Tiles of the largest width, if every row of the buffer is live: what a pair of CTAs each would have.
+    const long long groups = std::min(p.groups, p.rows_cap);
+    const long long f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
+    const long long pair_tiles = f_pairs * std::max<long long>(groups, p.rows_cap / 256);
+    const bool pair = pair_tiles * 2 > sms / 2;
+    p.slices = 1;
+    p.width = 16;
+    long long tiles = 0;
+    if (!pair) {
+        while (p.width < 128 && p.width * groups < p.rows_cap) p.width *= 2;
+        tiles = f_tiles * (p.rows_cap / p.width + groups);
+        while (p.slices < 8 && 2 * p.slices * tiles <= sms && 4 * p.slices <= p.chunks) p.slices *= 2;
+    }
+    p.stages = pair ? kMaxStages : std::max(2, std::min(kMaxStages, (p.chunks + p.slices - 1) / p.slices));
+    GroupedMaps maps;
+    bool ok = grouped_map(&maps.w, FP4, 3, w, p.K, p.N, p.n_weights, FP4 ? p.K / 2 : 2LL * p.K, 128);
+    for (int i = 0; i < kMaps && ok; ++i) ok = grouped_map(&maps.x[i], FP4, 2, x, p.K, p.rows_cap, 1, x_row_bytes, 16 << i);
+    if (!ok) return REGIONE_CUDA_ERROR;
+    if (pair) return grouped_launch<FP4, true>(maps, p, (unsigned)(sms / 2 * 2), 2, st);
+    return grouped_launch<FP4, false>(maps, p, (unsigned)(tiles * p.slices), p.slices, st);
+}
+
+}  // namespace regione
+
+using namespace regione;
+
+static int check_grouped(const void* x, const void* w, const void* bias, const void* begin, const void* end, int rows_cap, int groups,
+                         int n_weights, int K, int N, int activation, const void* out, long long out_stride) {
+    if (!w || (rows_cap && (!x || !out)) || (groups && (!begin || !end))) return REGIONE_INVALID_ARG;
+    if (rows_cap < 0 || groups < 0 || n_weights < 1 || K < 1 || N < 1) return REGIONE_INVALID_ARG;
+    if (activation != REGIONE_ACT_NONE && activation != REGIONE_ACT_GELU_TANH) return REGIONE_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(w) || !aligned16(out) || (bias && !aligned16(bias))) return REGIONE_INVALID_ARG;
+    if (out_stride < N) return REGIONE_INVALID_ARG;
+    if (N % 8 || out_stride % 8 || groups > kMaxGroups || n_weights > 65536 || K > (1 << 20) || N > (1 << 20) || rows_cap > (1 << 24))
+        return REGIONE_UNSUPPORTED;
+    // tiles are counted in 32 bits
+    if (((long long)rows_cap / 16 + groups) * ((N + kFeat - 1) / kFeat) >= 0x10000000LL) return REGIONE_UNSUPPORTED;
+    // the distance of two weight sets in a tensor map
+    if (2LL * K * N >= 1LL << 40) return REGIONE_UNSUPPORTED;
+    return REGIONE_OK;
+}
+
+extern "C" int regione_grouped_matmul(const regione_bf16* x, int64_t x_stride, const regione_bf16* w, const regione_bf16* bias,
+                                      const int32_t* row_begin, const int32_t* row_end, int rows_cap, int groups, int n_weights,
+                                      int K, int N, int activation, regione_bf16* out, int64_t out_stride, int32_t* dev_status,
+                                      void* stream) {
+    const int rc = check_grouped(x, w, bias, row_begin, row_end, rows_cap, groups, n_weights, K, N, activation, out, out_stride);
+    if (rc != REGIONE_OK) return rc;
+    if (x_stride < K) return REGIONE_INVALID_ARG;
+    if (K % 8 || x_stride % 8 || x_stride > (1LL << 32)) return REGIONE_UNSUPPORTED;
+    if (rows_cap == 0 || groups == 0) return REGIONE_OK;
+    GroupedArgs p = {};
+    p.row_begin = row_begin; p.row_end = row_end; p.groups = groups; p.n_weights = n_weights; p.rows_cap = rows_cap;
+    p.K = K; p.N = N; p.bias = bias; p.activation = activation; p.out = out; p.out_stride = out_stride; p.dev_status = dev_status;
+    return grouped_run<false>(x, 2 * x_stride, w, p, (cudaStream_t)stream);
+}
+
+extern "C" int regione_mxfp4_grouped_matmul(const uint8_t* x_q, const uint8_t* x_scale, const uint8_t* w_q, const uint8_t* w_scale,
+                                            const regione_bf16* bias, const int32_t* row_begin, const int32_t* row_end,
+                                            int rows_cap, int groups, int n_weights, int K, int N, int activation,
+                                            regione_bf16* out, int64_t out_stride, int32_t* dev_status, void* stream) {
+    const int rc = check_grouped(x_q, w_q, bias, row_begin, row_end, rows_cap, groups, n_weights, K, N, activation, out, out_stride);
+    if (rc != REGIONE_OK) return rc;
+    if ((rows_cap && !x_scale) || !w_scale || !aligned16(x_scale) || !aligned16(w_scale)) return REGIONE_INVALID_ARG;
+    if (K % 128) return REGIONE_UNSUPPORTED;
+    if (rows_cap == 0 || groups == 0) return REGIONE_OK;
+    GroupedArgs p = {};
+    p.row_begin = row_begin; p.row_end = row_end; p.groups = groups; p.n_weights = n_weights; p.rows_cap = rows_cap;
+    p.K = K; p.N = N; p.bias = bias; p.activation = activation; p.out = out; p.out_stride = out_stride; p.dev_status = dev_status;
+    p.x_scale = x_scale; p.w_scale = w_scale;
+    return grouped_run<true>(x_q, K / 2, w_q, p, (cudaStream_t)stream);
+}
