@@ -326,7 +326,7 @@ def rikv_load_e4m3(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_sta
 
 
 def _want(t, shape, name):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise RegionEError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
@@ -394,18 +394,24 @@ def rikv_load_mxfp4(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_st
         _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_rikv_load_mxfp4")
 
 
-def _rows(t, name):
-    """Device address and row distance of a bf16 CUDA matrix whose rows may lie apart."""
-    torch = _torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+def _rows(t, shape, dtype, name):
+    """Device address and row distance of a CUDA matrix of that shape whose rows may lie apart."""
+    rows, cols = shape
+    try:
+        if t.is_cuda and t.dtype == dtype and t.shape == shape:
+            step, unit = t.stride()
+            if unit == 1 and step >= cols and rows > 1:
+                return t.data_ptr(), step
+    except AttributeError:
+        pass
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise RegionEError(f"{name} must be a CUDA tensor")
-    if t.dtype != torch.bfloat16:
-        raise RegionEError(f"{name} must have dtype {torch.bfloat16}, got {t.dtype}")
-    rows, cols = t.shape
-    stride = t.stride(0) if rows > 1 else max(cols, 1)
-    if cols > 1 and t.stride(1) != 1 or stride < cols:
+    if t.dtype != dtype:
+        raise RegionEError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    _want(t, shape, name)
+    if cols > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < cols:
         raise RegionEError(f"the elements of a row of {name} must be contiguous and its rows apart")
-    return t.data_ptr(), stride
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols
 
 
 def grouped_matmul(x, w, row_begin, row_end, out, bias=None, activation=ACT_NONE, dev_status=None, stream=None):
@@ -417,11 +423,11 @@ def grouped_matmul(x, w, row_begin, row_end, out, bias=None, activation=ACT_NONE
     rows, K = x.shape
     sets, N, _ = w.shape
     _want(w, (sets, N, K), "w")
-    _want(out, (rows, N), "out")
     _want(row_end, row_begin.shape, "row_end")
     if bias is not None:
         _want(bias, (sets, N), "bias")
-    (xp, xs), (op, os_) = _rows(x, "x"), _rows(out, "out")
+    xp, xs = _rows(x, (rows, K), bf, "x")
+    op, os_ = _rows(out, (rows, N), bf, "out")
     _check(load().regione_grouped_matmul(
         xp, xs, _ptr(w, bf, "w"), _ptr(bias, bf, "bias"), _ptr(row_begin, i32, "row_begin"), _ptr(row_end, i32, "row_end"), rows,
         row_begin.numel(), sets, K, N, int(activation), op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)),
@@ -439,11 +445,10 @@ def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bi
     _want(x_scale, (rows, K // 32), "x_scale")
     _want(w_q, (sets, N, K // 2), "w_q")
     _want(w_scale, (sets, N, K // 32), "w_scale")
-    _want(out, (rows, N), "out")
     _want(row_end, row_begin.shape, "row_end")
     if bias is not None:
         _want(bias, (sets, N), "bias")
-    op, os_ = _rows(out, "out")
+    op, os_ = _rows(out, (rows, N), bf, "out")
     _check(load().regione_mxfp4_grouped_matmul(
         _ptr(x_q, u8, "x_q"), _ptr(x_scale, u8, "x_scale"), _ptr(w_q, u8, "w_q"), _ptr(w_scale, u8, "w_scale"),
         _ptr(bias, bf, "bias"), _ptr(row_begin, i32, "row_begin"), _ptr(row_end, i32, "row_end"), rows, row_begin.numel(), sets, K, N,

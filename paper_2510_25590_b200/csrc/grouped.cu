@@ -26,7 +26,7 @@ constexpr int kScaleA = 1024, kScaleB = 2048;         // scales of a stage: [2 o
 constexpr int kEpiWarps = 8;
 constexpr int kStagingBytes = 1024;                   // per epilogue warp: 16 rows of 32 features
 constexpr int kProducer = kEpiWarps, kIssuer = kEpiWarps + 1, kScaler = kEpiWarps + 2;
-constexpr int kScaleWarps = 4;
+constexpr int kScaleWarps = 8;
 constexpr long long kGroupedWait = 4000000000LL;      // cycles (about 2 s): bound of every wait
 constexpr int kMaps = 4;                              // boxes of 16, 32, 64 and 128 rows of x
 
@@ -134,6 +134,13 @@ __device__ __forceinline__ void load_x(uint32_t dst, const CUtensorMap* map, uin
                      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
 
+// Arrival on a barrier of this CTA or, through map_rank, of the pair's leader.  What it announces is read by the tensor core of this
+// SM (scales in its shared memory, behind a proxy fence; an accumulator, behind a tcgen05 fence), so that the scope is the CTA: at the
+// cluster's scope the arrival waits for every store of the warp that is on its way.
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // 16 lanes x 16 columns: thread l gets rows l / 4 and l / 4 + 8, columns 2 (l % 4) + {0, 1} and the same 8 further on.
 __device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -151,7 +158,7 @@ __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t a, uin
 // ---- waits: bounded; a wait that runs out is recorded and makes the other roles of the CTA give up -----------------
 __device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status) {
     const long long t0 = clock64();
-    while (!ptx::mbar_try_wait_cluster(bar, parity)) {
+    while (!ptx::mbar_try_wait(bar, parity)) {
         if (*abort_flag) return false;
         if (clock64() - t0 > kGroupedWait) {
             *abort_flag = 1;
@@ -162,14 +169,22 @@ __device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity,
     return true;
 }
 __device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, GroupedControl* ctl, int32_t* dev_status) {
-    return ptx::mbar_try_wait_cluster(bar, parity) || grouped_wait_slow(bar, parity, &ctl->abort_flag, dev_status);
+    return ptx::mbar_try_wait(bar, parity) || grouped_wait_slow(bar, parity, &ctl->abort_flag, dev_status);
 }
 
-// gelu(x) = x / 2 (1 + tanh(u)) = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3); the second form keeps its relative accuracy
-// where tanh(u) is near -1.
-__device__ __forceinline__ float gelu_tanh(float x) {
-    const float u = x * fmaf(0.044715f * 0.7978845608f, x * x, 0.7978845608f);
-    return __fdividef(x, 1.0f + fast_exp2(-2.8853900818f * u));
+// gelu(x) = x / 2 (1 + tanh(u)) = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3), of two values; the second form keeps its
+// relative accuracy where tanh(u) is near -1.  The two share a reciprocal, 1 / a = b / (a b): three results of the special
+// function unit, which sets the pace, in place of four.  exp(-2 u) is held at 2^62 so that a b stays finite: what is lost, from
+// x = -7.3 on, is below |x| 2^-62.
+__device__ __forceinline__ void gelu_tanh(float& x, float& y) {
+    constexpr float c = -2.0f * 1.4426950409f * 0.7978845608f;
+    const float e = fminf(fast_exp2(x * fmaf(c * 0.044715f, x * x, c)), 4.611686e18f);
+    const float f = fminf(fast_exp2(y * fmaf(c * 0.044715f, y * y, c)), 4.611686e18f);
+    const float a = 1.0f + e, b = 1.0f + f;
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a * b));
+    x *= b * r;
+    y *= a * r;
 }
 
 __device__ __forceinline__ int rows_of(const GroupedArgs& p, int g, int& begin) {
@@ -216,6 +231,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     constexpr int kElems = FP4 ? 256 : 64;            // of K in a chunk
     constexpr int kMaxWidth = PAIR ? (FP4 ? 224 : 256) : 128;
     constexpr int kAcc1 = PAIR ? kMaxWidth : 0;       // column of the second accumulator
+    constexpr int kScaleGroups = PAIR ? 3 : 2;         // of 32 rows, a warp of scales: 128 rows of W and up to 256 (128) of x, four warps to a chunk
     constexpr int kScaleCol = PAIR ? 448 : 128;       // columns of the scales: 2 x (8 of W, 16 of x)
     const uint32_t smem = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
     uint8_t* base = smem_raw + (smem - ptx::smem_addr(smem_raw));
@@ -229,7 +245,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            ptx::mbar_init(ptx::smem_addr(&ctl->full[s]), 1 + (FP4 ? (PAIR ? 2 : 1) : 0));
+            ptx::mbar_init(ptx::smem_addr(&ctl->full[s]), 1 + (FP4 ? kScaleWarps / 2 * (PAIR ? 2 : 1) : 0));
             ptx::mbar_init(ptx::smem_addr(&ctl->empty[s]), 1);
         }
         for (int a = 0; a < 2; ++a) {
@@ -249,8 +265,9 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     const int f_tiles = (p.N + (PAIR ? 2 : 1) * kFeat - 1) / ((PAIR ? 2 : 1) * kFeat);
     const int workers = PAIR ? gridDim.x / 2 : gridDim.x / cluster;
     if constexpr (PAIR) {
-        // Widths of 32 .. 256 (224) rows: one warp adds up the tiles of one width.  A round of tiles takes as long as its width, plus
-        // what a tile costs whatever its width; the width with the cheapest rounds is taken, the larger of equals.
+        // Widths of 32 .. 256 (224) rows: one warp adds up the tiles of one width.  A chunk of a tile takes the tensor core 2 cycles a row;
+        // its 128 + width / 2 rows of 128 bytes arrive at about 57 bytes a cycle.  The width with the cheapest rounds of tiles is
+        // taken, the larger of equals.  (4096 rows, K 4096, N 4096: rounds counted by width alone take 192, 123 us.)
         if (warp < kMaxWidth / 32) {
             const int width = 32 * (warp + 1);
             int n = 0;
@@ -260,7 +277,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             }
             n = __reduce_add_sync(0xffffffffu, n);
             const long long rounds = ((long long)n * f_tiles + workers - 1) / workers;
-            if (lane == 0) ctl->cost[warp] = (int)min(rounds * (max(width, 64) + 16), 0x7fffffffLL);
+            if (lane == 0) ctl->cost[warp] = (int)min(rounds * max(16 * width, 9 * (256 + width)), 0x7fffffffLL);
         }
         __syncthreads();
     }
@@ -321,17 +338,20 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             for (long long t = worker; t < total && ok; t += step) {
                 const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
                 const int half = PAIR ? tile.width / 2 : tile.width;
-                int box = 0;
-                while ((16 << box) < half) ++box;
-                const CUtensorMap* x_map = &maps.x[box];
-                const uint32_t bytes = (kTileBytes + (16u << box) * kChunkBytes) * (PAIR ? 2 : 1);
+                const uint32_t bytes = (kTileBytes + half * kChunkBytes) * (PAIR ? 2 : 1);
                 const int feature = tile.feature + (PAIR ? rank * kFeat : 0), row = tile.first + (PAIR ? rank * half : 0);
                 for (int c = c_begin; c < c_end; ++c) {
                     if (!grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
                     if (leader) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&ctl->full[s]), bytes);
                     const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * kStageBytes;
                     load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
-                    load_x<PAIR>(dst + kTileBytes, x_map, bar, c * (FP4 ? kChunkBytes : kElems), row);
+                    int at = 0;                                                  // boxes that make up the rows, the largest first
+#pragma unroll
+                    for (int box = kMaps - 1; box >= 0; --box)
+                        if (half & (16 << box)) {
+                            load_x<PAIR>(dst + kTileBytes + at * kChunkBytes, &maps.x[box], bar, c * (FP4 ? kChunkBytes : kElems), row + at);
+                            at += 16 << box;
+                        }
                     ++filled;
                     if (++s == p.stages) { s = 0; phase ^= 1; }
                 }
@@ -342,7 +362,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     uint32_t ph = phase;
                     if (q < 0) { q += p.stages; ph ^= 1; }
                     const long long t0 = clock64();
-                    while (!ptx::mbar_try_wait_cluster(ptx::smem_addr(&ctl->full[q]), ph) && clock64() - t0 < kGroupedWait / 8) {}
+                    while (!ptx::mbar_try_wait(ptx::smem_addr(&ctl->full[q]), ph) && clock64() - t0 < kGroupedWait / 8) {}
                 }
             }
         }
@@ -400,56 +420,81 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             if (!ok) {                                // products in flight end before tensor memory is given up
                 commit<PAIR>(ptx::smem_addr(&ctl->drain));
                 const long long t0 = clock64();
-                while (!ptx::mbar_try_wait_cluster(ptx::smem_addr(&ctl->drain), 0) && clock64() - t0 < kGroupedWait / 8) {}
+                while (!ptx::mbar_try_wait(ptx::smem_addr(&ctl->drain), 0) && clock64() - t0 < kGroupedWait / 8) {}
             }
         }
     } else if (FP4 && warp >= kScaler) {
-        // Scales of every fourth chunk: 8 bytes a row from device memory to the place in shared memory that the copy to tensor
-        // memory reads.
-        const int k32 = p.K / 32;
-        int seq = 0;                                  // chunks so far
-        bool ok = true;
-        for (long long t = worker; t < total && ok; t += step) {
-            const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
-            const int feature = tile.feature + (PAIR ? rank * kFeat : 0);
-            const uint8_t* w_base = p.w_scale + (size_t)tile.weights * p.N * k32;
-            for (int c = c_begin; c < c_end; ++c, ++seq) {
-                if ((seq & (kScaleWarps - 1)) != warp - kScaler) continue;
-                const int s = seq % p.stages;
-                const uint32_t phase = (seq / p.stages) & 1;
-                const bool two = (c + 1) * kElems <= p.K;                       // the chunk's second 128 elements are there
-                uint2 v[12];
+        // Scales: 8 bytes a row and chunk, from rows that lie K / 32 bytes apart to the places in shared memory that the copy to tensor
+        // memory reads.  Two teams of four warps take turns at parts of two chunks, 16 bytes a row; a warp has every fourth group of
+        // 32 rows.  (A team that waits for a stage is at most four chunks behind its last one and the ring has at least four stages:
+        // no phase of a barrier can be mistaken for the one two further on.)  Rows behind the matrices are read as their last one: their
+        // products are not stored.
+        const int k32 = p.K / 32, team = (warp - kScaler) >> 2, member = (warp - kScaler) & 3;
+        const bool vec = k32 % 16 == 0;
+        long long t = worker;
+        int c = c_begin, s = 0;
+        uint32_t phase = 0;
+        bool ok = true, fresh = true;                 // fresh: the next fetch is the first of its tile
+        const uint8_t* src[kScaleGroups];
+        auto fetch = [&](uint4 (&v)[kScaleGroups]) {
+            if (fresh) {
+                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+                const int feature = tile.feature + (PAIR ? rank * kFeat : 0);
 #pragma unroll
-                for (int i = 0; i < 12; ++i) {
-                    const int r = (i >> 2) * 128 - 128 + (lane >> 2) + 8 * (i & 3) + 32 * (lane & 3);   // row of W (below 0) or of x
-                    const uint8_t* src = nullptr;
-                    if (i < 4) {
-                        const int f = feature + r + 128;
-                        if (f < p.N) src = w_base + (size_t)f * k32;
-                    } else if (r < tile.width && tile.first + r < p.rows_cap) {
-                        src = p.x_scale + (size_t)(tile.first + r) * k32;
-                    }
-                    v[i] = make_uint2(0u, 0u);
-                    if (src != nullptr) {
-                        const uint32_t* q = reinterpret_cast<const uint32_t*>(src + (size_t)c * 8);
-                        v[i].x = __ldg(q);
-                        if (two) v[i].y = __ldg(q + 1);
-                    }
+                for (int i = 0; i < kScaleGroups; ++i) {
+                    const int group = member + 4 * i;                            // 4 groups of W, then those of x
+                    const int r = (group & 3) * 8 + (lane >> 2) + 32 * (lane & 3) + (group < 8 ? 0 : 128);
+                    src[i] = group < 4 ? p.w_scale + ((size_t)tile.weights * p.N + min(feature + r, p.N - 1)) * k32
+                                       : p.x_scale + (size_t)min(tile.first + r, p.rows_cap - 1) * k32;
                 }
-                ok = __all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status));
-                if (!ok) break;
-                uint32_t* sa = reinterpret_cast<uint32_t*>(scales + (size_t)s * (kScaleA + kScaleB));
-                uint32_t* sb = sa + kScaleA / 4;
+                fresh = false;
+            }
+            const int off = (c & ~1) * 8;
+            if (vec) {
 #pragma unroll
-                for (int i = 0; i < 12; ++i) {
-                    uint32_t* dst = i < 4 ? sa + 32 * i + lane : sb + ((i >> 2) - 1) * 128 + 32 * (i & 3) + lane;
-                    dst[0] = v[i].x;
-                    dst[i < 4 ? 128 : 256] = v[i].y;
+                for (int i = 0; i < kScaleGroups; ++i) v[i] = ldg128(src[i] + off);
+            } else {                                  // (words behind the row: its last one, for blocks that no product takes)
+#pragma unroll
+                for (int i = 0; i < kScaleGroups; ++i) {
+                    auto word = [&](int k) { return __ldg(reinterpret_cast<const uint32_t*>(src[i] + min(off + 4 * k, k32 - 4))); };
+                    v[i] = make_uint4(word(0), word(1), word(2), word(3));
+                }
+            }
+        };
+        auto advance = [&] {                          // to the next part, of whichever team
+            const int n = min(2 - (c & 1), c_end - c);
+            c += n;
+            s += n;
+            if (s >= p.stages) { s -= p.stages; phase ^= 1; }
+            if (c >= c_end) { c = c_begin; t += step; fresh = true; }
+        };
+        if (team == 1 && t < total) advance();
+        uint4 v[kScaleGroups];
+        if (t < total) fetch(v);
+        while (t < total && ok) {
+            const int first = c, n = min(2 - (c & 1), c_end - c);
+            int at = s;
+            uint32_t ph = phase;
+            for (int k = 0; k < n; ++k) {
+                ok = __all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->empty[at]), ph ^ 1, ctl, p.dev_status));
+                if (!ok) break;
+                uint32_t* sa = reinterpret_cast<uint32_t*>(scales + at * (kScaleA + kScaleB)) + lane;
+                const bool odd = (first + k) & 1;
+#pragma unroll
+                for (int i = 0; i < kScaleGroups; ++i) {
+                    const int group = member + 4 * i;
+                    uint32_t* dst = sa + (group < 4 ? 0 : kScaleA / 4 + (group < 8 ? 0 : 128)) + (group & 3) * 32;
+                    dst[0] = odd ? v[i].z : v[i].x;
+                    dst[group < 4 ? 128 : 256] = odd ? v[i].w : v[i].y;
                 }
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive_cluster(bar_at(&ctl->full[s]));
+                if (lane == 0) arrive_at(bar_at(&ctl->full[at]));
+                if (++at == p.stages) { at = 0; ph ^= 1; }
             }
+            advance();
+            if (t < total) advance();
+            if (t < total) fetch(v);
         }
     } else if (warp < kEpiWarps) {
         const int sub = warp & 3, part = warp >> 2;
@@ -480,17 +525,22 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     for (int i = 0; i < 16; ++i) sums[(c + i) * kFeat + 32 * sub + lane] = __uint_as_float(r[i]);
                 }
             } else {
+                // 16 rows at a time, the next ones on their way out of tensor memory meanwhile
+                uint32_t ahead[16];
+                auto fetch = [&](int c) {
+                    tmem_ld_16x256b_x2(acc + c, ahead);
+                    tmem_ld_16x256b_x2(acc + (16u << 16) + c, ahead + 8);
+                };
+                if (part * 16 < tile.live) fetch(part * 16);
                 for (int c = part * 16; c < tile.live; c += 32) {
-                    uint32_t r[16];
-                    tmem_ld_16x256b_x2(acc + c, r);
-                    tmem_ld_16x256b_x2(acc + (16u << 16) + c, r + 8);
-                    ptx::tmem_wait_ld();
                     float y[16];
+                    ptx::tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        y[i] = __uint_as_float(r[i]) + bias[(i >> 3) * 2 + ((i >> 1) & 1)];
-                        if (p.activation == REGIONE_ACT_GELU_TANH) y[i] = gelu_tanh(y[i]);
-                    }
+                    for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(ahead[i]) + bias[(i >> 3) * 2 + ((i >> 1) & 1)];
+                    if (c + 32 < tile.live) fetch(c + 32);
+                    if (p.activation == REGIONE_ACT_GELU_TANH)
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) gelu_tanh(y[i], y[i + 1]);
                     // row of the tile t at 64 t, its 16-byte pieces (8 features) turned by t / 2 so that eight rows meet eight banks
                     const int row = (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1, turn = (row >> 1) & 3;
                     stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
@@ -510,7 +560,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             }
             ptx::tc_fence_before_sync();
             __syncwarp();
-            if (PAIR && lane == 0) ptx::mbar_arrive_cluster(bar_at(&ctl->acc_empty[a]));
+            if (PAIR && lane == 0) arrive_at(bar_at(&ctl->acc_empty[a]));
         }
     }
 
@@ -539,7 +589,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 }
                 if (p.activation == REGIONE_ACT_GELU_TANH)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = gelu_tanh(y[e]);
+                    for (int e = 0; e < 8; e += 2) gelu_tanh(y[e], y[e + 1]);
                 uint4 o;
                 o.x = pack_bf16x2(y[0], y[1]); o.y = pack_bf16x2(y[2], y[3]);
                 o.z = pack_bf16x2(y[4], y[5]); o.w = pack_bf16x2(y[6], y[7]);
@@ -635,10 +685,12 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
         tiles = f_tiles * (p.rows_cap / p.width + groups);
         while (p.slices < 8 && 2 * p.slices * tiles <= sms && 4 * p.slices <= p.chunks) p.slices *= 2;
     }
-    p.stages = pair ? kMaxStages : std::max(2, std::min(kMaxStages, (p.chunks + p.slices - 1) / p.slices));
+    // (at least four: see the scales)
+    p.stages = pair ? kMaxStages : std::max(4, std::min(kMaxStages, (p.chunks + p.slices - 1) / p.slices));
     GroupedMaps maps;
     bool ok = grouped_map(&maps.w, FP4, 3, w, p.K, p.N, p.n_weights, FP4 ? p.K / 2 : 2LL * p.K, 128);
-    for (int i = 0; i < kMaps && ok; ++i) ok = grouped_map(&maps.x[i], FP4, 2, x, p.K, p.rows_cap, 1, x_row_bytes, 16 << i);
+    for (int i = 0; i < kMaps && ok && (pair || (16 << i) <= p.width); ++i)
+        ok = grouped_map(&maps.x[i], FP4, 2, x, p.K, p.rows_cap, 1, x_row_bytes, 16 << i);
     if (!ok) return REGIONE_CUDA_ERROR;
     if (pair) return grouped_launch<FP4, true>(maps, p, (unsigned)(sms / 2 * 2), 2, st);
     return grouped_launch<FP4, false>(maps, p, (unsigned)(tiles * p.slices), p.slices, st);
