@@ -317,7 +317,7 @@ int regione_rikv_load_mxfp4(const uint8_t* k_q, const uint8_t* v_q, const uint8_
  * [n_weights, N] or NULL; row_begin, row_end dev int32 [groups]; out dev bf16 [rows_cap, N], rows out_stride
  * elements apart.  Groups may be empty, rows may be in no group (theirs of out are left untouched), no row
  * may be in two; a range that is not within [0, rows_cap] is cut to it and REGIONE_DEV_BOUNDS recorded.
- * out may not overlap x or w.  K, N and the strides are multiples of 8, groups <= 1024, x, w, bias and out
+ * out may not overlap x or w.  K, N and the strides are multiples of 8, groups <= 512, x, w, bias and out
  * 16-byte aligned.  activation: REGIONE_ACT_NONE, or REGIONE_ACT_GELU_TANH,
  * act(y) = y / 2 (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))).  One kernel launch; nothing is allocated.
  *

@@ -19,14 +19,15 @@ namespace regione {
 constexpr int kFeat = 128;                            // features a CTA
 constexpr int kChunkBytes = 128;                      // of K: 64 bf16 or 256 4-bit elements, one swizzle row
 constexpr int kTileBytes = 128 * kChunkBytes;         // 128 rows of either operand
-constexpr int kStageBytes = 2 * kTileBytes;           // features, rows
 constexpr int kMaxStages = 6;
-constexpr int kMaxGroups = 1024;
+constexpr int kMaxGroups = 512;
 constexpr int kScaleA = 1024, kScaleB = 2048;         // scales of a stage: [2 of 128 elements][1 or 2 of 128 rows][512 bytes]
-constexpr int kEpiWarps = 8;
+// Warps of a CTA: 8 (4) that take sums out of tensor memory, one that loads, one that issues products, and with 4-bit operands 8 (4) that
+// bring the scales: a pair of CTAs fills its SMs, CTAs without a pair leave room for a second one.
+template <bool FP4, bool PAIR> struct Roles {
+    static constexpr int kEpi = PAIR ? 8 : 4, kScale = PAIR ? 8 : 4, kThreads = (kEpi + 2 + (FP4 ? kScale : 0)) * 32;
+};
 constexpr int kStagingBytes = 1024;                   // per epilogue warp: 16 rows of 32 features
-constexpr int kProducer = kEpiWarps, kIssuer = kEpiWarps + 1, kScaler = kEpiWarps + 2;
-constexpr int kScaleWarps = 8;
 constexpr long long kGroupedWait = 4000000000LL;      // cycles (about 2 s): bound of every wait
 constexpr int kMaps = 4;                              // boxes of 16, 32, 64 and 128 rows of x
 
@@ -34,7 +35,8 @@ struct GroupedArgs {
     const int32_t *row_begin, *row_end;
     int groups, n_weights, rows_cap, K, N;
     int chunks;                                       // of K
-    int stages;
+    int stages, stage_bytes;                          // a stage: 128 rows of W, then those of x
+    int tmem_columns, scale_column;
     int slices;                                       // of K, one per CTA of a cluster (the kernel without pairs)
     int width;                                        // rows of a tile at most (the kernel without pairs)
     const uint16_t* bias;                             // [n_weights, N] or NULL
@@ -47,6 +49,7 @@ struct GroupedArgs {
 struct GroupedMaps {
     CUtensorMap w;                                    // (K, N, n_weights), box 128 bytes x 128 rows
     CUtensorMap x[kMaps];                             // (K, rows), box 128 bytes x 16 << i rows
+    CUtensorMap out;                                  // (N, rows), box 32 features x 16 rows
 };
 
 struct GroupedControl {
@@ -55,26 +58,27 @@ struct GroupedControl {
     int abort_flag;
     int width, total;                                 // of the plan: rows of a tile at most, tiles
     int cost[8];
-    int first[kMaxGroups + 1];                        // first tile of a group (in units of its feature tiles' row tiles)
+    int first[kMaxGroups + 1];                        // of a group: row tiles ahead of it,
+    int begin[kMaxGroups], rows[kMaxGroups];          // its first row, how many
 };
 
 // ---- instructions that the pair of CTAs and the scaled product need -------------------------------------------
 namespace {
 
-template <bool PAIR> __device__ __forceinline__ void tmem_alloc512(uint32_t slot) {
-    if constexpr (PAIR)
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(slot) : "memory");
-    else
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(slot) : "memory");
-}
-template <bool PAIR> __device__ __forceinline__ void tmem_free512(uint32_t taddr) {
+template <bool PAIR> __device__ __forceinline__ void take_tmem(uint32_t slot, uint32_t columns) {
     if constexpr (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(taddr) : "memory");
     } else {
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(taddr) : "memory");
+        ptx::tmem_alloc(slot, columns);
+        ptx::tmem_relinquish();
     }
+}
+template <bool PAIR> __device__ __forceinline__ void free_tmem(uint32_t taddr, uint32_t columns) {
+    if constexpr (PAIR)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(columns) : "memory");
+    else
+        ptx::tmem_dealloc(taddr, columns);
 }
 
 template <bool PAIR, bool FP4>
@@ -141,6 +145,12 @@ __device__ __forceinline__ void arrive_at(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// 16 rows of 32 features from shared memory (64-byte swizzle) to the output; what lies behind the last feature is not written.
+__device__ __forceinline__ void store_out(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(c0), "r"(c1) : "memory");
+}
+
 // 16 lanes x 16 columns: thread l gets rows l / 4 and l / 4 + 8, columns 2 (l % 4) + {0, 1} and the same 8 further on.
 __device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -172,25 +182,50 @@ __device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, Grou
     return ptx::mbar_try_wait(bar, parity) || grouped_wait_slow(bar, parity, &ctl->abort_flag, dev_status);
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void parts_of(uint64_t p, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // gelu(x) = x / 2 (1 + tanh(u)) = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3), of two values; the second form keeps its
 // relative accuracy where tanh(u) is near -1.  The two share a reciprocal, 1 / a = b / (a b): three results of the special
 // function unit, which sets the pace, in place of four.  exp(-2 u) is held at 2^62 so that a b stays finite: what is lost, from
 // x = -7.3 on, is below |x| 2^-62.
-__device__ __forceinline__ void gelu_tanh(float& x, float& y) {
+__device__ __forceinline__ uint64_t gelu_tanh(uint64_t x) {
     constexpr float c = -2.0f * 1.4426950409f * 0.7978845608f;
-    const float e = fminf(fast_exp2(x * fmaf(c * 0.044715f, x * x, c)), 4.611686e18f);
-    const float f = fminf(fast_exp2(y * fmaf(c * 0.044715f, y * y, c)), 4.611686e18f);
-    const float a = 1.0f + e, b = 1.0f + f;
-    float r;
+    const uint64_t t = mul2(x, fma2(mul2(x, x), pair_of(c * 0.044715f, c * 0.044715f), pair_of(c, c)));
+    float e, f, a, b, r;
+    parts_of(t, e, f);
+    const uint64_t d = add2(pair_of(fminf(fast_exp2(e), 4.611686e18f), fminf(fast_exp2(f), 4.611686e18f)), pair_of(1.0f, 1.0f));
+    parts_of(d, a, b);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a * b));
-    x *= b * r;
-    y *= a * r;
+    return mul2(mul2(x, pair_of(b, a)), pair_of(r, r));
 }
 
-__device__ __forceinline__ int rows_of(const GroupedArgs& p, int g, int& begin) {
+// A group's rows within the buffer; false: the range as given is not within it.
+__device__ __forceinline__ bool rows_of(const GroupedArgs& p, int g, int& begin, int& rows) {
     const int b = p.row_begin[g], e = p.row_end[g];
     begin = min(max(b, 0), p.rows_cap);
-    return max(min(e, p.rows_cap) - begin, 0);
+    rows = max(min(e, p.rows_cap) - begin, 0);
+    return b >= 0 && e <= p.rows_cap && b <= e;
 }
 
 // Rows [first, first + live) of a group against a feature tile; `width` = columns of the product.
@@ -198,44 +233,41 @@ struct GroupedTile {
     int first, live, width, weights, feature;
 };
 
-// Tile t of the plan.  Tiles of a group run through eight feature tiles before they go on to the next rows, so that the tiles in
-// flight at one time share both operands.  PAIR: 256 features, widths in steps of 32.
+// Tile t of the plan, t not smaller than at the last call; `group` is where that one was.  Tiles of a group run through eight feature
+// tiles before they go on to the next rows, so that the tiles in flight at one time share both operands.  PAIR: 256 features,
+// widths in steps of 32.
 template <bool PAIR>
-__device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const GroupedControl* ctl, int t, int f_tiles) {
-    int lo = 0, hi = p.groups;                        // last group whose first tile is not behind t
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((long long)ctl->first[mid] * f_tiles <= t) lo = mid; else hi = mid;
-    }
-    int begin;
-    const int rows = rows_of(p, lo, begin), n = ctl->first[lo + 1] - ctl->first[lo];
-    int in = t - ctl->first[lo] * f_tiles;
-    const int block = in / (8 * n);
+__device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const GroupedControl* ctl, int t, int f_tiles, int& group) {
+    while (ctl->first[group + 1] * f_tiles <= t) ++group;
+    const int ahead = ctl->first[group], n = ctl->first[group + 1] - ahead, rows = ctl->rows[group];
+    int in = t - ahead * f_tiles;
+    const int block = f_tiles <= 8 ? 0 : in / (8 * n);
     in -= block * 8 * n;
     const int wide = min(8, f_tiles - block * 8), at = in / wide;
     constexpr int kStep = PAIR ? 32 : 16;
-    const int width = ((rows + n - 1) / n + kStep - 1) / kStep * kStep;       // n even tiles
+    const int width = ((rows + n - 1) / n + kStep - 1) & ~(kStep - 1);         // n even tiles
     GroupedTile tile;
-    tile.first = begin + at * width;
+    tile.first = ctl->begin[group] + at * width;
     tile.live = min(width, rows - at * width);
     tile.width = width;
-    tile.weights = lo % p.n_weights;
+    tile.weights = group % p.n_weights;
     tile.feature = (block * 8 + in - at * wide) * (PAIR ? 2 : 1) * kFeat;
     return tile;
 }
 
 template <bool FP4, bool PAIR>
-__global__ void __launch_bounds__((kEpiWarps + 2 + (FP4 ? kScaleWarps : 0)) * 32, 1)
+__global__ void __launch_bounds__(Roles<FP4, PAIR>::kThreads, PAIR ? 1 : 2)
 grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__ GroupedArgs p) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     constexpr int kElems = FP4 ? 256 : 64;            // of K in a chunk
     constexpr int kMaxWidth = PAIR ? (FP4 ? 224 : 256) : 128;
     constexpr int kAcc1 = PAIR ? kMaxWidth : 0;       // column of the second accumulator
+    constexpr int kEpiWarps = Roles<FP4, PAIR>::kEpi, kScaleWarps = Roles<FP4, PAIR>::kScale;
+    constexpr int kProducer = kEpiWarps, kIssuer = kEpiWarps + 1, kScaler = kEpiWarps + 2;
     constexpr int kScaleGroups = PAIR ? 3 : 2;         // of 32 rows, a warp of scales: 128 rows of W and up to 256 (128) of x, four warps to a chunk
-    constexpr int kScaleCol = PAIR ? 448 : 128;       // columns of the scales: 2 x (8 of W, 16 of x)
     const uint32_t smem = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
     uint8_t* base = smem_raw + (smem - ptx::smem_addr(smem_raw));
-    uint8_t* scales = base + (size_t)p.stages * kStageBytes;
+    uint8_t* scales = base + (size_t)p.stages * p.stage_bytes;
     uint8_t* staging = scales + (FP4 ? (size_t)p.stages * (kScaleA + kScaleB) : 0);
     GroupedControl* ctl = reinterpret_cast<GroupedControl*>(staging + kEpiWarps * kStagingBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -245,7 +277,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            ptx::mbar_init(ptx::smem_addr(&ctl->full[s]), 1 + (FP4 ? kScaleWarps / 2 * (PAIR ? 2 : 1) : 0));
+            ptx::mbar_init(ptx::smem_addr(&ctl->full[s]), 1 + (FP4 ? 4 * (PAIR ? 2 : 1) : 0));
             ptx::mbar_init(ptx::smem_addr(&ctl->empty[s]), 1);
         }
         for (int a = 0; a < 2; ++a) {
@@ -256,7 +288,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         ctl->abort_flag = 0;
         ptx::fence_barrier_init();
     }
-    if (warp == kIssuer) tmem_alloc512<PAIR>(ptx::smem_addr(&ctl->tmem));
+    if (warp == kIssuer) take_tmem<PAIR>(ptx::smem_addr(&ctl->tmem), p.tmem_columns);
     if (warp == kProducer && lane == 0) ptx::prefetch_tensormap(&maps.w);
     grid_dependency_wait();
     grid_launch_dependents();
@@ -272,8 +304,9 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             const int width = 32 * (warp + 1);
             int n = 0;
             for (int g = lane; g < p.groups; g += 32) {
-                int begin;
-                n += (rows_of(p, g, begin) + width - 1) / width;
+                int begin, rows;
+                rows_of(p, g, begin, rows);
+                n += (rows + width - 1) / width;
             }
             n = __reduce_add_sync(0xffffffffu, n);
             const long long rounds = ((long long)n * f_tiles + workers - 1) / workers;
@@ -294,11 +327,11 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             const int g = g0 + lane;
             int n = 0;
             if (g < p.groups) {
-                int begin;
-                const int rows = rows_of(p, g, begin);
+                int begin, rows;
+                if (!rows_of(p, g, begin, rows) && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
                 n = (rows + width - 1) / width;
-                if (blockIdx.x == 0 && (p.row_begin[g] < 0 || p.row_end[g] > p.rows_cap || p.row_end[g] < p.row_begin[g]))
-                    record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+                ctl->begin[g] = begin;
+                ctl->rows[g] = rows;
             }
             int sum = n;
             for (int d = 1; d < 32; d <<= 1) {
@@ -325,6 +358,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     // chunks of K that this CTA takes
     const int c_begin = PAIR ? 0 : (int)((long long)p.chunks * rank / p.slices);
     const int c_end = PAIR ? p.chunks : (int)((long long)p.chunks * (rank + 1) / p.slices);
+    int group = 0;                                    // of this thread's last tile
     auto bar_at = [&](const uint64_t* bar) {          // a barrier of the leader
         const uint32_t a = ptx::smem_addr(bar);
         return PAIR ? ptx::map_rank(a, 0) : a;
@@ -336,14 +370,14 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             uint32_t phase = 0;
             bool ok = true;
             for (long long t = worker; t < total && ok; t += step) {
-                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
                 const int half = PAIR ? tile.width / 2 : tile.width;
                 const uint32_t bytes = (kTileBytes + half * kChunkBytes) * (PAIR ? 2 : 1);
                 const int feature = tile.feature + (PAIR ? rank * kFeat : 0), row = tile.first + (PAIR ? rank * half : 0);
                 for (int c = c_begin; c < c_end; ++c) {
                     if (!grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
                     if (leader) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&ctl->full[s]), bytes);
-                    const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * kStageBytes;
+                    const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * p.stage_bytes;
                     load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
                     int at = 0;                                                  // boxes that make up the rows, the largest first
 #pragma unroll
@@ -374,7 +408,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             uint32_t phase = 0;
             bool ok = true;
             for (long long t = worker; t < total && ok; t += step, ++it) {
-                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
                 const int a = PAIR ? it & 1 : 0;
                 const uint32_t d = tmem + (a ? kAcc1 : 0);
                 if (it >= 2 && !grouped_wait(ptx::smem_addr(&ctl->acc_empty[a]), ((it >> 1) - 1) & 1, ctl, p.dev_status)) { ok = false; break; }
@@ -386,11 +420,11 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 for (int c = c_begin; c < c_end; ++c) {
                     if (!grouped_wait(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
                     ptx::tc_fence_after_sync();
-                    const uint32_t at = smem + s * kStageBytes;
+                    const uint32_t at = smem + s * p.stage_bytes;
                     const uint32_t a_lo = ptx::smem_desc_lo(at, 16), b_lo = ptx::smem_desc_lo(at + kTileBytes, 16);
                     uint32_t sfa = 0, sfb = 0;
                     if constexpr (FP4) {
-                        sfa = tmem + kScaleCol + sf * 32;
+                        sfa = tmem + p.scale_column + sf * 32;
                         sfb = sfa + 8;
                         sf ^= 1;
                         const uint32_t sa = ptx::smem_addr(scales) + s * (kScaleA + kScaleB), sb = sa + kScaleA;
@@ -425,10 +459,12 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         }
     } else if (FP4 && warp >= kScaler) {
         // Scales: 8 bytes a row and chunk, from rows that lie K / 32 bytes apart to the places in shared memory that the copy to tensor
-        // memory reads.  Two teams of four warps take turns at parts of two chunks, 16 bytes a row; a warp has every fourth group of
-        // 32 rows.  (A team that waits for a stage is at most four chunks behind its last one and the ring has at least four stages:
-        // no phase of a barrier can be mistaken for the one two further on.)  Rows behind the matrices are read as their last one: their
-        // products are not stored.
+        // memory reads.  A team of four warps takes a part of two chunks, 16 bytes a row; a pair of CTAs has two teams in turn, which is
+        // 8192^3 in 249 -> 214 us, and with 32 bytes a row in registers and no turns 221.  A warp has every fourth group of 32 rows.
+        // (The stage that a team waits for is at most four chunks behind its last one and the ring has at least four stages: no phase of
+        // a barrier can be mistaken for the one two further on.)  Rows behind the matrices are read as their last one: their products
+        // are not stored.
+        constexpr int kTeams = kScaleWarps / 4;
         const int k32 = p.K / 32, team = (warp - kScaler) >> 2, member = (warp - kScaler) & 3;
         const bool vec = k32 % 16 == 0;
         long long t = worker;
@@ -438,13 +474,13 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         const uint8_t* src[kScaleGroups];
         auto fetch = [&](uint4 (&v)[kScaleGroups]) {
             if (fresh) {
-                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
                 const int feature = tile.feature + (PAIR ? rank * kFeat : 0);
 #pragma unroll
                 for (int i = 0; i < kScaleGroups; ++i) {
-                    const int group = member + 4 * i;                            // 4 groups of W, then those of x
-                    const int r = (group & 3) * 8 + (lane >> 2) + 32 * (lane & 3) + (group < 8 ? 0 : 128);
-                    src[i] = group < 4 ? p.w_scale + ((size_t)tile.weights * p.N + min(feature + r, p.N - 1)) * k32
+                    const int part = member + 4 * i;                            // 4 groups of W, then those of x
+                    const int r = (part & 3) * 8 + (lane >> 2) + 32 * (lane & 3) + (part < 8 ? 0 : 128);
+                    src[i] = part < 4 ? p.w_scale + ((size_t)tile.weights * p.N + min(feature + r, p.N - 1)) * k32
                                        : p.x_scale + (size_t)min(tile.first + r, p.rows_cap - 1) * k32;
                 }
                 fresh = false;
@@ -468,7 +504,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             if (s >= p.stages) { s -= p.stages; phase ^= 1; }
             if (c >= c_end) { c = c_begin; t += step; fresh = true; }
         };
-        if (team == 1 && t < total) advance();
+        if (kTeams == 2 && team == 1 && t < total) advance();
         uint4 v[kScaleGroups];
         if (t < total) fetch(v);
         while (t < total && ok) {
@@ -482,10 +518,10 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 const bool odd = (first + k) & 1;
 #pragma unroll
                 for (int i = 0; i < kScaleGroups; ++i) {
-                    const int group = member + 4 * i;
-                    uint32_t* dst = sa + (group < 4 ? 0 : kScaleA / 4 + (group < 8 ? 0 : 128)) + (group & 3) * 32;
+                    const int part = member + 4 * i;
+                    uint32_t* dst = sa + (part < 4 ? 0 : kScaleA / 4 + (part < 8 ? 0 : 128)) + (part & 3) * 32;
                     dst[0] = odd ? v[i].z : v[i].x;
-                    dst[group < 4 ? 128 : 256] = odd ? v[i].w : v[i].y;
+                    dst[part < 4 ? 128 : 256] = odd ? v[i].w : v[i].y;
                 }
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
@@ -493,22 +529,25 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 if (++at == p.stages) { at = 0; ph ^= 1; }
             }
             advance();
-            if (t < total) advance();
+            if (kTeams == 2 && t < total) advance();
             if (t < total) fetch(v);
         }
     } else if (warp < kEpiWarps) {
+        constexpr int kEpiCols = 16 * (kEpiWarps / 4);
         const int sub = warp & 3, part = warp >> 2;
         const uint32_t stage = ptx::smem_addr(staging) + warp * kStagingBytes;
         int it = 0;
         for (long long t = worker; t < total; t += step, ++it) {
-            const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles);
+            const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
             const int a = PAIR ? it & 1 : 0;
             const int feature = tile.feature + (PAIR ? rank * kFeat : 0) + 32 * sub;
-            float bias[4] = {0.f, 0.f, 0.f, 0.f};     // of features lane / 4 + {0, 8, 16, 24}
+            uint64_t bias[4] = {0, 0, 0, 0};          // of features lane / 4 + {0, 8, 16, 24}, twice each
             if (p.bias != nullptr && (PAIR || p.slices == 1))
+#pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int f = feature + (lane >> 2) + 8 * i;
-                    if (f < p.N) bias[i] = __uint_as_float((uint32_t)p.bias[(size_t)tile.weights * p.N + f] << 16);
+                    const int f = min(feature + (lane >> 2) + 8 * i, p.N - 1);
+                    const float b = __uint_as_float((uint32_t)__ldg(p.bias + (size_t)tile.weights * p.N + f) << 16);
+                    bias[i] = pair_of(b, b);
                 }
             if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->acc_full[a]), (PAIR ? it >> 1 : 0) & 1, ctl, p.dev_status)))
                 break;
@@ -517,7 +556,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             if (!PAIR && p.slices > 1) {
                 // this slice's sums as [row][128 features] fp32 over the stages, which nothing reads any more
                 float* sums = reinterpret_cast<float*>(base);
-                for (int c = part * 16; c < tile.live; c += 32) {
+                for (int c = part * 16; c < tile.live; c += kEpiCols) {
                     uint32_t r[16];
                     ptx::tmem_ld16(acc + c, r);
                     ptx::tmem_wait_ld();
@@ -532,36 +571,56 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     tmem_ld_16x256b_x2(acc + (16u << 16) + c, ahead + 8);
                 };
                 if (part * 16 < tile.live) fetch(part * 16);
-                for (int c = part * 16; c < tile.live; c += 32) {
-                    float y[16];
+                for (int c = part * 16; c < tile.live; c += kEpiCols) {
+                    uint64_t y[8];                                               // two rows of one feature
                     ptx::tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(ahead[i]) + bias[(i >> 3) * 2 + ((i >> 1) & 1)];
-                    if (c + 32 < tile.live) fetch(c + 32);
+                    for (int i = 0; i < 8; ++i)
+                        y[i] = add2(pair_of(__uint_as_float(ahead[2 * i]), __uint_as_float(ahead[2 * i + 1])), bias[(i >> 2) * 2 + (i & 1)]);
+                    if (c + kEpiCols < tile.live) fetch(c + kEpiCols);
                     if (p.activation == REGIONE_ACT_GELU_TANH)
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) gelu_tanh(y[i], y[i + 1]);
+                        for (int i = 0; i < 8; ++i) y[i] = gelu_tanh(y[i]);
+                    uint32_t z[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float lo, hi;
+                        parts_of(y[i], lo, hi);
+                        z[i] = pack_bf16x2(lo, hi);
+                    }
                     // row of the tile t at 64 t, its 16-byte pieces (8 features) turned by t / 2 so that eight rows meet eight banks
                     const int row = (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1, turn = (row >> 1) & 3;
-                    stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
-                                      pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-                    stmatrix_x4_trans(stage + row * 64 + (((piece + 2) ^ turn) << 4), pack_bf16x2(y[8], y[9]),
-                                      pack_bf16x2(y[10], y[11]), pack_bf16x2(y[12], y[13]), pack_bf16x2(y[14], y[15]));
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int q = (lane >> 2) + 8 * i, j = lane & 3;
-                        const uint4 v = *reinterpret_cast<const uint4*>(staging + warp * kStagingBytes + q * 64 + ((j ^ ((q >> 1) & 3)) << 4));
-                        if (c + q < tile.live && feature + 8 * j < p.N)
-                            *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + c + q) * p.out_stride + feature + 8 * j) = v;
+                    if (PAIR) {                                                  // (the store of the step before)
+                        if (lane == 0) ptx::bulk_wait_read<0>();
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), z[0], z[1], z[2], z[3]);
+                    stmatrix_x4_trans(stage + row * 64 + (((piece + 2) ^ turn) << 4), z[4], z[5], z[6], z[7]);
+                    if (PAIR && c + 16 <= tile.live) {
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0 && feature < p.N) {
+                            store_out(&maps.out, stage, feature, tile.first + c);
+                            ptx::bulk_commit();
+                        }
+                    } else {
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int q = (lane >> 2) + 8 * i, j = lane & 3;
+                            const uint4 v = *reinterpret_cast<const uint4*>(staging + warp * kStagingBytes + q * 64 + ((j ^ ((q >> 1) & 3)) << 4));
+                            if (c + q < tile.live && feature + 8 * j < p.N)
+                                *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + c + q) * p.out_stride + feature + 8 * j) = v;
+                        }
+                        __syncwarp();
+                    }
                 }
             }
             ptx::tc_fence_before_sync();
             __syncwarp();
             if (PAIR && lane == 0) arrive_at(bar_at(&ctl->acc_empty[a]));
         }
+        if (PAIR && lane == 0) ptx::bulk_wait_all();
     }
 
     // ---- the slices of a tile meet --------------------------------------------------------------------------------------
@@ -569,7 +628,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     if (!PAIR && p.slices > 1) {
         ptx::cluster_sync();
         if (warp < kEpiWarps && worker < total && !ctl->abort_flag) {
-            const GroupedTile tile = tile_at<PAIR>(p, ctl, worker, f_tiles);
+            const GroupedTile tile = tile_at<PAIR>(p, ctl, worker, f_tiles, group);
             // pieces of 8 features of a row, dealt over the cluster's threads; slices are added in their order
             for (int u = threadIdx.x * p.slices + rank; u < tile.live * (kFeat / 8); u += kEpiWarps * 32 * p.slices) {
                 const int q = u / (kFeat / 8), j = u % (kFeat / 8), f = tile.feature + 8 * j;
@@ -589,7 +648,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 }
                 if (p.activation == REGIONE_ACT_GELU_TANH)
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2) gelu_tanh(y[e], y[e + 1]);
+                    for (int e = 0; e < 8; e += 2) parts_of(gelu_tanh(pair_of(y[e], y[e + 1])), y[e], y[e + 1]);
                 uint4 o;
                 o.x = pack_bf16x2(y[0], y[1]); o.y = pack_bf16x2(y[2], y[3]);
                 o.z = pack_bf16x2(y[4], y[5]); o.w = pack_bf16x2(y[6], y[7]);
@@ -600,7 +659,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     ptx::tc_fence_before_sync();
     if (cluster > 1) ptx::cluster_sync(); else __syncthreads();
     ptx::tc_fence_after_sync();
-    if (warp == kIssuer) tmem_free512<PAIR>(tmem);
+    if (warp == kIssuer) free_tmem<PAIR>(tmem, p.tmem_columns);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
@@ -633,14 +692,14 @@ static bool grouped_map(CUtensorMap* map, bool fp4, int rank, const void* at, lo
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool FP4> static constexpr size_t grouped_smem(int stages) {
-    return 1024 + (size_t)stages * (kStageBytes + (FP4 ? kScaleA + kScaleB : 0)) + kEpiWarps * kStagingBytes + sizeof(GroupedControl);
+template <bool FP4, bool PAIR> static size_t grouped_smem(int stages, int stage_bytes) {
+    return 1024 + (size_t)stages * (stage_bytes + (FP4 ? kScaleA + kScaleB : 0)) + Roles<FP4, PAIR>::kEpi * kStagingBytes + sizeof(GroupedControl);
 }
 
 template <bool FP4, bool PAIR> static bool grouped_configure(int dev) {
     static int configured[kMaxDevices] = {};
     if (__atomic_load_n(&configured[dev], __ATOMIC_ACQUIRE)) return true;
-    if (cudaFuncSetAttribute(grouped_kernel<FP4, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)grouped_smem<FP4>(kMaxStages)) !=
+    if (cudaFuncSetAttribute(grouped_kernel<FP4, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)grouped_smem<FP4, PAIR>(kMaxStages, 2 * kTileBytes)) !=
         cudaSuccess)
         return false;
     __atomic_store_n(&configured[dev], 1, __ATOMIC_RELEASE);
@@ -653,8 +712,8 @@ static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, unsigne
     if (dev < 0 || !grouped_configure<FP4, PAIR>(dev)) return REGIONE_CUDA_ERROR;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3((kEpiWarps + 2 + (FP4 ? kScaleWarps : 0)) * 32);
-    cfg.dynamicSmemBytes = grouped_smem<FP4>(p.stages);
+    cfg.blockDim = dim3(Roles<FP4, PAIR>::kThreads);
+    cfg.dynamicSmemBytes = grouped_smem<FP4, PAIR>(p.stages, p.stage_bytes);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -672,25 +731,58 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
     constexpr int kElems = FP4 ? 256 : 64;
     const int sms = sm_count();
     p.chunks = (p.K + kElems - 1) / kElems;
-    // Tiles of the largest width, if every row of the buffer is live: what a pair of CTAs each would have.
-    const long long groups = std::min(p.groups, p.rows_cap);
+    const long long groups = std::min(p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
     const long long f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
-    const long long pair_tiles = f_pairs * std::max<long long>(groups, p.rows_cap / 256);
-    const bool pair = pair_tiles * 2 > sms / 2;
-    p.slices = 1;
-    p.width = 16;
-    long long tiles = 0;
-    if (!pair) {
-        while (p.width < 128 && p.width * groups < p.rows_cap) p.width *= 2;
-        tiles = f_tiles * (p.rows_cap / p.width + groups);
-        while (p.slices < 8 && 2 * p.slices * tiles <= sms && 4 * p.slices <= p.chunks) p.slices *= 2;
+    // What the launch will take, in cycles, if every row of the buffer is live and the groups are alike: rounds of tiles times what a
+    // chunk takes the tensor core or the way from L2 (see the plan in the kernel), and what a launch takes besides.
+    long long best = 0x7fffffffffffffffLL;
+    for (int width = 32; width <= (FP4 ? 224 : 256); width += 32) {
+        const long long rounds = (f_pairs * groups * ((each + width - 1) / width) + sms / 2 - 1) / (sms / 2);
+        best = std::min(best, rounds * p.chunks * std::max(2 * width, (256 + width) * 9 / 8) + 3000);
     }
-    // (at least four: see the scales)
-    p.stages = pair ? kMaxStages : std::max(4, std::min(kMaxStages, (p.chunks + p.slices - 1) / p.slices));
+    bool pair = true;
+    long long tiles = 0;
+    p.slices = 1;
+    p.width = 0;
+    for (int width = 16; width <= 128; width *= 2) {
+        const long long n = f_tiles * (p.rows_cap / width + groups);            // at most, however the rows are spread over the groups
+        if (n > 0x7fffffffLL / 8) continue;
+        for (int slices = 1; slices <= 8 && 2 * slices <= std::max(p.chunks, 2); slices *= 2) {
+            const long long rounds = (n * slices + sms - 1) / sms, mine = (p.chunks + slices - 1) / slices;
+            const long long cost = rounds * mine * std::max(2 * width, (128 + width) * 9 / 4) + (slices > 1 ? 2500 : 1500) +
+                                   (rounds - 1) * 1500;
+            if (cost >= best) continue;
+            best = cost;
+            pair = false;
+            p.width = width;
+            p.slices = slices;
+            tiles = n;
+        }
+    }
+    if (pair) {
+        p.stages = kMaxStages;
+        p.stage_bytes = 2 * kTileBytes;
+        p.tmem_columns = 512;
+        p.scale_column = 448;
+    } else {
+        // two CTAs an SM, with all of their part of K in the ring if it fits; at least four stages (see the scales)
+        p.stage_bytes = kTileBytes + p.width * kChunkBytes;
+        const int room = (int)((113 * 1024 - grouped_smem<FP4, false>(0, 0)) / (p.stage_bytes + (FP4 ? kScaleA + kScaleB : 0)));
+        p.stages = std::max(4, std::min({kMaxStages, room, (p.chunks + p.slices - 1) / p.slices}));
+        p.scale_column = p.width <= 64 ? 64 : 128;
+        p.tmem_columns = FP4 ? 2 * p.scale_column : std::max(32, p.width);
+    }
     GroupedMaps maps;
     bool ok = grouped_map(&maps.w, FP4, 3, w, p.K, p.N, p.n_weights, FP4 ? p.K / 2 : 2LL * p.K, 128);
     for (int i = 0; i < kMaps && ok && (pair || (16 << i) <= p.width); ++i)
         ok = grouped_map(&maps.x[i], FP4, 2, x, p.K, p.rows_cap, 1, x_row_bytes, 16 << i);
+    if (ok && pair) {
+        const cuuint64_t dims[2] = {(cuuint64_t)p.N, (cuuint64_t)p.rows_cap}, strides[1] = {(cuuint64_t)(2 * p.out_stride)};
+        const cuuint32_t box[2] = {32u, 16u}, ones[2] = {1u, 1u};
+        ok = grouped_encode_fn()(&maps.out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.out, dims, strides, box, ones,
+                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    }
     if (!ok) return REGIONE_CUDA_ERROR;
     if (pair) return grouped_launch<FP4, true>(maps, p, (unsigned)(sms / 2 * 2), 2, st);
     return grouped_launch<FP4, false>(maps, p, (unsigned)(tiles * p.slices), p.slices, st);
