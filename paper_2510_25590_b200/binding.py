@@ -400,8 +400,8 @@ def _rows(t, shape, dtype, name):
     try:
         if t.is_cuda and t.dtype == dtype and t.shape == shape:
             step, unit = t.stride()
-            if unit == 1 and step >= cols and rows > 1:
-                return t.data_ptr(), step
+            if unit == 1 and step >= cols:
+                return t.data_ptr(), step if rows > 1 else cols
     except AttributeError:
         pass
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:

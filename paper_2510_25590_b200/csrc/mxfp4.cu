@@ -34,10 +34,26 @@ struct Fp4Rows {
     int32_t* dev_status;
 };
 
-// Two fp32 -> two E2M1 codes (round to nearest even, saturating); `lo` lands in bits [3:0].
-__device__ __forceinline__ uint32_t pack_e2m1x2(float lo, float hi) {
+// Eight bf16 times a power of two `inv` (bf16, exact in fp32) -> eight E2M1 codes (round to nearest even, saturating), the first
+// element in bits [3:0].
+__device__ __forceinline__ uint32_t pack_e2m1x8(const uint32_t* w, uint32_t inv) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm("{.reg .b16 lo, hi, s, z;\n\t"
+            "mov.b32 {lo, hi}, %2;\n\t"
+            "mov.b32 {s, z}, %3;\n\t"
+            "fma.rn.f32.bf16 %0, lo, s, %4;\n\t"
+            "fma.rn.f32.bf16 %1, hi, s, %4;}"
+            : "=f"(x[2 * i]), "=f"(x[2 * i + 1]) : "r"(w[i]), "r"(inv), "f"(-0.0f));
     uint32_t r;
-    asm("{.reg .b8 c; cvt.rn.satfinite.e2m1x2.f32 c, %1, %2; cvt.u32.u8 %0, c;}" : "=r"(r) : "f"(hi), "f"(lo));
+    asm("{.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};}"
+        : "=r"(r) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
     return r;
 }
 // Eight codes -> four packed pairs of half-precision values (exact).
@@ -62,100 +78,120 @@ __device__ __forceinline__ float pow2(int k) {
 }
 
 // k + 127 of a block's scale from its largest magnitude as bf16 bits without their sign.  With exponent field E and seven mantissa
-// bits M: e = E - 126 and m > 0.75 where M > 64.  (Infinity saturates like the largest finite value; a subnormal maximum is below
-// 6 * 2^-127 and ends at the floor.)
+// bits M: e = E - 126 and m > 0.75 where M > 64, which adding 63 carries into E.  (Infinity saturates like the largest finite value; a
+// subnormal maximum is below 6 * 2^-127 and ends at the floor.)
 __device__ __forceinline__ int fp4_scale_code(uint32_t amax) {
-    if (amax == 0) return 127;
-    amax = min(amax, 0x7f7fu);
-    return max((int)(amax >> 7) - 2 + ((amax & 127) > 64 ? 1 : 0), 0);
+    const int code = max((int)((min(amax, 0x7f7fu) + 63) >> 7) - 2, 0);
+    return amax == 0 ? 127 : code;
 }
 
-__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+// Per half: the larger magnitude, with some sign.  (A NaN element is ignored.)
+__device__ __forceinline__ uint32_t max_magnitude_bf16x2(uint32_t a, uint32_t b) {
     uint32_t r;
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));      // (a NaN element is ignored)
+    asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 
+// 32 bytes that are read once, in one load (WIDE: 32-byte aligned) or two.
+template <bool WIDE> __device__ __forceinline__ void ld_stream256(const uint16_t* src, uint32_t* w) {
+    if constexpr (WIDE) {
+        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(src));
+    } else {
+        const uint4 a = ldg128(src), b = ldg128(src + 8);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+}
+
 // What a warp's task is: a tensor, its row of the source and of the destination, and the first element.  False: nothing to do.
-__device__ __forceinline__ bool fp4_task(const Fp4Rows& p, long long task, int lane, int& tensor, long long& src_row,
-                                         long long& dst_row, long long& first) {
-    const long long per_row = (long long)p.tensors * p.segs;
-    dst_row = task / per_row;
-    const int in = (int)(task - dst_row * per_row);
-    tensor = in / p.segs;
-    first = (long long)(in - tensor * p.segs) * kTask;
-    const int b = (int)(dst_row / p.cap);
-    const long long j = dst_row - b * p.cap;
+struct Fp4Task {
+    int tensor;
+    long long src_row, dst_row, first;
+};
+__device__ __forceinline__ bool fp4_task(const Fp4Rows& p, long long at, int lane, Fp4Task& t) {
+    if (at >= p.tasks) return false;
+    const int per_row = p.tensors * p.segs;
+    int in, b, j;
+    if (p.tasks <= 0x7fffffffLL) {                      // (a division in 64 bits takes as long as the task's arithmetic)
+        const uint32_t row = (uint32_t)at / (uint32_t)per_row;
+        in = (int)((uint32_t)at - row * per_row);
+        b = (int)(row / (uint32_t)p.cap);
+        j = (int)(row - b * (uint32_t)p.cap);
+        t.dst_row = row;
+    } else {
+        t.dst_row = at / per_row;
+        in = (int)(at - t.dst_row * per_row);
+        b = (int)(t.dst_row / p.cap);
+        j = (int)(t.dst_row - b * p.cap);
+    }
+    t.tensor = in >= p.segs;
+    t.first = (long long)(in - t.tensor * p.segs) * kTask;
+    const int row = p.idx != nullptr ? p.idx[t.dst_row] : j;
     if (p.n != nullptr) {
         const int live = p.n[b];
         if ((live < 0 || live > p.cap) && j == 0 && in == 0 && lane == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
         if (j >= live) return false;
     }
-    long long row = j;
-    if (p.idx != nullptr) row = p.idx[dst_row];
     if (row < 0 || row >= p.src_rows) {
         if (lane == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
         return false;
     }
-    src_row = b * p.src_rows + row;
+    t.src_row = b * p.src_rows + row;
     return true;
 }
 
+// 16 elements to a lane: the arithmetic is 4 instructions an element, which at 80 % of the issue slots was what bounded the form with 8
+// elements to a lane (7 an element; 16384 x 8192 in 65 us).
+template <bool WIDE>
 __global__ void __launch_bounds__(kFp4Threads) mxfp4_quantize_kernel(const Fp4Rows p) {
     grid_dependency_wait();
     grid_launch_dependents();
     const int lane = threadIdx.x & 31;
-    const long long task = (long long)blockIdx.x * (kFp4Threads / 32) + (threadIdx.x >> 5);
-    if (task >= p.tasks) return;
-    int tensor;
-    long long src_row, dst_row, first;
-    if (!fp4_task(p, task, lane, tensor, src_row, dst_row, first)) return;
-    const uint16_t* src = (tensor ? p.src[1] : p.src[0]) + src_row * p.E + first;
-    uint8_t* codes = (tensor ? p.codes[1] : p.codes[0]) + (dst_row * p.E + first) / 2;
-    const int live = (int)min((long long)kTask, p.E - first);            // elements, a multiple of 32
-    uint4 w[kFp4Unroll];
+    Fp4Task t;
+    if (!fp4_task(p, (long long)blockIdx.x * (kFp4Threads / 32) + (threadIdx.x >> 5), lane, t)) return;
+    const uint16_t* src = (t.tensor ? p.src[1] : p.src[0]) + t.src_row * p.E + t.first + lane * 16;
+    const long long at = t.dst_row * p.E + t.first;
+    uint8_t* codes = (t.tensor ? p.codes[1] : p.codes[0]) + at / 2 + lane * 8;
+    const int live = (int)min((long long)kTask, p.E - t.first);          // elements, a multiple of 32
+    uint32_t w[kTask / 512][8];
 #pragma unroll
-    for (int u = 0; u < kFp4Unroll; ++u) {
-        const int e = (u * 32 + lane) * 8;
-        w[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (e < live) w[u] = ld_stream128(src + e);
-    }
-    int mine = 0;                                                       // scale of block `lane` of the task
+    for (int u = 0; u < kTask / 512; ++u) {
 #pragma unroll
-    for (int u = 0; u < kFp4Unroll; ++u) {
-        constexpr uint32_t kAbs = 0x7fff7fffu;
-        uint32_t m = max_bf16x2(max_bf16x2(w[u].x & kAbs, w[u].y & kAbs), max_bf16x2(w[u].z & kAbs, w[u].w & kAbs));
-        m = max_bf16x2(m, 0u);                                           // (four pairs of NaN)
-        m = max_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        const int code = fp4_scale_code(max(m & 0xffffu, m >> 16));
-        const float inv = pow2(127 - code);
-        const int from = __shfl_sync(0xffffffffu, code, (lane & 7) * 4);
-        if ((lane >> 3) == u) mine = from;
-        const uint32_t q = pack_e2m1x2(bf16_lo(w[u].x) * inv, bf16_hi(w[u].x) * inv) |
-                           (pack_e2m1x2(bf16_lo(w[u].y) * inv, bf16_hi(w[u].y) * inv) << 8) |
-                           (pack_e2m1x2(bf16_lo(w[u].z) * inv, bf16_hi(w[u].z) * inv) << 16) |
-                           (pack_e2m1x2(bf16_lo(w[u].w) * inv, bf16_hi(w[u].w) * inv) << 24);
-        const int e = (u * 32 + lane) * 8;
-        if (e < live) *reinterpret_cast<uint32_t*>(codes + e / 2) = q;
+        for (int i = 0; i < 8; ++i) w[u][i] = 0u;
+        if (u * 512 + lane * 16 < live) ld_stream256<WIDE>(src + u * 512, w[u]);
     }
-    if (lane * 32 < live) (tensor ? p.scales[1] : p.scales[0])[(dst_row * p.E + first) / 32 + lane] = (uint8_t)mine;
+    int scale = 0;                                                      // of block `lane` of the task
+#pragma unroll
+    for (int u = 0; u < kTask / 512; ++u) {
+        uint32_t m = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max_magnitude_bf16x2(m, w[u][i]);
+        m = max_magnitude_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        const int code = fp4_scale_code(max(m & 0x7fffu, (m >> 16) & 0x7fffu));
+        const uint32_t inv = (uint32_t)(254 - code) << 7;               // 2^(127 - code) as bf16; code is at most 253
+        const int from = __shfl_sync(0xffffffffu, code, (lane & 15) * 2);
+        if ((lane >> 4) == u) scale = from;
+        uint2 q;
+        q.x = pack_e2m1x8(w[u], inv);
+        q.y = pack_e2m1x8(w[u] + 4, inv);
+        if (u * 512 + lane * 16 < live) *reinterpret_cast<uint2*>(codes + u * 256) = q;
+    }
+    if (lane * 32 < live) (t.tensor ? p.scales[1] : p.scales[0])[at / 32 + lane] = (uint8_t)scale;
 }
 
 __global__ void __launch_bounds__(kFp4Threads) mxfp4_dequantize_kernel(const Fp4Rows p) {
     grid_dependency_wait();
     grid_launch_dependents();
     const int lane = threadIdx.x & 31;
-    const long long task = (long long)blockIdx.x * (kFp4Threads / 32) + (threadIdx.x >> 5);
-    if (task >= p.tasks) return;
-    int tensor;
-    long long row, dst_row, first;
-    if (!fp4_task(p, task, lane, tensor, row, dst_row, first)) return;
-    const long long at = dst_row * p.E + first;
+    Fp4Task t;
+    if (!fp4_task(p, (long long)blockIdx.x * (kFp4Threads / 32) + (threadIdx.x >> 5), lane, t)) return;
+    const int tensor = t.tensor;
+    const long long at = t.dst_row * p.E + t.first;
     const uint8_t* codes = (tensor ? p.codes[1] : p.codes[0]) + at / 2;
     const uint8_t* scales = (tensor ? p.scales[1] : p.scales[0]) + at / 32;
     uint16_t* dst = (tensor ? p.dst[1] : p.dst[0]) + at;
-    const int live = (int)min((long long)kTask, p.E - first);
+    const int live = (int)min((long long)kTask, p.E - t.first);
     uint32_t q[kFp4Unroll];
 #pragma unroll
     for (int u = 0; u < kFp4Unroll; ++u) {
@@ -178,7 +214,7 @@ __global__ void __launch_bounds__(kFp4Threads) mxfp4_dequantize_kernel(const Fp4
 }
 
 // Rows that lie one behind the other and are all live are one long row.
-static int launch_fp4_rows(void (*kernel)(Fp4Rows), Fp4Rows p, int B, cudaStream_t st) {
+static int launch_fp4_rows(bool quantize, Fp4Rows p, int B, cudaStream_t st) {
     if (p.idx == nullptr && p.n == nullptr && p.src_rows == p.cap) {
         p.E *= p.cap * B;
         p.cap = p.src_rows = 1;
@@ -190,7 +226,10 @@ static int launch_fp4_rows(void (*kernel)(Fp4Rows), Fp4Rows p, int B, cudaStream
     p.tasks = (long long)B * p.cap * p.tensors * segs;
     const long long blocks = (p.tasks + kFp4Threads / 32 - 1) / (kFp4Threads / 32);
     if (blocks > 0x7fffffffLL) return REGIONE_UNSUPPORTED;
-    return launch_status(launch_overlapped(kernel, dim3((unsigned)blocks), dim3(kFp4Threads), 0, st, p));
+    const bool wide = ((reinterpret_cast<uintptr_t>(p.src[0]) | reinterpret_cast<uintptr_t>(p.src[1])) & 31) == 0;
+    return launch_status(launch_overlapped(!quantize ? mxfp4_dequantize_kernel : wide ? mxfp4_quantize_kernel<true>
+                                                                                      : mxfp4_quantize_kernel<false>,
+                                           dim3((unsigned)blocks), dim3(kFp4Threads), 0, st, p));
 }
 
 }  // namespace regione
@@ -216,7 +255,7 @@ extern "C" int regione_mxfp4_quantize(const regione_bf16* x, const int32_t* idx,
     p.src[0] = x; p.codes[0] = codes; p.scales[0] = scales;
     p.idx = idx; p.n = n; p.tensors = 1;
     p.src_rows = src_rows; p.cap = cap; p.E = K; p.dev_status = dev_status;
-    return launch_fp4_rows(mxfp4_quantize_kernel, p, B, (cudaStream_t)stream);
+    return launch_fp4_rows(true, p, B, (cudaStream_t)stream);
 }
 
 extern "C" int regione_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, const int32_t* n, int B, int64_t cap,
@@ -228,7 +267,7 @@ extern "C" int regione_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sca
     p.dst[0] = x; p.codes[0] = const_cast<uint8_t*>(codes); p.scales[0] = const_cast<uint8_t*>(scales);
     p.n = n; p.tensors = 1;
     p.src_rows = p.cap = cap; p.E = K; p.dev_status = dev_status;
-    return launch_fp4_rows(mxfp4_dequantize_kernel, p, B, (cudaStream_t)stream);
+    return launch_fp4_rows(false, p, B, (cudaStream_t)stream);
 }
 
 static int check_fp4_cache(const void* k, const void* v, const void* k_q, const void* v_q, const void* k_scale,
@@ -253,7 +292,7 @@ extern "C" int regione_rikv_store_mxfp4(const regione_bf16* k_full, const region
     p.src[1] = v_full; p.codes[1] = v_q; p.scales[1] = v_scale;
     p.idx = keep_rows; p.n = n_keep; p.tensors = 2;
     p.src_rows = N_full; p.cap = Nc_cap; p.E = (long long)H * D; p.dev_status = dev_status;
-    return launch_fp4_rows(mxfp4_quantize_kernel, p, B, (cudaStream_t)stream);
+    return launch_fp4_rows(true, p, B, (cudaStream_t)stream);
 }
 
 extern "C" int regione_rikv_load_mxfp4(const uint8_t* k_q, const uint8_t* v_q, const uint8_t* k_scale,
@@ -267,5 +306,5 @@ extern "C" int regione_rikv_load_mxfp4(const uint8_t* k_q, const uint8_t* v_q, c
     p.dst[1] = v_cache; p.codes[1] = const_cast<uint8_t*>(v_q); p.scales[1] = const_cast<uint8_t*>(v_scale);
     p.n = n_keep; p.tensors = 2;
     p.src_rows = p.cap = Nc_cap; p.E = (long long)H * D; p.dev_status = dev_status;
-    return launch_fp4_rows(mxfp4_dequantize_kernel, p, B, (cudaStream_t)stream);
+    return launch_fp4_rows(false, p, B, (cudaStream_t)stream);
 }
