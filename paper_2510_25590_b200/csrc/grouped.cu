@@ -19,7 +19,7 @@ namespace regione {
 constexpr int kFeat = 128;                            // features a CTA
 constexpr int kChunkBytes = 128;                      // of K: 64 bf16 or 256 4-bit elements, one swizzle row
 constexpr int kTileBytes = 128 * kChunkBytes;         // 128 rows of either operand
-constexpr int kMaxStages = 6;
+constexpr int kMaxStages = 12;
 constexpr int kMaxGroups = 512;
 constexpr int kScaleA = 1024, kScaleB = 2048;         // scales of a stage: [2 of 128 elements][1 or 2 of 128 rows][512 bytes]
 // Warps of a CTA: 8 (4) that take sums out of tensor memory, one that loads, one that issues products, and with 4-bit operands 8 (4) that
@@ -35,7 +35,7 @@ struct GroupedArgs {
     const int32_t *row_begin, *row_end;
     int groups, n_weights, rows_cap, K, N;
     int chunks;                                       // of K
-    int stages, stage_bytes;                          // a stage: 128 rows of W, then those of x
+    int ring_bytes;                                   // for stages: 128 rows of W and a tile's of x each, and the scales of both
     int tmem_columns, scale_column;
     int slices;                                       // of K, one per CTA of a cluster (the kernel without pairs)
     int width;                                        // rows of a tile at most (the kernel without pairs)
@@ -110,10 +110,10 @@ template <bool PAIR> __device__ __forceinline__ void copy_scales(uint32_t taddr,
 }
 
 // All tcgen05 operations issued so far by this thread arrive on `bar`, in a pair on the barrier at that place in both CTAs.
-template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar) {
+template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar, uint32_t pair_mask) {
     if constexpr (PAIR)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+                     ::"r"(bar), "h"((uint16_t)pair_mask) : "memory");
     else
         ptx::mma_commit(bar);
 }
@@ -267,16 +267,17 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     constexpr int kScaleGroups = PAIR ? 3 : 2;         // of 32 rows, a warp of scales: 128 rows of W and up to 256 (128) of x, four warps to a chunk
     const uint32_t smem = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
     uint8_t* base = smem_raw + (smem - ptx::smem_addr(smem_raw));
-    uint8_t* scales = base + (size_t)p.stages * p.stage_bytes;
-    uint8_t* staging = scales + (FP4 ? (size_t)p.stages * (kScaleA + kScaleB) : 0);
+    uint8_t* staging = base + p.ring_bytes;
     GroupedControl* ctl = reinterpret_cast<GroupedControl*>(staging + kEpiWarps * kStagingBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cluster = PAIR ? 2 : p.slices;
+    // a cluster has a tile's slices of K, a slice is a CTA or a pair; `half`: which of the pair
+    const int cluster = (PAIR ? 2 : 1) * p.slices;
     const int rank = cluster > 1 ? (int)(blockIdx.x % cluster) : 0;
-    const bool leader = !PAIR || rank == 0;
+    const int half = PAIR ? rank & 1 : 0, slice = PAIR ? rank >> 1 : rank;
+    const bool leader = half == 0, split = p.slices > 1;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) {
+        for (int s = 0; s < kMaxStages; ++s) {
             ptx::mbar_init(ptx::smem_addr(&ctl->full[s]), 1 + (FP4 ? 4 * (PAIR ? 2 : 1) : 0));
             ptx::mbar_init(ptx::smem_addr(&ctl->empty[s]), 1);
         }
@@ -295,7 +296,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
 
     // ---- plan: from the groups' row counts, which only the device knows --------------------------------------------
     const int f_tiles = (p.N + (PAIR ? 2 : 1) * kFeat - 1) / ((PAIR ? 2 : 1) * kFeat);
-    const int workers = PAIR ? gridDim.x / 2 : gridDim.x / cluster;
+    const int workers = gridDim.x / cluster;
     if constexpr (PAIR) {
         // Widths of 32 .. 256 (224) rows: one warp adds up the tiles of one width.  A chunk of a tile takes the tensor core 2 cycles a row;
         // its 128 + width / 2 rows of 128 bytes arrive at about 57 bytes a cycle.  The width with the cheapest rounds of tiles is
@@ -343,10 +344,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         }
         if (lane == 0) {
             ctl->first[p.groups] = at;
-            const long long total = (long long)at * f_tiles;
-            // (one tile per cluster without pairs: the grid covers every set of ranges that do not overlap)
-            if (!PAIR && total > workers && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
-            ctl->total = (int)min(total, 0x7fffffffLL);
+            ctl->width = width;
+            ctl->total = (int)min((long long)at * f_tiles, 0x7fffffffLL);
         }
     }
     ptx::tc_fence_before_sync();
@@ -354,308 +353,320 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     ptx::tc_fence_after_sync();
     const uint32_t tmem = ctl->tmem;
     const int worker = blockIdx.x / cluster, total = ctl->total;
-    const int step = PAIR ? workers : 0x40000000;
-    // chunks of K that this CTA takes
-    const int c_begin = PAIR ? 0 : (int)((long long)p.chunks * rank / p.slices);
-    const int c_end = PAIR ? p.chunks : (int)((long long)p.chunks * (rank + 1) / p.slices);
-    int group = 0;                                    // of this thread's last tile
-    auto bar_at = [&](const uint64_t* bar) {          // a barrier of the leader
+    // The narrower the tiles, the more stages: what bounds the loads is how many bytes are on their way (about 2 us under load).
+    const int stage_bytes = kTileBytes + ctl->width * (PAIR ? kChunkBytes / 2 : kChunkBytes);
+    const int stages = min(kMaxStages, p.ring_bytes / (stage_bytes + (FP4 ? kScaleA + kScaleB : 0)));
+    uint8_t* scales = base + stages * stage_bytes;
+    // chunks of K that this slice takes
+    const int c_begin = (int)((long long)p.chunks * slice / p.slices), c_end = (int)((long long)p.chunks * (slice + 1) / p.slices);
+    auto bar_at = [&](const uint64_t* bar) {          // a barrier of the pair's leader
         const uint32_t a = ptx::smem_addr(bar);
-        return PAIR ? ptx::map_rank(a, 0) : a;
+        return PAIR ? ptx::map_rank(a, rank & ~1) : a;
     };
+    // What a role keeps from tile to tile: its group, its place in the ring, its tiles so far.
+    int group = 0, s = 0, it = 0, filled = 0, sf = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    const bool elected = ptx::elect_one();
+    const uint32_t pair_mask = 3u << (rank & ~1);     // of the cluster's CTAs
+    constexpr int kAccs = PAIR ? 2 : 1;
 
-    if (warp == kProducer) {
-        if (ptx::elect_one()) {
-            int s = 0, filled = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (long long t = worker; t < total && ok; t += step) {
-                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
-                const int half = PAIR ? tile.width / 2 : tile.width;
-                const uint32_t bytes = (kTileBytes + half * kChunkBytes) * (PAIR ? 2 : 1);
-                const int feature = tile.feature + (PAIR ? rank * kFeat : 0), row = tile.first + (PAIR ? rank * half : 0);
-                for (int c = c_begin; c < c_end; ++c) {
-                    if (!grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
-                    if (leader) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&ctl->full[s]), bytes);
-                    const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * p.stage_bytes;
-                    load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
-                    int at = 0;                                                  // boxes that make up the rows, the largest first
+    // A cluster goes through its tiles without a stop; where slices meet, one tile at a time.
+    for (long long t0 = worker; t0 < total; t0 += split ? workers : total) {
+        const long long t_end = split ? t0 + 1 : total;
+        if (warp == kProducer) {
+            if (elected) {
+                for (long long t = t0; t < t_end && ok; t += workers) {
+                    const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
+                    const int rows = PAIR ? tile.width / 2 : tile.width;                     // of x, for this CTA
+                    const uint32_t bytes = (kTileBytes + rows * kChunkBytes) * (PAIR ? 2 : 1);
+                    const int feature = tile.feature + half * kFeat, row = tile.first + half * rows;
+                    for (int c = c_begin; c < c_end; ++c) {
+                        if (!grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
+                        if (leader) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&ctl->full[s]), bytes);
+                        const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * stage_bytes;
+                        load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
+                        int at = 0;                                                  // boxes that make up the rows, the largest first
 #pragma unroll
-                    for (int box = kMaps - 1; box >= 0; --box)
-                        if (half & (16 << box)) {
-                            load_x<PAIR>(dst + kTileBytes + at * kChunkBytes, &maps.x[box], bar, c * (FP4 ? kChunkBytes : kElems), row + at);
-                            at += 16 << box;
-                        }
-                    ++filled;
-                    if (++s == p.stages) { s = 0; phase ^= 1; }
+                        for (int box = kMaps - 1; box >= 0; --box)
+                            if (rows & (16 << box)) {
+                                load_x<PAIR>(dst + kTileBytes + at * kChunkBytes, &maps.x[box], bar, c * (FP4 ? kChunkBytes : kElems), row + at);
+                                at += 16 << box;
+                            }
+                        ++filled;
+                        if (++s == stages) { s = 0; phase ^= 1; }
+                    }
                 }
             }
-            if (!ok && leader) {                      // copies in flight land before shared memory is given up
-                for (int i = min(filled, p.stages); i > 0; --i) {
-                    int q = s - i;
-                    uint32_t ph = phase;
-                    if (q < 0) { q += p.stages; ph ^= 1; }
-                    const long long t0 = clock64();
-                    while (!ptx::mbar_try_wait(ptx::smem_addr(&ctl->full[q]), ph) && clock64() - t0 < kGroupedWait / 8) {}
-                }
-            }
-        }
-    } else if (warp == kIssuer) {
-        if (leader && ptx::elect_one()) {
-            constexpr uint32_t hi = ptx::smem_desc_hi_sw128(1024);              // 8-row groups 1024 bytes apart
-            constexpr uint32_t hi_plain = (128u >> 4) | (1u << 14);             // scales: no swizzle, 8 rows of 16 bytes
-            int s = 0, it = 0, sf = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (long long t = worker; t < total && ok; t += step, ++it) {
-                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
-                const int a = PAIR ? it & 1 : 0;
-                const uint32_t d = tmem + (a ? kAcc1 : 0);
-                if (it >= 2 && !grouped_wait(ptx::smem_addr(&ctl->acc_empty[a]), ((it >> 1) - 1) & 1, ctl, p.dev_status)) { ok = false; break; }
-                ptx::tc_fence_after_sync();
-                const uint32_t idesc = FP4 ? (1u << 7) | (1u << 10) | ((uint32_t)(tile.width >> 3) << 17) | (1u << 23) |
-                                                 ((PAIR ? 2u : 1u) << 27)
-                                           : ptx::idesc_bf16_f32(PAIR ? 256 : 128, tile.width, false);
-                uint32_t accumulate = 0;
-                for (int c = c_begin; c < c_end; ++c) {
-                    if (!grouped_wait(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
+        } else if (warp == kIssuer) {
+            if (leader && elected) {
+                constexpr uint32_t hi = ptx::smem_desc_hi_sw128(1024);              // 8-row groups 1024 bytes apart
+                constexpr uint32_t hi_plain = (128u >> 4) | (1u << 14);             // scales: no swizzle, 8 rows of 16 bytes
+                for (long long t = t0; t < t_end && ok; t += workers, ++it) {
+                    const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
+                    const int a = it % kAccs, use = it / kAccs;
+                    const uint32_t d = tmem + (a ? kAcc1 : 0);
+                    if (use > 0 && !grouped_wait(ptx::smem_addr(&ctl->acc_empty[a]), (use - 1) & 1, ctl, p.dev_status)) { ok = false; break; }
                     ptx::tc_fence_after_sync();
-                    const uint32_t at = smem + s * p.stage_bytes;
-                    const uint32_t a_lo = ptx::smem_desc_lo(at, 16), b_lo = ptx::smem_desc_lo(at + kTileBytes, 16);
-                    uint32_t sfa = 0, sfb = 0;
-                    if constexpr (FP4) {
-                        sfa = tmem + p.scale_column + sf * 32;
-                        sfb = sfa + 8;
-                        sf ^= 1;
-                        const uint32_t sa = ptx::smem_addr(scales) + s * (kScaleA + kScaleB), sb = sa + kScaleA;
-                        for (int k = 0; k < 2; ++k) {
-                            copy_scales<PAIR>(sfa + 4 * k, ptx::smem_desc_join(ptx::smem_desc_lo(sa + k * 512, 16), hi_plain));
-                            copy_scales<PAIR>(sfb + 8 * k, ptx::smem_desc_join(ptx::smem_desc_lo(sb + k * 1024, 16), hi_plain));
-                            if (tile.width > 128)
-                                copy_scales<PAIR>(sfb + 8 * k + 4, ptx::smem_desc_join(ptx::smem_desc_lo(sb + k * 1024 + 512, 16), hi_plain));
+                    const uint32_t idesc = FP4 ? (1u << 7) | (1u << 10) | ((uint32_t)(tile.width >> 3) << 17) | (1u << 23) |
+                                                     ((PAIR ? 2u : 1u) << 27)
+                                               : ptx::idesc_bf16_f32(PAIR ? 256 : 128, tile.width, false);
+                    uint32_t accumulate = 0;
+                    for (int c = c_begin; c < c_end; ++c) {
+                        if (!grouped_wait(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
+                        ptx::tc_fence_after_sync();
+                        const uint32_t at = smem + s * stage_bytes;
+                        const uint32_t a_lo = ptx::smem_desc_lo(at, 16), b_lo = ptx::smem_desc_lo(at + kTileBytes, 16);
+                        uint32_t sfa = 0, sfb = 0;
+                        if constexpr (FP4) {
+                            sfa = tmem + p.scale_column + sf * 32;
+                            sfb = sfa + 8;
+                            sf ^= 1;
+                            const uint32_t sa = ptx::smem_addr(scales) + s * (kScaleA + kScaleB), sb = sa + kScaleA;
+                            for (int k = 0; k < 2; ++k) {
+                                copy_scales<PAIR>(sfa + 4 * k, ptx::smem_desc_join(ptx::smem_desc_lo(sa + k * 512, 16), hi_plain));
+                                copy_scales<PAIR>(sfb + 8 * k, ptx::smem_desc_join(ptx::smem_desc_lo(sb + k * 1024, 16), hi_plain));
+                                if (tile.width > 128)
+                                    copy_scales<PAIR>(sfb + 8 * k + 4, ptx::smem_desc_join(ptx::smem_desc_lo(sb + k * 1024 + 512, 16), hi_plain));
+                            }
+                        }
+                        // 32 bytes of K to an instruction; what lies behind K is zero and left out
+                        const int left = (p.K - c * kElems + kElems / 4 - 1) / (kElems / 4);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            if (k >= left) break;
+                            // (bits 4 and 29: which half of a scale word the two blocks of 32 have)
+                            const uint32_t id = FP4 && (k & 1) ? idesc | (2u << 4) | (2u << 29) : idesc;
+                            mma<PAIR, FP4>(d, ptx::smem_desc_join(a_lo + 2 * k, hi), ptx::smem_desc_join(b_lo + 2 * k, hi), id,
+                                           sfa + 4 * (k >> 1), sfb + 8 * (k >> 1), accumulate);
+                            accumulate = 1;
+                        }
+                        commit<PAIR>(ptx::smem_addr(&ctl->empty[s]), pair_mask);
+                        if (++s == stages) { s = 0; phase ^= 1; }
+                    }
+                    if (ok) commit<PAIR>(ptx::smem_addr(&ctl->acc_full[a]), pair_mask);
+                }
+            }
+        } else if (FP4 && warp >= kScaler) {
+            // Scales: 8 bytes a row and chunk, from rows that lie K / 32 bytes apart to the places in shared memory that the copy to tensor
+            // memory reads.  A team of four warps takes a part of two chunks, 16 bytes a row; a pair of CTAs has two teams in turn, which is
+            // 8192^3 in 249 -> 214 us, and with 32 bytes a row in registers and no turns 221.  A warp has every fourth group of 32 rows.
+            // (The stage that a team waits for is at most four chunks behind its last one and the ring has at least four stages: no phase of
+            // a barrier can be mistaken for the one two further on.)  Rows behind the matrices are read as their last one: their products
+            // are not stored.
+            constexpr int kTeams = kScaleWarps / 4;
+            const int k32 = p.K / 32, team = (warp - kScaler) >> 2, member = (warp - kScaler) & 3;
+            const bool vec = k32 % 16 == 0;
+            long long t = t0;
+            int c = c_begin, q = s;                       // the next chunk and its stage
+            uint32_t turn = phase;
+            bool fresh = true;                            // the next fetch is the first of its tile
+            const uint8_t* src[kScaleGroups];
+            auto fetch = [&](uint4 (&v)[kScaleGroups]) {
+                if (fresh) {
+                    const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
+                    const int feature = tile.feature + half * kFeat;
+#pragma unroll
+                    for (int i = 0; i < kScaleGroups; ++i) {
+                        const int part = member + 4 * i;                            // 4 groups of W, then those of x
+                        const int r = (part & 3) * 8 + (lane >> 2) + 32 * (lane & 3) + (part < 8 ? 0 : 128);
+                        src[i] = part < 4 ? p.w_scale + ((size_t)tile.weights * p.N + min(feature + r, p.N - 1)) * k32
+                                           : p.x_scale + (size_t)min(tile.first + r, p.rows_cap - 1) * k32;
+                    }
+                    fresh = false;
+                }
+                const int off = (c & ~1) * 8;
+                if (vec) {
+#pragma unroll
+                    for (int i = 0; i < kScaleGroups; ++i) v[i] = ldg128(src[i] + off);
+                } else {                                  // (words behind the row: its last one, for blocks that no product takes)
+#pragma unroll
+                    for (int i = 0; i < kScaleGroups; ++i) {
+                        auto word = [&](int k) { return __ldg(reinterpret_cast<const uint32_t*>(src[i] + min(off + 4 * k, k32 - 4))); };
+                        v[i] = make_uint4(word(0), word(1), word(2), word(3));
+                    }
+                }
+            };
+            auto advance = [&] {                          // to the next part, of whichever team
+                const int n = min(2 - (c & 1), c_end - c);
+                c += n;
+                q += n;
+                if (q >= stages) { q -= stages; turn ^= 1; }
+                if (c >= c_end) { c = c_begin; t += workers; fresh = true; }
+            };
+            if (kTeams == 2 && team == 1 && t < t_end) advance();
+            uint4 v[kScaleGroups];
+            if (t < t_end) fetch(v);
+            while (t < t_end && ok) {
+                const int first = c, n = min(2 - (c & 1), c_end - c);
+                int at = q;
+                uint32_t ph = turn;
+                for (int k = 0; k < n; ++k) {
+                    ok = __all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->empty[at]), ph ^ 1, ctl, p.dev_status));
+                    if (!ok) break;
+                    uint32_t* sa = reinterpret_cast<uint32_t*>(scales + at * (kScaleA + kScaleB)) + lane;
+                    const bool odd = (first + k) & 1;
+#pragma unroll
+                    for (int i = 0; i < kScaleGroups; ++i) {
+                        const int part = member + 4 * i;
+                        uint32_t* dst = sa + (part < 4 ? 0 : kScaleA / 4 + (part < 8 ? 0 : 128)) + (part & 3) * 32;
+                        dst[0] = odd ? v[i].z : v[i].x;
+                        dst[part < 4 ? 128 : 256] = odd ? v[i].w : v[i].y;
+                    }
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) arrive_at(bar_at(&ctl->full[at]));
+                    if (++at == stages) { at = 0; ph ^= 1; }
+                }
+                advance();
+                if (kTeams == 2 && t < t_end) advance();
+                if (t < t_end) fetch(v);
+            }
+            if (split) {                                  // where the ring stands behind this slice's chunks
+                s += c_end - c_begin;
+                while (s >= stages) { s -= stages; phase ^= 1; }
+            }
+        } else if (warp < kEpiWarps) {
+            constexpr int kEpiCols = 16 * (kEpiWarps / 4);
+            const int sub = warp & 3, part = warp >> 2;
+            const uint32_t stage = ptx::smem_addr(staging) + warp * kStagingBytes;
+            for (long long t = t0; t < t_end; t += workers, ++it) {
+                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
+                const int a = it % kAccs, use = it / kAccs;
+                const int feature = tile.feature + half * kFeat + 32 * sub;
+                uint64_t bias[4] = {0, 0, 0, 0};          // of features lane / 4 + {0, 8, 16, 24}, twice each
+                if (p.bias != nullptr && !split)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int f = min(feature + (lane >> 2) + 8 * i, p.N - 1);
+                        const float b = __uint_as_float((uint32_t)__ldg(p.bias + (size_t)tile.weights * p.N + f) << 16);
+                        bias[i] = pair_of(b, b);
+                    }
+                if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->acc_full[a]), use & 1, ctl, p.dev_status)))
+                    break;
+                ptx::tc_fence_after_sync();
+                const uint32_t acc = tmem + (a ? kAcc1 : 0) + ((uint32_t)(32 * sub) << 16);
+                if (split) {
+                    // this slice's sums as [row][128 features] fp32 over the stages, which nothing reads any more
+                    float* sums = reinterpret_cast<float*>(base);
+                    for (int c = part * 16; c < tile.live; c += kEpiCols) {
+                        uint32_t r[16];
+                        ptx::tmem_ld16(acc + c, r);
+                        ptx::tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sums[(c + i) * kFeat + 32 * sub + lane] = __uint_as_float(r[i]);
+                    }
+                } else {
+                    // 16 rows at a time, the next ones on their way out of tensor memory meanwhile
+                    uint32_t ahead[16];
+                    auto fetch = [&](int c) {
+                        tmem_ld_16x256b_x2(acc + c, ahead);
+                        tmem_ld_16x256b_x2(acc + (16u << 16) + c, ahead + 8);
+                    };
+                    if (part * 16 < tile.live) fetch(part * 16);
+                    for (int c = part * 16; c < tile.live; c += kEpiCols) {
+                        uint64_t y[8];                                               // two rows of one feature
+                        ptx::tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            y[i] = add2(pair_of(__uint_as_float(ahead[2 * i]), __uint_as_float(ahead[2 * i + 1])), bias[(i >> 2) * 2 + (i & 1)]);
+                        if (c + kEpiCols < tile.live) fetch(c + kEpiCols);
+                        if (p.activation == REGIONE_ACT_GELU_TANH)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) y[i] = gelu_tanh(y[i]);
+                        uint32_t z[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            float lo, hi;
+                            parts_of(y[i], lo, hi);
+                            z[i] = pack_bf16x2(lo, hi);
+                        }
+                        // row of the tile t at 64 t, its 16-byte pieces (8 features) turned by t / 2 so that eight rows meet eight banks
+                        const int row = (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1, turn = (row >> 1) & 3;
+                        if (PAIR) {                                                  // (the store of the step before)
+                            if (lane == 0) ptx::bulk_wait_read<0>();
+                            __syncwarp();
+                        }
+                        stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), z[0], z[1], z[2], z[3]);
+                        stmatrix_x4_trans(stage + row * 64 + (((piece + 2) ^ turn) << 4), z[4], z[5], z[6], z[7]);
+                        if (PAIR && c + 16 <= tile.live) {
+                            ptx::fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0 && feature < p.N) {
+                                store_out(&maps.out, stage, feature, tile.first + c);
+                                ptx::bulk_commit();
+                            }
+                        } else {
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int q = (lane >> 2) + 8 * i, j = lane & 3;
+                                const uint4 v = *reinterpret_cast<const uint4*>(staging + warp * kStagingBytes + q * 64 + ((j ^ ((q >> 1) & 3)) << 4));
+                                if (c + q < tile.live && feature + 8 * j < p.N)
+                                    *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + c + q) * p.out_stride + feature + 8 * j) = v;
+                            }
+                            __syncwarp();
                         }
                     }
-                    // 32 bytes of K to an instruction; what lies behind K is zero and left out
-                    const int left = (p.K - c * kElems + kElems / 4 - 1) / (kElems / 4);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (k >= left) break;
-                        // (bits 4 and 29: which half of a scale word the two blocks of 32 have)
-                        const uint32_t id = FP4 && (k & 1) ? idesc | (2u << 4) | (2u << 29) : idesc;
-                        mma<PAIR, FP4>(d, ptx::smem_desc_join(a_lo + 2 * k, hi), ptx::smem_desc_join(b_lo + 2 * k, hi), id,
-                                       sfa + 4 * (k >> 1), sfb + 8 * (k >> 1), accumulate);
-                        accumulate = 1;
-                    }
-                    commit<PAIR>(ptx::smem_addr(&ctl->empty[s]));
-                    if (++s == p.stages) { s = 0; phase ^= 1; }
                 }
-                if (ok) commit<PAIR>(ptx::smem_addr(&ctl->acc_full[a]));
-            }
-            if (!ok) {                                // products in flight end before tensor memory is given up
-                commit<PAIR>(ptx::smem_addr(&ctl->drain));
-                const long long t0 = clock64();
-                while (!ptx::mbar_try_wait(ptx::smem_addr(&ctl->drain), 0) && clock64() - t0 < kGroupedWait / 8) {}
-            }
-        }
-    } else if (FP4 && warp >= kScaler) {
-        // Scales: 8 bytes a row and chunk, from rows that lie K / 32 bytes apart to the places in shared memory that the copy to tensor
-        // memory reads.  A team of four warps takes a part of two chunks, 16 bytes a row; a pair of CTAs has two teams in turn, which is
-        // 8192^3 in 249 -> 214 us, and with 32 bytes a row in registers and no turns 221.  A warp has every fourth group of 32 rows.
-        // (The stage that a team waits for is at most four chunks behind its last one and the ring has at least four stages: no phase of
-        // a barrier can be mistaken for the one two further on.)  Rows behind the matrices are read as their last one: their products
-        // are not stored.
-        constexpr int kTeams = kScaleWarps / 4;
-        const int k32 = p.K / 32, team = (warp - kScaler) >> 2, member = (warp - kScaler) & 3;
-        const bool vec = k32 % 16 == 0;
-        long long t = worker;
-        int c = c_begin, s = 0;
-        uint32_t phase = 0;
-        bool ok = true, fresh = true;                 // fresh: the next fetch is the first of its tile
-        const uint8_t* src[kScaleGroups];
-        auto fetch = [&](uint4 (&v)[kScaleGroups]) {
-            if (fresh) {
-                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
-                const int feature = tile.feature + (PAIR ? rank * kFeat : 0);
-#pragma unroll
-                for (int i = 0; i < kScaleGroups; ++i) {
-                    const int part = member + 4 * i;                            // 4 groups of W, then those of x
-                    const int r = (part & 3) * 8 + (lane >> 2) + 32 * (lane & 3) + (part < 8 ? 0 : 128);
-                    src[i] = part < 4 ? p.w_scale + ((size_t)tile.weights * p.N + min(feature + r, p.N - 1)) * k32
-                                       : p.x_scale + (size_t)min(tile.first + r, p.rows_cap - 1) * k32;
-                }
-                fresh = false;
-            }
-            const int off = (c & ~1) * 8;
-            if (vec) {
-#pragma unroll
-                for (int i = 0; i < kScaleGroups; ++i) v[i] = ldg128(src[i] + off);
-            } else {                                  // (words behind the row: its last one, for blocks that no product takes)
-#pragma unroll
-                for (int i = 0; i < kScaleGroups; ++i) {
-                    auto word = [&](int k) { return __ldg(reinterpret_cast<const uint32_t*>(src[i] + min(off + 4 * k, k32 - 4))); };
-                    v[i] = make_uint4(word(0), word(1), word(2), word(3));
-                }
-            }
-        };
-        auto advance = [&] {                          // to the next part, of whichever team
-            const int n = min(2 - (c & 1), c_end - c);
-            c += n;
-            s += n;
-            if (s >= p.stages) { s -= p.stages; phase ^= 1; }
-            if (c >= c_end) { c = c_begin; t += step; fresh = true; }
-        };
-        if (kTeams == 2 && team == 1 && t < total) advance();
-        uint4 v[kScaleGroups];
-        if (t < total) fetch(v);
-        while (t < total && ok) {
-            const int first = c, n = min(2 - (c & 1), c_end - c);
-            int at = s;
-            uint32_t ph = phase;
-            for (int k = 0; k < n; ++k) {
-                ok = __all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->empty[at]), ph ^ 1, ctl, p.dev_status));
-                if (!ok) break;
-                uint32_t* sa = reinterpret_cast<uint32_t*>(scales + at * (kScaleA + kScaleB)) + lane;
-                const bool odd = (first + k) & 1;
-#pragma unroll
-                for (int i = 0; i < kScaleGroups; ++i) {
-                    const int part = member + 4 * i;
-                    uint32_t* dst = sa + (part < 4 ? 0 : kScaleA / 4 + (part < 8 ? 0 : 128)) + (part & 3) * 32;
-                    dst[0] = odd ? v[i].z : v[i].x;
-                    dst[part < 4 ? 128 : 256] = odd ? v[i].w : v[i].y;
-                }
-                ptx::fence_proxy_async_smem();
+                ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) arrive_at(bar_at(&ctl->full[at]));
-                if (++at == p.stages) { at = 0; ph ^= 1; }
+                if (lane == 0) arrive_at(bar_at(&ctl->acc_empty[a]));
             }
-            advance();
-            if (kTeams == 2 && t < total) advance();
-            if (t < total) fetch(v);
         }
-    } else if (warp < kEpiWarps) {
-        constexpr int kEpiCols = 16 * (kEpiWarps / 4);
-        const int sub = warp & 3, part = warp >> 2;
-        const uint32_t stage = ptx::smem_addr(staging) + warp * kStagingBytes;
-        int it = 0;
-        for (long long t = worker; t < total; t += step, ++it) {
-            const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
-            const int a = PAIR ? it & 1 : 0;
-            const int feature = tile.feature + (PAIR ? rank * kFeat : 0) + 32 * sub;
-            uint64_t bias[4] = {0, 0, 0, 0};          // of features lane / 4 + {0, 8, 16, 24}, twice each
-            if (p.bias != nullptr && (PAIR || p.slices == 1))
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int f = min(feature + (lane >> 2) + 8 * i, p.N - 1);
-                    const float b = __uint_as_float((uint32_t)__ldg(p.bias + (size_t)tile.weights * p.N + f) << 16);
-                    bias[i] = pair_of(b, b);
-                }
-            if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->acc_full[a]), (PAIR ? it >> 1 : 0) & 1, ctl, p.dev_status)))
-                break;
-            ptx::tc_fence_after_sync();
-            const uint32_t acc = tmem + (a ? kAcc1 : 0) + ((uint32_t)(32 * sub) << 16);
-            if (!PAIR && p.slices > 1) {
-                // this slice's sums as [row][128 features] fp32 over the stages, which nothing reads any more
-                float* sums = reinterpret_cast<float*>(base);
-                for (int c = part * 16; c < tile.live; c += kEpiCols) {
-                    uint32_t r[16];
-                    ptx::tmem_ld16(acc + c, r);
-                    ptx::tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) sums[(c + i) * kFeat + 32 * sub + lane] = __uint_as_float(r[i]);
-                }
-            } else {
-                // 16 rows at a time, the next ones on their way out of tensor memory meanwhile
-                uint32_t ahead[16];
-                auto fetch = [&](int c) {
-                    tmem_ld_16x256b_x2(acc + c, ahead);
-                    tmem_ld_16x256b_x2(acc + (16u << 16) + c, ahead + 8);
-                };
-                if (part * 16 < tile.live) fetch(part * 16);
-                for (int c = part * 16; c < tile.live; c += kEpiCols) {
-                    uint64_t y[8];                                               // two rows of one feature
-                    ptx::tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        y[i] = add2(pair_of(__uint_as_float(ahead[2 * i]), __uint_as_float(ahead[2 * i + 1])), bias[(i >> 2) * 2 + (i & 1)]);
-                    if (c + kEpiCols < tile.live) fetch(c + kEpiCols);
+        // ---- the slices of a tile meet --------------------------------------------------------------------------------------
+        __syncwarp();
+        if (split) {
+            ptx::cluster_sync();
+            if (warp < kEpiWarps && !ctl->abort_flag) {
+                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t0, f_tiles, group);
+                // pieces of 8 features of a row, dealt over the slices' threads; slices are added in their order
+                for (int u = threadIdx.x * p.slices + slice; u < tile.live * (kFeat / 8); u += kEpiWarps * 32 * p.slices) {
+                    const int q = u / (kFeat / 8), j = u % (kFeat / 8), f = tile.feature + half * kFeat + 8 * j;
+                    if (f >= p.N) continue;
+                    float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    const uint32_t at = smem + (q * kFeat + 8 * j) * 4;
+                    for (int i = 0; i < p.slices; ++i) {
+                        const uint32_t from = ptx::map_rank(at, PAIR ? 2 * i + half : i);
+                        const float4 lo = ptx::ld_cluster_f4(from), hi = ptx::ld_cluster_f4(from + 16);
+                        y[0] += lo.x; y[1] += lo.y; y[2] += lo.z; y[3] += lo.w;
+                        y[4] += hi.x; y[5] += hi.y; y[6] += hi.z; y[7] += hi.w;
+                    }
+                    if (p.bias != nullptr) {
+                        const uint4 b = ldg128(p.bias + (size_t)tile.weights * p.N + f);
+                        y[0] += bf16_lo(b.x); y[1] += bf16_hi(b.x); y[2] += bf16_lo(b.y); y[3] += bf16_hi(b.y);
+                        y[4] += bf16_lo(b.z); y[5] += bf16_hi(b.z); y[6] += bf16_lo(b.w); y[7] += bf16_hi(b.w);
+                    }
                     if (p.activation == REGIONE_ACT_GELU_TANH)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = gelu_tanh(y[i]);
-                    uint32_t z[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float lo, hi;
-                        parts_of(y[i], lo, hi);
-                        z[i] = pack_bf16x2(lo, hi);
-                    }
-                    // row of the tile t at 64 t, its 16-byte pieces (8 features) turned by t / 2 so that eight rows meet eight banks
-                    const int row = (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1, turn = (row >> 1) & 3;
-                    if (PAIR) {                                                  // (the store of the step before)
-                        if (lane == 0) ptx::bulk_wait_read<0>();
-                        __syncwarp();
-                    }
-                    stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), z[0], z[1], z[2], z[3]);
-                    stmatrix_x4_trans(stage + row * 64 + (((piece + 2) ^ turn) << 4), z[4], z[5], z[6], z[7]);
-                    if (PAIR && c + 16 <= tile.live) {
-                        ptx::fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0 && feature < p.N) {
-                            store_out(&maps.out, stage, feature, tile.first + c);
-                            ptx::bulk_commit();
-                        }
-                    } else {
-                        __syncwarp();
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int q = (lane >> 2) + 8 * i, j = lane & 3;
-                            const uint4 v = *reinterpret_cast<const uint4*>(staging + warp * kStagingBytes + q * 64 + ((j ^ ((q >> 1) & 3)) << 4));
-                            if (c + q < tile.live && feature + 8 * j < p.N)
-                                *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + c + q) * p.out_stride + feature + 8 * j) = v;
-                        }
-                        __syncwarp();
-                    }
+                        for (int e = 0; e < 8; e += 2) parts_of(gelu_tanh(pair_of(y[e], y[e + 1])), y[e], y[e + 1]);
+                    uint4 o;
+                    o.x = pack_bf16x2(y[0], y[1]); o.y = pack_bf16x2(y[2], y[3]);
+                    o.z = pack_bf16x2(y[4], y[5]); o.w = pack_bf16x2(y[6], y[7]);
+                    *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + q) * p.out_stride + f) = o;
                 }
             }
-            ptx::tc_fence_before_sync();
-            __syncwarp();
-            if (PAIR && lane == 0) arrive_at(bar_at(&ctl->acc_empty[a]));
+            ptx::fence_proxy_async_smem();                // (the ring's next copies write where the sums were)
+            ptx::cluster_sync();
         }
-        if (PAIR && lane == 0) ptx::bulk_wait_all();
     }
 
-    // ---- the slices of a tile meet --------------------------------------------------------------------------------------
-    __syncwarp();
-    if (!PAIR && p.slices > 1) {
-        ptx::cluster_sync();
-        if (warp < kEpiWarps && worker < total && !ctl->abort_flag) {
-            const GroupedTile tile = tile_at<PAIR>(p, ctl, worker, f_tiles, group);
-            // pieces of 8 features of a row, dealt over the cluster's threads; slices are added in their order
-            for (int u = threadIdx.x * p.slices + rank; u < tile.live * (kFeat / 8); u += kEpiWarps * 32 * p.slices) {
-                const int q = u / (kFeat / 8), j = u % (kFeat / 8), f = tile.feature + 8 * j;
-                if (f >= p.N) continue;
-                float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                const uint32_t at = smem + (q * kFeat + 8 * j) * 4;
-                for (int s = 0; s < p.slices; ++s) {
-                    const uint32_t from = ptx::map_rank(at, s);
-                    const float4 lo = ptx::ld_cluster_f4(from), hi = ptx::ld_cluster_f4(from + 16);
-                    y[0] += lo.x; y[1] += lo.y; y[2] += lo.z; y[3] += lo.w;
-                    y[4] += hi.x; y[5] += hi.y; y[6] += hi.z; y[7] += hi.w;
-                }
-                if (p.bias != nullptr) {
-                    const uint4 b = ldg128(p.bias + (size_t)tile.weights * p.N + f);
-                    y[0] += bf16_lo(b.x); y[1] += bf16_hi(b.x); y[2] += bf16_lo(b.y); y[3] += bf16_hi(b.y);
-                    y[4] += bf16_lo(b.z); y[5] += bf16_hi(b.z); y[6] += bf16_lo(b.w); y[7] += bf16_hi(b.w);
-                }
-                if (p.activation == REGIONE_ACT_GELU_TANH)
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) parts_of(gelu_tanh(pair_of(y[e], y[e + 1])), y[e], y[e + 1]);
-                uint4 o;
-                o.x = pack_bf16x2(y[0], y[1]); o.y = pack_bf16x2(y[2], y[3]);
-                o.z = pack_bf16x2(y[4], y[5]); o.w = pack_bf16x2(y[6], y[7]);
-                *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + q) * p.out_stride + f) = o;
-            }
+    if (PAIR && warp < kEpiWarps && lane == 0) ptx::bulk_wait_all();
+    if (!ok && leader && elected && warp == kProducer) { // copies in flight land before shared memory is given up
+        for (int i = min(filled, stages); i > 0; --i) {
+            int q = s - i;
+            uint32_t ph = phase;
+            if (q < 0) { q += stages; ph ^= 1; }
+            const long long t0 = clock64();
+            while (!ptx::mbar_try_wait(ptx::smem_addr(&ctl->full[q]), ph) && clock64() - t0 < kGroupedWait / 8) {}
         }
     }
+    if (!ok && leader && elected && warp == kIssuer) {  // products in flight end before tensor memory is given up
+        commit<PAIR>(ptx::smem_addr(&ctl->drain), pair_mask);
+        const long long t0 = clock64();
+        while (!ptx::mbar_try_wait(ptx::smem_addr(&ctl->drain), 0) && clock64() - t0 < kGroupedWait / 8) {}
+    }
+    __syncwarp();
     ptx::tc_fence_before_sync();
     if (cluster > 1) ptx::cluster_sync(); else __syncthreads();
     ptx::tc_fence_after_sync();
@@ -692,30 +703,20 @@ static bool grouped_map(CUtensorMap* map, bool fp4, int rank, const void* at, lo
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool FP4, bool PAIR> static size_t grouped_smem(int stages, int stage_bytes) {
-    return 1024 + (size_t)stages * (stage_bytes + (FP4 ? kScaleA + kScaleB : 0)) + Roles<FP4, PAIR>::kEpi * kStagingBytes + sizeof(GroupedControl);
+template <bool FP4, bool PAIR> static size_t grouped_smem(int ring_bytes) {
+    return 1024 + ring_bytes + Roles<FP4, PAIR>::kEpi * kStagingBytes + sizeof(GroupedControl);
 }
+// One CTA on an SM of a pair, two without.
+constexpr int kSmemCta = 232448, kSmemHalf = 113 * 1024;
+template <bool FP4, bool PAIR> static int grouped_ring(int smem) { return (smem - (int)grouped_smem<FP4, PAIR>(0)) & ~1023; }
 
-template <bool FP4, bool PAIR> static bool grouped_configure(int dev) {
-    static int configured[kMaxDevices] = {};
-    if (__atomic_load_n(&configured[dev], __ATOMIC_ACQUIRE)) return true;
-    if (cudaFuncSetAttribute(grouped_kernel<FP4, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)grouped_smem<FP4, PAIR>(kMaxStages, 2 * kTileBytes)) !=
-        cudaSuccess)
-        return false;
-    __atomic_store_n(&configured[dev], 1, __ATOMIC_RELEASE);
-    return true;
-}
-
-template <bool FP4, bool PAIR>
-static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, unsigned blocks, int cluster, cudaStream_t st) {
-    const int dev = current_device();
-    if (dev < 0 || !grouped_configure<FP4, PAIR>(dev)) return REGIONE_CUDA_ERROR;
-    cudaLaunchConfig_t cfg = {};
+template <bool FP4, bool PAIR> static void grouped_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, unsigned blocks, int cluster,
+                                                          size_t smem, cudaStream_t st) {
+    cfg = {};
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(Roles<FP4, PAIR>::kThreads);
-    cfg.dynamicSmemBytes = grouped_smem<FP4, PAIR>(p.stages, p.stage_bytes);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -723,32 +724,74 @@ static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, unsigne
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
+}
+
+// Clusters of pairs that the device holds at one time, by their slices of K (1, 2, 4); 0 where the kernel cannot be set up.
+template <bool FP4> static const int* grouped_pairs(int dev) {
+    static int held[kMaxDevices][4] = {};
+    int* h = held[dev];
+    if (__atomic_load_n(&h[3], __ATOMIC_ACQUIRE)) return h;
+    const size_t smem = grouped_smem<FP4, true>(grouped_ring<FP4, true>(kSmemCta));
+    if (cudaFuncSetAttribute(grouped_kernel<FP4, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess ||
+        cudaFuncSetAttribute(grouped_kernel<FP4, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess)
+        return nullptr;
+    for (int i = 0; i < 3; ++i) {
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[2];
+        grouped_config<FP4, true>(cfg, attr, 2u << i, 2 << i, smem, nullptr);
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, grouped_kernel<FP4, true>, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            n = 0;
+        }
+        __atomic_store_n(&h[i], n, __ATOMIC_RELAXED);
+    }
+    __atomic_store_n(&h[3], 1, __ATOMIC_RELEASE);
+    return h;
+}
+
+template <bool FP4, bool PAIR>
+static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, long long clusters, cudaStream_t st) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    const int cluster = (PAIR ? 2 : 1) * p.slices;
+    grouped_config<FP4, PAIR>(cfg, attr, (unsigned)(clusters * cluster), cluster, grouped_smem<FP4, PAIR>(p.ring_bytes), st);
     return launch_status(launch_counted(&cfg, grouped_kernel<FP4, PAIR>, maps, p));
 }
 
 template <bool FP4>
 static int grouped_run(const void* x, long long x_row_bytes, const void* w, GroupedArgs p, cudaStream_t st) {
     constexpr int kElems = FP4 ? 256 : 64;
-    const int sms = sm_count();
+    const int dev = current_device(), sms = sm_count();
+    const int* held = dev < 0 ? nullptr : grouped_pairs<FP4>(dev);
+    if (!held) return REGIONE_CUDA_ERROR;
     p.chunks = (p.K + kElems - 1) / kElems;
     const long long groups = std::min(p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
     const long long f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
-    // What the launch will take, in cycles, if every row of the buffer is live and the groups are alike: rounds of tiles times what a
-    // chunk takes the tensor core or the way from L2 (see the plan in the kernel), and what a launch takes besides.
-    long long best = 0x7fffffffffffffffLL;
-    for (int width = 32; width <= (FP4 ? 224 : 256); width += 32) {
-        const long long rounds = (f_pairs * groups * ((each + width - 1) / width) + sms / 2 - 1) / (sms / 2);
-        best = std::min(best, rounds * p.chunks * std::max(2 * width, (256 + width) * 9 / 8) + 3000);
-    }
+    // What the launch will take, in cycles, if every row of the buffer is live and the groups are alike: rounds of tiles, each the chunks of
+    // a slice times what a chunk takes the tensor core or the way from L2 (see the plan in the kernel), and the way out of the
+    // slices' sums; and what a launch takes besides.
+    long long best = 0x7fffffffffffffffLL, clusters = 0;
     bool pair = true;
-    long long tiles = 0;
     p.slices = 1;
     p.width = 0;
+    for (int i = 0; i < 3; ++i) {
+        const int slices = 1 << i;
+        if (held[i] < 1 || (i > 0 && 8 * slices > p.chunks)) continue;
+        for (int width = 32; width <= (FP4 ? 224 : 256); width += 32) {
+            const long long tiles = f_pairs * groups * ((each + width - 1) / width), rounds = (tiles + held[i] - 1) / held[i];
+            const long long mine = (p.chunks + slices - 1) / slices;
+            const long long cost = rounds * (mine * std::max(2 * width, (256 + width) * 9 / 8) + (i > 0 ? 2000 + 12 * width : 0)) + 3000;
+            if (cost >= best) continue;
+            best = cost;
+            p.slices = slices;
+            clusters = held[i];
+        }
+    }
     for (int width = 16; width <= 128; width *= 2) {
-        const long long n = f_tiles * (p.rows_cap / width + groups);            // at most, however the rows are spread over the groups
-        if (n > 0x7fffffffLL / 8) continue;
+        const long long tiles = f_tiles * (p.rows_cap / width + groups);        // at most, however the rows are spread over the groups
         for (int slices = 1; slices <= 8 && 2 * slices <= std::max(p.chunks, 2); slices *= 2) {
-            const long long rounds = (n * slices + sms - 1) / sms, mine = (p.chunks + slices - 1) / slices;
+            const long long rounds = (tiles * slices + sms - 1) / sms, mine = (p.chunks + slices - 1) / slices;
             const long long cost = rounds * mine * std::max(2 * width, (128 + width) * 9 / 4) + (slices > 1 ? 2500 : 1500) +
                                    (rounds - 1) * 1500;
             if (cost >= best) continue;
@@ -756,19 +799,18 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
             pair = false;
             p.width = width;
             p.slices = slices;
-            tiles = n;
+            clusters = std::min(tiles, 4LL * sms);
         }
     }
+    if (pair && clusters == 0) return REGIONE_CUDA_ERROR;
     if (pair) {
-        p.stages = kMaxStages;
-        p.stage_bytes = 2 * kTileBytes;
+        p.ring_bytes = grouped_ring<FP4, true>(kSmemCta);
         p.tmem_columns = 512;
         p.scale_column = 448;
     } else {
-        // two CTAs an SM, with all of their part of K in the ring if it fits; at least four stages (see the scales)
-        p.stage_bytes = kTileBytes + p.width * kChunkBytes;
-        const int room = (int)((113 * 1024 - grouped_smem<FP4, false>(0, 0)) / (p.stage_bytes + (FP4 ? kScaleA + kScaleB : 0)));
-        p.stages = std::max(4, std::min({kMaxStages, room, (p.chunks + p.slices - 1) / p.slices}));
+        // two CTAs an SM, with a slice's chunks in the ring if they fit; at least four stages (see the scales)
+        const int stage = kTileBytes + p.width * kChunkBytes + (FP4 ? kScaleA + kScaleB : 0), mine = (p.chunks + p.slices - 1) / p.slices;
+        p.ring_bytes = std::max(4 * stage, std::min(grouped_ring<FP4, false>(kSmemHalf), std::min(kMaxStages, mine) * stage));
         p.scale_column = p.width <= 64 ? 64 : 128;
         p.tmem_columns = FP4 ? 2 * p.scale_column : std::max(32, p.width);
     }
@@ -784,8 +826,7 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     }
     if (!ok) return REGIONE_CUDA_ERROR;
-    if (pair) return grouped_launch<FP4, true>(maps, p, (unsigned)(sms / 2 * 2), 2, st);
-    return grouped_launch<FP4, false>(maps, p, (unsigned)(tiles * p.slices), p.slices, st);
+    return pair ? grouped_launch<FP4, true>(maps, p, clusters, st) : grouped_launch<FP4, false>(maps, p, clusters, st);
 }
 
 }  // namespace regione

@@ -63,7 +63,12 @@ MANY = [([0], [700], 700, 1, 512, 2048), ([0, 256], [256, 1075], 1300, 2, 1024, 
         ([0, 600, 1300, 1900], [600, 1200, 1900, 2333], 2400, 2, 384, 768)]
 
 
-@pytest.mark.parametrize("case", FEW + MANY, ids=lambda c: f"{c[2]}x{c[4]}x{c[5]}g{len(c[0])}")
+# the slices of K of a pair's tiles meet, also over several rounds of tiles (groups far from alike)
+SLICED = [([0], [640], 640, 1, 4096, 1024), ([0, 60, 70], [60, 70, 2000], 2000, 3, 8192, 264), ([0, 10], [10, 4000], 4000, 2, 4224, 136),
+          ([0, 1, 2, 3, 4, 5, 6, 7], [1, 2, 3, 4, 5, 6, 7, 3000], 3000, 8, 2176, 72)]
+
+
+@pytest.mark.parametrize("case", FEW + MANY + SLICED, ids=lambda c: f"{c[2]}x{c[4]}x{c[5]}g{len(c[0])}")
 @pytest.mark.parametrize("fp4", [False, True], ids=["bf16", "mxfp4"])
 def test_whole_numbers_are_exact(fp4, case):
     begin, end, rows, sets, K, N = case
