@@ -255,16 +255,117 @@ __device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const Group
     return tile;
 }
 
-template <bool FP4, bool PAIR>
+// Scales of the tiles [t0, t_end): 8 bytes a row and chunk, from rows that lie K / 32 bytes apart to the places in shared memory that
+// the copy to tensor memory reads.  A team of four warps takes a part of two chunks, 16 bytes a row, a warp every fourth group
+// of 32 rows; a pair of CTAs has two teams that take turns (8192^3: 249 us with one team, 209 with two).  Loads for the next part
+// are not sent ahead: the proxy fence would wait for them.  The stage that a team waits for is at most four chunks behind its last
+// one and the ring has at least four stages: no phase of a barrier can be mistaken for the one two further on.
+// VEC, rows on 16 bytes: a lane reads its row's 16 bytes, 32 rows in one load.  Else four lanes read a word each, 8 rows in one load: as
+// many lines of the L1 a row (2 x 4992 x 296 for four times 764 rows: 14.9 us, a lane with the four words of its row 20.8).
+// Rows behind the matrices are read as their last one, words behind a row as its last: what they scale is not stored.
+struct ScaleRole {
+    GroupedControl* ctl;
+    uint8_t* scales;
+    int stages, f_tiles, workers, rank, warp, lane, c_begin, c_end;
+    long long t0, t_end;
+    int s, group;                                     // the ring's next stage, the last tile's group
+    uint32_t phase;
+};
+template <bool PAIR, bool VEC>
+__device__ __forceinline__ bool bring_scales(const GroupedArgs& p, const ScaleRole r) {
+    constexpr int kTeams = PAIR ? 2 : 1, kGroups = PAIR ? 3 : 2;     // groups of 32 rows a warp: 128 rows of W, up to 256 (128) of x
+    int s = r.s, group = r.group;
+    uint32_t phase = r.phase;
+    const int k32 = p.K / 32, team = r.warp >> 2, member = r.warp & 3, lane = r.lane;
+    const int in_group = VEC ? (lane >> 2) + 32 * (lane & 3) : (lane >> 4) + 32 * ((lane >> 2) & 3);
+    long long t = r.t0;
+    int c = r.c_begin;
+    bool fresh = true;                                // the next fetch is the first of its tile
+    const uint8_t* src[kGroups];
+    int room[kGroups];                                // rows of the matrix behind the lane's first
+    auto fetch = [&](uint4 (&v)[kGroups]) {
+        if (fresh) {
+            const GroupedTile tile = tile_at<PAIR>(p, r.ctl, (int)t, r.f_tiles, group);
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {       // part i: 4 groups of W, then those of x
+                const int row = (i == 0 ? tile.feature + (PAIR ? r.rank & 1 : 0) * kFeat : tile.first) + member * 8 + in_group + (i == 2 ? 128 : 0);
+                const int last = (i == 0 ? p.N : p.rows_cap) - 1;
+                src[i] = (i == 0 ? p.w_scale + (size_t)tile.weights * p.N * k32 : p.x_scale) + (size_t)min(row, last) * k32;
+                room[i] = max(last - row, 0);
+            }
+            fresh = false;
+        }
+        const int off = (c & ~1) * 8;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            if constexpr (VEC) {
+                v[i] = ldg128(src[i] + off);
+            } else {
+                const int word = min(off + 4 * (lane & 3), k32 - 4);
+                auto at = [&](int n) { return __ldg(reinterpret_cast<const uint32_t*>(src[i] + (min(2 * n, room[i]) * k32 + word))); };
+                v[i] = make_uint4(at(0), at(1), at(2), at(3));
+            }
+        }
+    };
+    auto advance = [&] {                              // to the next part, of whichever team
+        const int n = min(2 - (c & 1), r.c_end - c);
+        c += n;
+        s += n;
+        if (s >= r.stages) { s -= r.stages; phase ^= 1; }
+        if (c >= r.c_end) { c = r.c_begin; t += r.workers; fresh = true; }
+    };
+    if (kTeams == 2 && team == 1 && t < r.t_end) advance();
+    uint4 v[kGroups];
+    if (t < r.t_end) fetch(v);
+    while (t < r.t_end) {
+        const int first = c, n = min(2 - (c & 1), r.c_end - c);
+        int at = s;
+        uint32_t turn = phase;
+        for (int k = 0; k < n; ++k) {
+            if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&r.ctl->empty[at]), turn ^ 1, r.ctl, p.dev_status))) return false;
+            uint32_t* base = reinterpret_cast<uint32_t*>(r.scales + at * (kScaleA + kScaleB)) + member * 32;
+            const bool odd = (first + k) & 1;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                uint32_t* dst = base + (i == 0 ? 0 : kScaleA / 4 + (i == 1 ? 0 : 128));
+                constexpr int kNextW = 128, kNextX = 256;             // words to the second 128 elements
+                const int next = i == 0 ? kNextW : kNextX;
+                if constexpr (VEC) {
+                    dst[lane] = odd ? v[i].z : v[i].x;
+                    dst[next + lane] = odd ? v[i].w : v[i].y;
+                } else if (((lane >> 1) & 1) == odd) {
+                    dst += (lane & 1) * next + (lane >> 2);
+                    dst[0] = v[i].x;
+                    dst[8] = v[i].y;
+                    dst[16] = v[i].z;
+                    dst[24] = v[i].w;
+                }
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                const uint32_t bar = ptx::smem_addr(&r.ctl->full[at]);
+                arrive_at(PAIR ? ptx::map_rank(bar, r.rank & ~1) : bar);
+            }
+            if (++at == r.stages) { at = 0; turn ^= 1; }
+        }
+        advance();
+        if (kTeams == 2 && t < r.t_end) advance();
+        if (t < r.t_end) fetch(v);
+    }
+    return true;
+}
+
+// VEC: of 4-bit operands, K is a multiple of 512 (see bring_scales).
+template <bool FP4, bool PAIR, bool VEC>
 __global__ void __launch_bounds__(Roles<FP4, PAIR>::kThreads, PAIR ? 1 : 2)
 grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__ GroupedArgs p) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     constexpr int kElems = FP4 ? 256 : 64;            // of K in a chunk
     constexpr int kMaxWidth = PAIR ? (FP4 ? 224 : 256) : 128;
     constexpr int kAcc1 = PAIR ? kMaxWidth : 0;       // column of the second accumulator
-    constexpr int kEpiWarps = Roles<FP4, PAIR>::kEpi, kScaleWarps = Roles<FP4, PAIR>::kScale;
+    constexpr int kEpiWarps = Roles<FP4, PAIR>::kEpi;
     constexpr int kProducer = kEpiWarps, kIssuer = kEpiWarps + 1, kScaler = kEpiWarps + 2;
-    constexpr int kScaleGroups = PAIR ? 3 : 2;         // of 32 rows, a warp of scales: 128 rows of W and up to 256 (128) of x, four warps to a chunk
     const uint32_t smem = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
     uint8_t* base = smem_raw + (smem - ptx::smem_addr(smem_raw));
     uint8_t* staging = base + p.ring_bytes;
@@ -448,80 +549,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 }
             }
         } else if (FP4 && warp >= kScaler) {
-            // Scales: 8 bytes a row and chunk, from rows that lie K / 32 bytes apart to the places in shared memory that the copy to tensor
-            // memory reads.  A team of four warps takes a part of two chunks, 16 bytes a row; a pair of CTAs has two teams in turn, which is
-            // 8192^3 in 249 -> 214 us, and with 32 bytes a row in registers and no turns 221.  A warp has every fourth group of 32 rows.
-            // (The stage that a team waits for is at most four chunks behind its last one and the ring has at least four stages: no phase of
-            // a barrier can be mistaken for the one two further on.)  Rows behind the matrices are read as their last one: their products
-            // are not stored.
-            constexpr int kTeams = kScaleWarps / 4;
-            const int k32 = p.K / 32, team = (warp - kScaler) >> 2, member = (warp - kScaler) & 3;
-            const bool vec = k32 % 16 == 0;
-            long long t = t0;
-            int c = c_begin, q = s;                       // the next chunk and its stage
-            uint32_t turn = phase;
-            bool fresh = true;                            // the next fetch is the first of its tile
-            const uint8_t* src[kScaleGroups];
-            auto fetch = [&](uint4 (&v)[kScaleGroups]) {
-                if (fresh) {
-                    const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
-                    const int feature = tile.feature + half * kFeat;
-#pragma unroll
-                    for (int i = 0; i < kScaleGroups; ++i) {
-                        const int part = member + 4 * i;                            // 4 groups of W, then those of x
-                        const int r = (part & 3) * 8 + (lane >> 2) + 32 * (lane & 3) + (part < 8 ? 0 : 128);
-                        src[i] = part < 4 ? p.w_scale + ((size_t)tile.weights * p.N + min(feature + r, p.N - 1)) * k32
-                                           : p.x_scale + (size_t)min(tile.first + r, p.rows_cap - 1) * k32;
-                    }
-                    fresh = false;
-                }
-                const int off = (c & ~1) * 8;
-                if (vec) {
-#pragma unroll
-                    for (int i = 0; i < kScaleGroups; ++i) v[i] = ldg128(src[i] + off);
-                } else {                                  // (words behind the row: its last one, for blocks that no product takes)
-#pragma unroll
-                    for (int i = 0; i < kScaleGroups; ++i) {
-                        auto word = [&](int k) { return __ldg(reinterpret_cast<const uint32_t*>(src[i] + min(off + 4 * k, k32 - 4))); };
-                        v[i] = make_uint4(word(0), word(1), word(2), word(3));
-                    }
-                }
-            };
-            auto advance = [&] {                          // to the next part, of whichever team
-                const int n = min(2 - (c & 1), c_end - c);
-                c += n;
-                q += n;
-                if (q >= stages) { q -= stages; turn ^= 1; }
-                if (c >= c_end) { c = c_begin; t += workers; fresh = true; }
-            };
-            if (kTeams == 2 && team == 1 && t < t_end) advance();
-            uint4 v[kScaleGroups];
-            if (t < t_end) fetch(v);
-            while (t < t_end && ok) {
-                const int first = c, n = min(2 - (c & 1), c_end - c);
-                int at = q;
-                uint32_t ph = turn;
-                for (int k = 0; k < n; ++k) {
-                    ok = __all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->empty[at]), ph ^ 1, ctl, p.dev_status));
-                    if (!ok) break;
-                    uint32_t* sa = reinterpret_cast<uint32_t*>(scales + at * (kScaleA + kScaleB)) + lane;
-                    const bool odd = (first + k) & 1;
-#pragma unroll
-                    for (int i = 0; i < kScaleGroups; ++i) {
-                        const int part = member + 4 * i;
-                        uint32_t* dst = sa + (part < 4 ? 0 : kScaleA / 4 + (part < 8 ? 0 : 128)) + (part & 3) * 32;
-                        dst[0] = odd ? v[i].z : v[i].x;
-                        dst[part < 4 ? 128 : 256] = odd ? v[i].w : v[i].y;
-                    }
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) arrive_at(bar_at(&ctl->full[at]));
-                    if (++at == stages) { at = 0; ph ^= 1; }
-                }
-                advance();
-                if (kTeams == 2 && t < t_end) advance();
-                if (t < t_end) fetch(v);
-            }
+            const ScaleRole role = {ctl, scales, stages, f_tiles, workers, rank, warp - kScaler, lane, c_begin, c_end, t0, t_end, s, group, phase};
+            ok = bring_scales<PAIR, VEC>(p, role) && ok;
             if (split) {                                  // where the ring stands behind this slice's chunks
                 s += c_end - c_begin;
                 while (s >= stages) { s -= stages; phase ^= 1; }
@@ -624,13 +653,21 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 for (int u = threadIdx.x * p.slices + slice; u < tile.live * (kFeat / 8); u += kEpiWarps * 32 * p.slices) {
                     const int q = u / (kFeat / 8), j = u % (kFeat / 8), f = tile.feature + half * kFeat + 8 * j;
                     if (f >= p.N) continue;
-                    float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                     const uint32_t at = smem + (q * kFeat + 8 * j) * 4;
-                    for (int i = 0; i < p.slices; ++i) {
-                        const uint32_t from = ptx::map_rank(at, PAIR ? 2 * i + half : i);
-                        const float4 lo = ptx::ld_cluster_f4(from), hi = ptx::ld_cluster_f4(from + 16);
-                        y[0] += lo.x; y[1] += lo.y; y[2] += lo.z; y[3] += lo.w;
-                        y[4] += hi.x; y[5] += hi.y; y[6] += hi.z; y[7] += hi.w;
+                    float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    for (int i0 = 0; i0 < p.slices; i0 += 2) {                   // (two at a time, an even number)
+                        float4 lo[2], hi[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t from = ptx::map_rank(at, PAIR ? 2 * (i0 + i) + half : i0 + i);
+                            lo[i] = ptx::ld_cluster_f4(from);
+                            hi[i] = ptx::ld_cluster_f4(from + 16);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            y[0] += lo[i].x; y[1] += lo[i].y; y[2] += lo[i].z; y[3] += lo[i].w;
+                            y[4] += hi[i].x; y[5] += hi[i].y; y[6] += hi[i].z; y[7] += hi[i].w;
+                        }
                     }
                     if (p.bias != nullptr) {
                         const uint4 b = ldg128(p.bias + (size_t)tile.weights * p.N + f);
@@ -727,20 +764,20 @@ template <bool FP4, bool PAIR> static void grouped_config(cudaLaunchConfig_t& cf
 }
 
 // Clusters of pairs that the device holds at one time, by their slices of K (1, 2, 4); 0 where the kernel cannot be set up.
-template <bool FP4> static const int* grouped_pairs(int dev) {
+template <bool FP4, bool VEC> static const int* grouped_pairs(int dev) {
     static int held[kMaxDevices][4] = {};
     int* h = held[dev];
     if (__atomic_load_n(&h[3], __ATOMIC_ACQUIRE)) return h;
     const size_t smem = grouped_smem<FP4, true>(grouped_ring<FP4, true>(kSmemCta));
-    if (cudaFuncSetAttribute(grouped_kernel<FP4, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess ||
-        cudaFuncSetAttribute(grouped_kernel<FP4, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess)
+    if (cudaFuncSetAttribute(grouped_kernel<FP4, true, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess ||
+        cudaFuncSetAttribute(grouped_kernel<FP4, false, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess)
         return nullptr;
     for (int i = 0; i < 3; ++i) {
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attr[2];
         grouped_config<FP4, true>(cfg, attr, 2u << i, 2 << i, smem, nullptr);
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, grouped_kernel<FP4, true>, &cfg) != cudaSuccess) {
+        if (cudaOccupancyMaxActiveClusters(&n, grouped_kernel<FP4, true, VEC>, &cfg) != cudaSuccess) {
             cudaGetLastError();
             n = 0;
         }
@@ -750,27 +787,27 @@ template <bool FP4> static const int* grouped_pairs(int dev) {
     return h;
 }
 
-template <bool FP4, bool PAIR>
+template <bool FP4, bool PAIR, bool VEC>
 static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, long long clusters, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     const int cluster = (PAIR ? 2 : 1) * p.slices;
     grouped_config<FP4, PAIR>(cfg, attr, (unsigned)(clusters * cluster), cluster, grouped_smem<FP4, PAIR>(p.ring_bytes), st);
-    return launch_status(launch_counted(&cfg, grouped_kernel<FP4, PAIR>, maps, p));
+    return launch_status(launch_counted(&cfg, grouped_kernel<FP4, PAIR, VEC>, maps, p));
 }
 
-template <bool FP4>
+template <bool FP4, bool VEC>
 static int grouped_run(const void* x, long long x_row_bytes, const void* w, GroupedArgs p, cudaStream_t st) {
     constexpr int kElems = FP4 ? 256 : 64;
     const int dev = current_device(), sms = sm_count();
-    const int* held = dev < 0 ? nullptr : grouped_pairs<FP4>(dev);
+    const int* held = dev < 0 ? nullptr : grouped_pairs<FP4, VEC>(dev);
     if (!held) return REGIONE_CUDA_ERROR;
     p.chunks = (p.K + kElems - 1) / kElems;
     const long long groups = std::min(p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
     const long long f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
-    // What the launch will take, in cycles, if every row of the buffer is live and the groups are alike: rounds of tiles, each the chunks of
-    // a slice times what a chunk takes the tensor core or the way from L2 (see the plan in the kernel), and the way out of the
-    // slices' sums; and what a launch takes besides.
+    // What the launch will take, in ns, if every row of the buffer is live and the groups are alike: what a launch takes before and behind
+    // its tiles, and rounds of tiles, each the chunks of a slice times what a chunk takes (no less than 200 by latency; 105 bytes
+    // a ns to an SM; the tensor core), and the way of the slices' sums to each other.
     long long best = 0x7fffffffffffffffLL, clusters = 0;
     bool pair = true;
     p.slices = 1;
@@ -780,8 +817,8 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
         if (held[i] < 1 || (i > 0 && 8 * slices > p.chunks)) continue;
         for (int width = 32; width <= (FP4 ? 224 : 256); width += 32) {
             const long long tiles = f_pairs * groups * ((each + width - 1) / width), rounds = (tiles + held[i] - 1) / held[i];
-            const long long mine = (p.chunks + slices - 1) / slices;
-            const long long cost = rounds * (mine * std::max(2 * width, (256 + width) * 9 / 8) + (i > 0 ? 2000 + 12 * width : 0)) + 3000;
+            const long long mine = (p.chunks + slices - 1) / slices, chunk = std::max(200, std::max(width * 14 / 13, 156 + width * 8 / 13));
+            const long long cost = rounds * (mine * chunk + (i > 0 ? 2500 + 18 * width : 0)) + 6300;
             if (cost >= best) continue;
             best = cost;
             p.slices = slices;
@@ -792,8 +829,8 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
         const long long tiles = f_tiles * (p.rows_cap / width + groups);        // at most, however the rows are spread over the groups
         for (int slices = 1; slices <= 8 && 2 * slices <= std::max(p.chunks, 2); slices *= 2) {
             const long long rounds = (tiles * slices + sms - 1) / sms, mine = (p.chunks + slices - 1) / slices;
-            const long long cost = rounds * mine * std::max(2 * width, (128 + width) * 9 / 4) + (slices > 1 ? 2500 : 1500) +
-                                   (rounds - 1) * 1500;
+            const long long chunk = std::max(200, 156 + width * 16 / 13);
+            const long long cost = rounds * (mine * chunk + (slices > 1 ? 2000 + 18 * width : 0)) + (rounds - 1) * 800 + 4300;
             if (cost >= best) continue;
             best = cost;
             pair = false;
@@ -826,7 +863,7 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     }
     if (!ok) return REGIONE_CUDA_ERROR;
-    return pair ? grouped_launch<FP4, true>(maps, p, clusters, st) : grouped_launch<FP4, false>(maps, p, clusters, st);
+    return pair ? grouped_launch<FP4, true, VEC>(maps, p, clusters, st) : grouped_launch<FP4, false, VEC>(maps, p, clusters, st);
 }
 
 }  // namespace regione
@@ -861,7 +898,7 @@ extern "C" int regione_grouped_matmul(const regione_bf16* x, int64_t x_stride, c
     GroupedArgs p = {};
     p.row_begin = row_begin; p.row_end = row_end; p.groups = groups; p.n_weights = n_weights; p.rows_cap = rows_cap;
     p.K = K; p.N = N; p.bias = bias; p.activation = activation; p.out = out; p.out_stride = out_stride; p.dev_status = dev_status;
-    return grouped_run<false>(x, 2 * x_stride, w, p, (cudaStream_t)stream);
+    return grouped_run<false, false>(x, 2 * x_stride, w, p, (cudaStream_t)stream);
 }
 
 extern "C" int regione_mxfp4_grouped_matmul(const uint8_t* x_q, const uint8_t* x_scale, const uint8_t* w_q, const uint8_t* w_scale,
@@ -877,5 +914,6 @@ extern "C" int regione_mxfp4_grouped_matmul(const uint8_t* x_q, const uint8_t* x
     p.row_begin = row_begin; p.row_end = row_end; p.groups = groups; p.n_weights = n_weights; p.rows_cap = rows_cap;
     p.K = K; p.N = N; p.bias = bias; p.activation = activation; p.out = out; p.out_stride = out_stride; p.dev_status = dev_status;
     p.x_scale = x_scale; p.w_scale = w_scale;
-    return grouped_run<true>(x_q, K / 2, w_q, p, (cudaStream_t)stream);
+    return K % 512 ? grouped_run<true, false>(x_q, K / 2, w_q, p, (cudaStream_t)stream)
+                   : grouped_run<true, true>(x_q, K / 2, w_q, p, (cudaStream_t)stream);
 }
