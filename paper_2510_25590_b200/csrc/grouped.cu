@@ -59,7 +59,8 @@ struct GroupedControl {
     int width, total;                                 // of the plan: rows of a tile at most, tiles
     int cost[8];
     int first[kMaxGroups + 1];                        // of a group: row tiles ahead of it,
-    int begin[kMaxGroups], rows[kMaxGroups];          // its first row, how many
+    int begin[kMaxGroups], rows[kMaxGroups];          // its first row, how many,
+    int16_t widths[kMaxGroups];                       // rows of its tiles, which are even
 };
 
 // ---- instructions that the pair of CTAs and the scaled product need -------------------------------------------
@@ -239,18 +240,18 @@ struct GroupedTile {
 template <bool PAIR>
 __device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const GroupedControl* ctl, int t, int f_tiles, int& group) {
     while (ctl->first[group + 1] * f_tiles <= t) ++group;
-    const int ahead = ctl->first[group], n = ctl->first[group + 1] - ahead, rows = ctl->rows[group];
-    int in = t - ahead * f_tiles;
-    const int block = f_tiles <= 8 ? 0 : in / (8 * n);
-    in -= block * 8 * n;
-    const int wide = min(8, f_tiles - block * 8), at = in / wide;
-    constexpr int kStep = PAIR ? 32 : 16;
-    const int width = ((rows + n - 1) / n + kStep - 1) & ~(kStep - 1);         // n even tiles
+    const int ahead = ctl->first[group], n = ctl->first[group + 1] - ahead, width = ctl->widths[group];
+    int in = t - ahead * f_tiles, block = 0;
+    if (f_tiles > 8 && in >= 8 * n) {
+        block = in / (8 * n);
+        in -= block * 8 * n;
+    }
+    const int wide = min(8, f_tiles - block * 8), at = wide == 8 ? in >> 3 : in / wide;
     GroupedTile tile;
     tile.first = ctl->begin[group] + at * width;
-    tile.live = min(width, rows - at * width);
+    tile.live = min(width, ctl->rows[group] - at * width);
     tile.width = width;
-    tile.weights = group % p.n_weights;
+    tile.weights = group < p.n_weights ? group : group % p.n_weights;
     tile.feature = (block * 8 + in - at * wide) * (PAIR ? 2 : 1) * kFeat;
     return tile;
 }
@@ -434,6 +435,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 n = (rows + width - 1) / width;
                 ctl->begin[g] = begin;
                 ctl->rows[g] = rows;
+                constexpr int kStep = PAIR ? 32 : 16;
+                if (n > 0) ctl->widths[g] = (int16_t)(((rows + n - 1) / n + kStep - 1) & ~(kStep - 1));
             }
             int sum = n;
             for (int d = 1; d < 32; d <<= 1) {
