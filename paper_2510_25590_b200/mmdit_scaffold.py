@@ -14,6 +14,13 @@ It offers the two callbacks the sampler loop (``loop.RegionELoop``) asks of a ve
                                       attention equation as printed) through every block, their queries
                                       attending over their own fresh K, V and the kept K, V of all other rows
 
+``products`` names what multiplies the rows with the weight set of their stream (text, or image and
+reference): "torch", two library products and a concatenation; "grouped", one ``grouped_matmul`` with both weight
+sets, the rows' ranges on the device and the activation in its epilogue; "mxfp4", the same on 4-bit operands
+(weights quantised once, rows in front of each product; the modulation's single rows stay in bf16).  ``cache``
+names how the blocks' kept K and V are stored between a full step and the region steps behind it: "bf16", or
+"mxfp4" (4 bits, widened in front of each attention).
+
 Outside a planted mask the velocity is replaced by the straight line to the reference latent, so that
 the Adaptive Region Partition has a region to find in a stack that was never trained.  One request
 (batch 1); the block definition is stated in the oracle's counterpart of this file.
@@ -25,8 +32,11 @@ from . import binding
 
 class MMDiTScaffold:
     def __init__(self, weights, n_text, n_img, n_ref, heads, head_dim, blocks, cos, sin, ref, planted,
-                 membership=binding.ROWS_PAPER):
+                 membership=binding.ROWS_PAPER, products="torch", cache="bf16"):
         import torch
+        if products not in ("torch", "grouped", "mxfp4") or cache not in ("bf16", "mxfp4"):
+            raise binding.RegionEError(f"no products {products!r} or cache {cache!r}")
+        self.products, self.cache = products, cache
         self.w = weights                                   # name -> bf16 CUDA tensor
         self.n_text, self.n_img, self.n_ref = n_text, n_img, n_ref
         self.n_full = n_text + n_img + n_ref
@@ -39,8 +49,12 @@ class MMDiTScaffold:
         buf = lambda rows: torch.empty((1, rows, H, D), dtype=bf, device=dev)
         self.k_full = [buf(n) for _ in range(blocks)]       # K, V of every row at the last storing step
         self.v_full = [buf(n) for _ in range(blocks)]
-        self.k_cache = [buf(n) for _ in range(blocks)]      # the rows a region step does not recompute
-        self.v_cache = [buf(n) for _ in range(blocks)]
+        # the rows a region step does not recompute: of every block, or codes of every block and one block's widened
+        self.k_cache = [buf(n) for _ in range(blocks if cache == "bf16" else 1)]
+        self.v_cache = [buf(n) for _ in range(blocks if cache == "bf16" else 1)]
+        if cache == "mxfp4":
+            bits = lambda d: torch.empty((1, n, H, D // d), dtype=torch.uint8, device=dev)
+            self.codes = [(bits(2), bits(2), bits(32), bits(32)) for _ in range(blocks)]
         self.scratch = [buf(n) for _ in range(5)]
         self.all_rows = torch.arange(n, dtype=i32, device=dev).view(1, n)
         self.n_all = torch.tensor([n], dtype=i32, device=dev)
@@ -54,6 +68,8 @@ class MMDiTScaffold:
         self._stale = True                                   # row lists / compacted caches need rebuilding
         self._nq = 0
         self.library_launches = 0
+        if products != "torch":
+            self._lay_out_weights()
 
     def bind(self, loop):
         """The loop whose partition lists (keep_idx) the region steps read."""
@@ -65,9 +81,62 @@ class MMDiTScaffold:
         import torch
         return torch.nn.functional.layer_norm(h.float(), (self.hidden,), eps=1e-6)
 
-    def _mm(self, a, name, n_text_rows):
+    # ---- products of both streams in one call ------------------------------------------------
+    def _lay_out_weights(self):
+        """Both streams' weights of a product as [2, N, K] (codes and scales with 4-bit products), once."""
+        import torch
+        hd, dev, i32 = self.hidden, self.ref.device, torch.int32
+        self.sets = {}
+        for l in range(self.L):
+            for name in (f"q{l}", f"k{l}", f"v{l}", f"o{l}", f"fc1_{l}", f"fc2_{l}", f"mod{l}"):
+                if name[0] in "qkv":
+                    j = "qkv".index(name[0])
+                    both = [self.w[f"qkv{l}_{s}"][:, j * hd:(j + 1) * hd] for s in (0, 1)]
+                else:
+                    both = [self.w[f"{name}_{s}"] for s in (0, 1)]
+                w = torch.stack([b.T.contiguous() for b in both])
+                if self.products == "mxfp4" and not name.startswith("mod"):
+                    codes = torch.empty((2, w.shape[1], w.shape[2] // 2), dtype=torch.uint8, device=dev)
+                    scales = torch.empty((2, w.shape[1], w.shape[2] // 32), dtype=torch.uint8, device=dev)
+                    binding.mxfp4_quantize(w, codes, scales, dev_status=self.dev_status)
+                    w = (codes, scales)
+                self.sets[name] = w
+        ints = lambda *v: torch.tensor(v, dtype=i32, device=dev)
+        self.one_each = ints(0, 1), ints(1, 2)               # the modulation's rows: one per stream
+        self.full_ranges = ints(0, self.n_text), ints(self.n_text, self.n_full)
+        self.region_begin, self.region_end = ints(0, 0), ints(0, 0)
+
+    def _operand(self, a):
+        """Rows as a product of ``products`` takes them."""
+        import torch
+        if self.products != "mxfp4":
+            return a
+        rows, K = a.shape
+        codes = torch.empty((1, rows, K // 2), dtype=torch.uint8, device=a.device)
+        scales = torch.empty((1, rows, K // 32), dtype=torch.uint8, device=a.device)
+        binding.mxfp4_quantize(a[None], codes, scales, dev_status=self.dev_status)
+        self.library_launches += 1
+        return codes[0], scales[0]
+
+    def _product(self, operand, name, ranges, out, activation=binding.ACT_NONE):
+        """out[r] = act(rows times the weight set of their range's stream)."""
+        w = self.sets[name]
+        if isinstance(w, tuple):
+            binding.mxfp4_grouped_matmul(*operand, *w, *ranges, out, activation=activation, dev_status=self.dev_status)
+        else:
+            binding.grouped_matmul(operand, w, *ranges, out, activation=activation, dev_status=self.dev_status)
+        self.library_launches += 1
+        return out
+
+    def _mm(self, a, name, n_text_rows, activation=binding.ACT_NONE):
         """Rows [text | others] times the weight set of their stream."""
         import torch
+        if self.products != "torch":
+            w = self.sets[name]
+            out = torch.empty((a.shape[0], (w[0] if isinstance(w, tuple) else w).shape[1]), dtype=torch.bfloat16, device=a.device)
+            return self._product(self._operand(a), name, self.ranges, out, activation)
+        if activation == binding.ACT_GELU_TANH:
+            return torch.nn.functional.gelu(self._mm(a, name, n_text_rows), approximate="tanh")
         w0, w1 = self.w[f"{name}_0"], self.w[f"{name}_1"]
         if n_text_rows == 0:
             return a @ w1
@@ -76,7 +145,11 @@ class MMDiTScaffold:
     def _mods(self, t, l, n_text_rows, rows):
         import torch
         c = torch.tanh(t * self.w["t_a"].float() + self.w["t_b"].float()).to(torch.bfloat16)[None]
-        m = [(c @ self.w[f"mod{l}_{s}"]).float() for s in (0, 1)]               # [1, 6 * hidden] per stream
+        if self.products != "torch":
+            both = torch.empty((2, 6 * self.hidden), dtype=torch.bfloat16, device=c.device)
+            m = self._product(c.expand(2, -1).contiguous(), f"mod{l}", self.one_each, both).float().split(1)
+        else:
+            m = [(c @ self.w[f"mod{l}_{s}"]).float() for s in (0, 1)]           # [1, 6 * hidden] per stream
         full = torch.cat([m[0].expand(n_text_rows, -1), m[1].expand(rows - n_text_rows, -1)])
         return full.chunk(6, dim=-1)
 
@@ -89,8 +162,12 @@ class MMDiTScaffold:
             sh1, sc1, g1, sh2, sc2, g2 = self._mods(t, l, n_text_rows, rows)
             a = (self._ln(h) * (1.0 + sc1) + sh1).to(bf)
             wq = lambda s: self.w[f"qkv{l}_{s}"]
+            operand = None if self.products == "torch" else self._operand(a)
             for j, dst in enumerate((q_s, k_s, v_s)):            # three projections, each into its own buffer
                 out = dst.view(-1, hd)[:rows]
+                if operand is not None:
+                    self._product(operand, f"{'qkv'[j]}{l}", self.ranges, out)
+                    continue
                 if n_text_rows:
                     torch.matmul(a[:n_text_rows], wq(0)[:, j * hd:(j + 1) * hd], out=out[:n_text_rows])
                 torch.matmul(a[n_text_rows:], wq(1)[:, j * hd:(j + 1) * hd], out=out[n_text_rows:])
@@ -103,7 +180,7 @@ class MMDiTScaffold:
             o = o_d.view(-1, hd)[:rows]
             h = (h.float() + g1 * self._mm(o, f"o{l}", n_text_rows).float()).to(bf)
             m = (self._ln(h) * (1.0 + sc2) + sh2).to(bf)
-            u = torch.nn.functional.gelu(self._mm(m, f"fc1_{l}", n_text_rows), approximate="tanh")
+            u = self._mm(m, f"fc1_{l}", n_text_rows, binding.ACT_GELU_TANH)
             h = (h.float() + g2 * self._mm(u, f"fc2_{l}", n_text_rows).float()).to(bf)
         return h
 
@@ -134,6 +211,8 @@ class MMDiTScaffold:
                                      workspace=self.workspace, dev_status=self.dev_status)
             self.library_launches += 2
 
+        if self.products != "torch":
+            self.ranges = self.full_ranges
         # (the scratch buffers span the whole sequence here, so no slicing copies happen)
         h = self._blocks(h, float(t), self.all_rows, self.n_all, self.n_text, attend, keep_kv=bool(store))
         if store:
@@ -146,8 +225,12 @@ class MMDiTScaffold:
         binding.region_rows(edit_idx, lp.keep_idx, n_edit, self.n_text, self.n_ref, self.membership,
                             self.query_rows, self.n_query, self.cache_rows, self.n_cache, dev_status=self.dev_status)
         for l in range(self.L):
-            binding.rikv_store(self.k_full[l], self.v_full[l], self.cache_rows, self.n_cache, self.k_cache[l],
-                               self.v_cache[l], dev_status=self.dev_status)
+            if self.cache == "mxfp4":
+                binding.rikv_store_mxfp4(self.k_full[l], self.v_full[l], self.cache_rows, self.n_cache, *self.codes[l],
+                                         dev_status=self.dev_status)
+            else:
+                binding.rikv_store(self.k_full[l], self.v_full[l], self.cache_rows, self.n_cache, self.k_cache[l],
+                                   self.v_cache[l], dev_status=self.dev_status)
         self.library_launches += 1 + self.L
         self._nq = int(self.n_query.item())                  # one host read per run of region steps: the GEMM sizes
         self._stale = False
@@ -166,9 +249,19 @@ class MMDiTScaffold:
         if with_text:
             h = torch.cat([w["text_emb"], h])
         positions = self.query_rows[:, :nq].contiguous()
+        if self.products != "torch":                         # text rows [0, nt), the others [nt, n_query)
+            self.region_begin[1:].fill_(nt)
+            self.region_end[:1].fill_(nt)
+            self.region_end[1:].copy_(self.n_query)
+            self.ranges = self.region_begin, self.region_end
 
         def attend(l, q, k, v, o):
-            binding.region_attention(q, k, v, self.k_cache[l], self.v_cache[l], self.n_query, self.n_query,
+            at = l
+            if self.cache == "mxfp4":
+                at = 0
+                binding.rikv_load_mxfp4(*self.codes[l], self.n_cache, self.k_cache[0], self.v_cache[0], dev_status=self.dev_status)
+                self.library_launches += 1
+            binding.region_attention(q, k, v, self.k_cache[at], self.v_cache[at], self.n_query, self.n_query,
                                      self.n_cache, o, workspace=self.workspace, dev_status=self.dev_status)
             self.library_launches += 2
 
