@@ -218,7 +218,7 @@ __device__ __forceinline__ uint64_t gelu_tanh(uint64_t x) {
     const uint64_t d = add2(pair_of(fminf(fast_exp2(e), 4.611686e18f), fminf(fast_exp2(f), 4.611686e18f)), pair_of(1.0f, 1.0f));
     parts_of(d, a, b);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a * b));
-    return mul2(mul2(x, pair_of(b, a)), pair_of(r, r));
+    return mul2(x, mul2(pair_of(b, a), pair_of(r, r)));        // (x b could overflow)
 }
 
 // A group's rows within the buffer; false: the range as given is not within it.
