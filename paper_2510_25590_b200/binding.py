@@ -420,17 +420,17 @@ def grouped_matmul(x, w, row_begin, row_end, out, bias=None, activation=ACT_NONE
     ranges on the device; rows of no group are left as they are."""
     torch = _torch()
     bf, i32 = torch.bfloat16, torch.int32
-    rows, K = x.shape
-    sets, N, _ = w.shape
-    _want(w, (sets, N, K), "w")
-    _want(row_end, row_begin.shape, "row_end")
-    if bias is not None:
+    rows, K = shape = x.shape
+    sets, N, k = w.shape
+    if k != K or row_end.shape != row_begin.shape or bias is not None and bias.shape != (sets, N):
+        _want(w, (sets, N, K), "w")
+        _want(row_end, row_begin.shape, "row_end")
         _want(bias, (sets, N), "bias")
-    xp, xs = _rows(x, (rows, K), bf, "x")
+    xp, xs = _rows(x, shape, bf, "x")
     op, os_ = _rows(out, (rows, N), bf, "out")
     _check(load().regione_grouped_matmul(
         xp, xs, _ptr(w, bf, "w"), _ptr(bias, bf, "bias"), _ptr(row_begin, i32, "row_begin"), _ptr(row_end, i32, "row_end"), rows,
-        row_begin.numel(), sets, K, N, int(activation), op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)),
+        row_begin.numel(), sets, K, N, activation, op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)),
         "regione_grouped_matmul")
 
 
@@ -440,19 +440,21 @@ def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bi
     [rows, K / 32] and [sets, N, K / 32]."""
     torch = _torch()
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
-    rows, K = x_q.shape[0], 2 * x_q.shape[1]
-    sets, N, _ = w_q.shape
-    _want(x_scale, (rows, K // 32), "x_scale")
-    _want(w_q, (sets, N, K // 2), "w_q")
-    _want(w_scale, (sets, N, K // 32), "w_scale")
-    _want(row_end, row_begin.shape, "row_end")
-    if bias is not None:
+    rows, half = x_q.shape
+    sets, N, k = w_q.shape
+    K = 2 * half
+    if (k != half or x_scale.shape != (rows, K // 32) or w_scale.shape != (sets, N, K // 32) or
+            row_end.shape != row_begin.shape or bias is not None and bias.shape != (sets, N)):
+        _want(x_scale, (rows, K // 32), "x_scale")
+        _want(w_q, (sets, N, K // 2), "w_q")
+        _want(w_scale, (sets, N, K // 32), "w_scale")
+        _want(row_end, row_begin.shape, "row_end")
         _want(bias, (sets, N), "bias")
     op, os_ = _rows(out, (rows, N), bf, "out")
     _check(load().regione_mxfp4_grouped_matmul(
         _ptr(x_q, u8, "x_q"), _ptr(x_scale, u8, "x_scale"), _ptr(w_q, u8, "w_q"), _ptr(w_scale, u8, "w_scale"),
         _ptr(bias, bf, "bias"), _ptr(row_begin, i32, "row_begin"), _ptr(row_end, i32, "row_end"), rows, row_begin.numel(), sets, K, N,
-        int(activation), op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_grouped_matmul")
+        activation, op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_grouped_matmul")
 
 
 def fresh_qkv(q_src, k_src, v_src, idx, n, q_weight, k_weight, eps, cos_table, sin_table, rope_layout,

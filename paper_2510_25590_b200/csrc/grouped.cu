@@ -791,7 +791,7 @@ template <bool FP4, bool VEC> static const int* grouped_pairs(int dev) {
 }
 
 template <bool FP4, bool PAIR, bool VEC>
-static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, long long clusters, cudaStream_t st) {
+static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, int clusters, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     const int cluster = (PAIR ? 2 : 1) * p.slices;
@@ -806,22 +806,24 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
     const int* held = dev < 0 ? nullptr : grouped_pairs<FP4, VEC>(dev);
     if (!held) return REGIONE_CUDA_ERROR;
     p.chunks = (p.K + kElems - 1) / kElems;
-    const long long groups = std::min(p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
-    const long long f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
+    const int groups = std::min(p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
+    const int f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
     // What the launch will take, in ns, if every row of the buffer is live and the groups are alike: what a launch takes before and behind
     // its tiles, and rounds of tiles, each the chunks of a slice times what a chunk takes (no less than 200 by latency; 105 bytes
     // a ns to an SM; the tensor core), and the way of the slices' sums to each other.
-    long long best = 0x7fffffffffffffffLL, clusters = 0;
+    long long best = 0x7fffffffffffffffLL;
+    int clusters = 0;
     bool pair = true;
     p.slices = 1;
     p.width = 0;
     for (int i = 0; i < 3; ++i) {
         const int slices = 1 << i;
-        if (held[i] < 1 || (i > 0 && 8 * slices > p.chunks)) continue;
+        if (held[i] < 1 || (i > 0 && 8 * slices > p.chunks)) break;
+        const int mine = (p.chunks + slices - 1) / slices;
         for (int width = 32; width <= (FP4 ? 224 : 256); width += 32) {
-            const long long tiles = f_pairs * groups * ((each + width - 1) / width), rounds = (tiles + held[i] - 1) / held[i];
-            const long long mine = (p.chunks + slices - 1) / slices, chunk = std::max(200, std::max(width * 14 / 13, 156 + width * 8 / 13));
-            const long long cost = rounds * (mine * chunk + (i > 0 ? 2500 + 18 * width : 0)) + 6300;
+            const int tiles = f_pairs * groups * ((each + width - 1) / width), rounds = (tiles + held[i] - 1) / held[i];
+            const int chunk = std::max(200, std::max(width * 14 / 13, 156 + width * 8 / 13));
+            const long long cost = (long long)rounds * ((long long)mine * chunk + (i > 0 ? 2500 + 18 * width : 0)) + 6300;
             if (cost >= best) continue;
             best = cost;
             p.slices = slices;
@@ -829,17 +831,19 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
         }
     }
     for (int width = 16; width <= 128; width *= 2) {
-        const long long tiles = f_tiles * (p.rows_cap / width + groups);        // at most, however the rows are spread over the groups
+        const int tiles = f_tiles * (p.rows_cap / width + groups);              // at most, however the rows are spread over the groups
+        const int chunk = std::max(200, 156 + width * 16 / 13);
         for (int slices = 1; slices <= 8 && 2 * slices <= std::max(p.chunks, 2); slices *= 2) {
-            const long long rounds = (tiles * slices + sms - 1) / sms, mine = (p.chunks + slices - 1) / slices;
-            const long long chunk = std::max(200, 156 + width * 16 / 13);
-            const long long cost = rounds * (mine * chunk + (slices > 1 ? 2000 + 18 * width : 0)) + (rounds - 1) * 800 + 4300;
+            if (slices > 1 && tiles > sms) break;                               // (the SMs are taken)
+            const int rounds = (tiles * slices + sms - 1) / sms, mine = (p.chunks + slices - 1) / slices;
+            const long long cost = (long long)rounds * ((long long)mine * chunk + (slices > 1 ? 2000 + 18 * width : 15 * width)) +
+                                   (rounds - 1) * 800LL + 4300;
             if (cost >= best) continue;
             best = cost;
             pair = false;
             p.width = width;
             p.slices = slices;
-            clusters = std::min(tiles, 4LL * sms);
+            clusters = std::min(tiles, 4 * sms);
         }
     }
     if (pair && clusters == 0) return REGIONE_CUDA_ERROR;

@@ -133,3 +133,66 @@ def test_cache_store_and_load(H, D):
             assert np.array_equal(host_f64(cache)[b, :n[b]], _widened(c, s))
             assert np.all(host_f64(cache)[b, n[b]:] == -3.0) and np.all(codes[b, n[b]:].cpu().numpy() == 0x5a)
     assert int(st[0]) == 0
+
+
+def test_rows_on_16_bytes_only_and_captured():
+    """A base that is not on 32 bytes takes the narrower loads; a captured call follows the counts."""
+    import torch
+    x = _rand(np.random.default_rng(5), (1, 40, 160))
+    buf = torch.empty(8 + x.size, dtype=torch.bfloat16, device="cuda")
+    dx = buf[8:].view(1, 40, 160)
+    dx.copy_(dev_bf16(x))
+    assert dx.data_ptr() % 32 == 16
+    n = dev_i32([40])
+    codes = torch.full((1, 40, 80), 0x5a, dtype=torch.uint8, device="cuda")
+    scales = torch.full((1, 40, 5), 0x5a, dtype=torch.uint8, device="cuda")
+    want_c, want_s = orc.mxfp4_quantize(x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        binding.mxfp4_quantize(dx, codes, scales, n=n)
+        side.synchronize()
+        assert _same_codes(codes.cpu().numpy(), want_c) and np.array_equal(scales.cpu().numpy(), want_s)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            binding.mxfp4_quantize(dx, codes, scales, n=n)
+    codes.fill_(0x5a)
+    n.fill_(17)
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert _same_codes(codes[:, :17].cpu().numpy(), want_c[:, :17]) and bool((codes[:, 17:] == 0x5a).all())
+
+
+def test_offsets_beyond_32_bits():
+    import torch
+    rows, K = 2_200_000, 1024
+    x = torch.zeros((1, rows, K), dtype=torch.bfloat16, device="cuda")
+    tail = _rand(np.random.default_rng(6), (1, 9, K))
+    x[:, -9:] = dev_bf16(tail)
+    codes = torch.empty((1, rows, K // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((1, rows, K // 32), dtype=torch.uint8, device="cuda")
+    binding.mxfp4_quantize(x, codes, scales)
+    c, s = orc.mxfp4_quantize(tail)
+    assert _same_codes(codes[:, -9:].cpu().numpy(), c) and np.array_equal(scales[:, -9:].cpu().numpy(), s)
+    idx = torch.arange(rows - 9, rows, dtype=torch.int32, device="cuda")[None]
+    few = torch.empty((1, 9, K // 2), dtype=torch.uint8, device="cuda"), torch.empty((1, 9, K // 32), dtype=torch.uint8, device="cuda")
+    binding.mxfp4_quantize(x, *few, idx=idx)
+    assert torch.equal(few[0], codes[:, -9:]) and torch.equal(few[1], scales[:, -9:])
+    binding.mxfp4_dequantize(codes, scales, x)
+    assert np.array_equal(host_f64(x[:, -9:]), _widened(c, s))
+
+
+def test_refusals_and_nothing_to_do():
+    import torch
+    t = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")
+    u = lambda *s: torch.empty(s, dtype=torch.uint8, device="cuda")
+    for x, c, s, kw in ((t(1, 4, 48), u(1, 4, 24), u(1, 4, 1), {}), (t(1, 4, 64), u(1, 4, 32), u(1, 4, 3), {}), (t(1, 4, 64), u(1, 5, 32), u(1, 5, 2), {}),
+                        (t(1, 4, 64), u(1, 4, 32), u(1, 4, 2), dict(idx=dev_i32([[0, 1]]))), (t(1, 4, 128)[:, :, :64], u(1, 4, 32), u(1, 4, 2), {}),
+                        (t(1, 4, 64).half(), u(1, 4, 32), u(1, 4, 2), {}), (t(1, 4, 64), u(1, 4, 32), u(1, 4, 2), dict(n=dev_i32([1, 2])))):
+        with pytest.raises(binding.RegionEError):
+            binding.mxfp4_quantize(x, c, s, **kw)
+    before = binding.kernel_launches()
+    binding.mxfp4_quantize(t(1, 0, 64), u(1, 0, 32), u(1, 0, 2))
+    binding.mxfp4_dequantize(u(1, 0, 32), u(1, 0, 2), t(1, 0, 64))
+    assert binding.kernel_launches() == before
