@@ -206,19 +206,25 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     return r;
 }
 
-// gelu(x) = x / 2 (1 + tanh(u)) = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3), of two values; the second form keeps its
-// relative accuracy where tanh(u) is near -1.  The two share a reciprocal, 1 / a = b / (a b): three results of the special
+// gelu(x) = x / 2 (1 + tanh(u)) = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3), of N pairs of values; the second form keeps its
+// relative accuracy where tanh(u) is near -1.  A pair shares a reciprocal, 1 / a = b / (a b): three results of the special
 // function unit, which sets the pace, in place of four.  exp(-2 u) is held at 2^62 so that a b stays finite: what is lost, from
-// x = -7.3 on, is below |x| 2^-62.
-__device__ __forceinline__ uint64_t gelu_tanh(uint64_t x) {
+// x = -7.3 on, is below |x| 2^-62.  Step by step for all pairs, and the compiler held to it: left to interleave it keeps few in
+// flight (4 bits, 16896 x 2048 x 8192: 195 us pair by pair, 175 so).
+template <int N> __device__ __forceinline__ void gelu_tanh(uint64_t (&x)[N]) {
     constexpr float c = -2.0f * 1.4426950409f * 0.7978845608f;
-    const uint64_t t = mul2(x, fma2(mul2(x, x), pair_of(c * 0.044715f, c * 0.044715f), pair_of(c, c)));
-    float e, f, a, b, r;
-    parts_of(t, e, f);
-    const uint64_t d = add2(pair_of(fminf(fast_exp2(e), 4.611686e18f), fminf(fast_exp2(f), 4.611686e18f)), pair_of(1.0f, 1.0f));
-    parts_of(d, a, b);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a * b));
-    return mul2(x, mul2(pair_of(b, a), pair_of(r, r)));        // (x b could overflow)
+    float e[2 * N], r[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        parts_of(mul2(x[i], fma2(mul2(x[i], x[i]), pair_of(c * 0.044715f, c * 0.044715f), pair_of(c, c))), e[2 * i], e[2 * i + 1]);
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[i]));
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) e[i] = 1.0f + fminf(e[i], 4.611686e18f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("rcp.approx.ftz.f32 %0, %1;" : "=f"(r[i]) : "f"(e[2 * i] * e[2 * i + 1]));
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = mul2(x[i], mul2(pair_of(e[2 * i + 1], e[2 * i]), pair_of(r[i], r[i])));   // (x b could overflow)
 }
 
 // A group's rows within the buffer; false: the range as given is not within it.
@@ -603,9 +609,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         for (int i = 0; i < 8; ++i)
                             y[i] = add2(pair_of(__uint_as_float(ahead[2 * i]), __uint_as_float(ahead[2 * i + 1])), bias[(i >> 2) * 2 + (i & 1)]);
                         if (c + kEpiCols < tile.live) fetch(c + kEpiCols);
-                        if (p.activation == REGIONE_ACT_GELU_TANH)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) y[i] = gelu_tanh(y[i]);
+                        if (p.activation == REGIONE_ACT_GELU_TANH) gelu_tanh(y);
                         uint32_t z[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -677,9 +681,12 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         y[0] += bf16_lo(b.x); y[1] += bf16_hi(b.x); y[2] += bf16_lo(b.y); y[3] += bf16_hi(b.y);
                         y[4] += bf16_lo(b.z); y[5] += bf16_hi(b.z); y[6] += bf16_lo(b.w); y[7] += bf16_hi(b.w);
                     }
-                    if (p.activation == REGIONE_ACT_GELU_TANH)
+                    if (p.activation == REGIONE_ACT_GELU_TANH) {
+                        uint64_t z[4] = {pair_of(y[0], y[1]), pair_of(y[2], y[3]), pair_of(y[4], y[5]), pair_of(y[6], y[7])};
+                        gelu_tanh(z);
 #pragma unroll
-                        for (int e = 0; e < 8; e += 2) parts_of(gelu_tanh(pair_of(y[e], y[e + 1])), y[e], y[e + 1]);
+                        for (int i = 0; i < 4; ++i) parts_of(z[i], y[2 * i], y[2 * i + 1]);
+                    }
                     uint4 o;
                     o.x = pack_bf16x2(y[0], y[1]); o.y = pack_bf16x2(y[2], y[3]);
                     o.z = pack_bf16x2(y[4], y[5]); o.w = pack_bf16x2(y[6], y[7]);
