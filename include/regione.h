@@ -316,9 +316,9 @@ int regione_rikv_load_mxfp4(const uint8_t* k_q, const uint8_t* v_q, const uint8_
  * x dev bf16 [rows_cap, K], rows x_stride elements apart; w dev bf16 [n_weights, N, K]; bias dev bf16
  * [n_weights, N] or NULL; row_begin, row_end dev int32 [groups]; out dev bf16 [rows_cap, N], rows out_stride
  * elements apart.  Groups may be empty, rows may be in no group (theirs of out are left untouched), no row
- * may be in two; a range that is not within [0, rows_cap] is cut to it and REGIONE_DEV_BOUNDS recorded.
- * out may not overlap x or w.  K, N and the strides are multiples of 8, groups <= 512, x, w, bias and out
- * 16-byte aligned.  activation: REGIONE_ACT_NONE, or REGIONE_ACT_GELU_TANH,
+ * may be in two (which of its results stands, or none, is not said); a range that is not within [0, rows_cap] is cut to it and REGIONE_DEV_BOUNDS recorded.
+ * out may not overlap x or w.  K, N and the strides are multiples of 8, groups <= 512, K, N <= 2^20,
+ * rows_cap <= 2^24, n_weights <= 65536 (REGIONE_UNSUPPORTED beyond), x, w, bias and out 16-byte aligned.  activation: REGIONE_ACT_NONE, or REGIONE_ACT_GELU_TANH,
  * act(y) = y / 2 (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))).  One kernel launch; nothing is allocated.
  *
  * regione_mxfp4_grouped_matmul: the same with x and w in the 4-bit format (rows quantised along K): x_q

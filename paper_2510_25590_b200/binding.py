@@ -330,10 +330,17 @@ def _want(t, shape, name):
         raise RegionEError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
+def _here(t, name):
+    """The calls below launch on the current device: a tensor of another one is refused."""
+    if t.is_cuda and t.get_device() != _torch()._C._cuda_getDevice():
+        raise RegionEError(f"{name} is on {t.device}, which is not the current device")
+
+
 def mxfp4_quantize(x, codes, scales, idx=None, n=None, dev_status=None, stream=None):
     """Rows of bf16 ``x`` [B, rows, K] to 4-bit microscaled ``codes`` [B, cap, K / 2] and ``scales`` [B, cap, K / 32]: row j of
     request b is row idx[b, j] (without ``idx`` row j), j < n[b] (without ``n`` every one)."""
     torch = _torch()
+    _here(x, "x")
     u8, i32 = torch.uint8, torch.int32
     B, rows, K = x.shape
     cap = codes.shape[1]
@@ -351,6 +358,7 @@ def mxfp4_quantize(x, codes, scales, idx=None, n=None, dev_status=None, stream=N
 def mxfp4_dequantize(codes, scales, x, n=None, dev_status=None, stream=None):
     """Widens rows j < n[b] of ``mxfp4_quantize`` back to bf16 ``x`` [B, cap, K] (exactly the quantised values)."""
     torch = _torch()
+    _here(x, "x")
     u8, i32 = torch.uint8, torch.int32
     B, cap, K = x.shape
     _want(codes, (B, cap, K // 2), "codes")
@@ -365,6 +373,7 @@ def mxfp4_dequantize(codes, scales, x, n=None, dev_status=None, stream=None):
 def rikv_store_mxfp4(k_full, v_full, keep_rows, n_keep, k_q, v_q, k_scale, v_scale, dev_status=None, stream=None):
     """``rikv_store`` into a 4-bit microscaled cache: codes [B, cap, H, D / 2], a scale per 32 elements [B, cap, H, D / 32]."""
     torch = _torch()
+    _here(k_full, "k_full")
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
     B, n_full, H, D = k_full.shape
     cap = keep_rows.shape[1]
@@ -382,6 +391,7 @@ def rikv_store_mxfp4(k_full, v_full, keep_rows, n_keep, k_q, v_q, k_scale, v_sca
 def rikv_load_mxfp4(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_status=None, stream=None):
     """Widens a 4-bit cache back to bf16 (exactly the quantised values) for the attention."""
     torch = _torch()
+    _here(k_cache, "k_cache")
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
     B, cap, H, D = k_cache.shape
     _want(v_cache, k_cache.shape, "v_cache")
@@ -419,6 +429,7 @@ def grouped_matmul(x, w, row_begin, row_end, out, bias=None, activation=ACT_NONE
     i = g % w.shape[0].  ``x`` [rows, K], ``out`` [rows, N] (rows may lie apart), ``w`` [sets, N, K], ``bias`` [sets, N], the
     ranges on the device; rows of no group are left as they are."""
     torch = _torch()
+    _here(x, "x")
     bf, i32 = torch.bfloat16, torch.int32
     rows, K = shape = x.shape
     sets, N, k = w.shape
@@ -439,6 +450,7 @@ def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bi
     """``grouped_matmul`` of rows and weights in the 4-bit format: codes [rows, K / 2] and [sets, N, K / 2], scales
     [rows, K / 32] and [sets, N, K / 32]."""
     torch = _torch()
+    _here(x_q, "x_q")
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
     rows, half = x_q.shape
     sets, N, k = w_q.shape

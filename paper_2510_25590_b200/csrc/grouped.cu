@@ -431,6 +431,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 if (ctl->cost[i] < ctl->cost[best]) best = i;
             width = 32 * (best + 1);
         }
+        // (no more tiles than ranges without a common row have: ranges that overlap are cut there)
+        const int most = p.rows_cap / width + p.groups;
         int at = 0;
         for (int g0 = 0; g0 < p.groups; g0 += 32) {
             const int g = g0 + lane;
@@ -449,13 +451,15 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 const int up = __shfl_up_sync(0xffffffffu, sum, d);
                 if (lane >= d) sum += up;
             }
-            if (g < p.groups) ctl->first[g] = at + sum - n;
+            if (g < p.groups) ctl->first[g] = min(at + sum - n, most);
             at += __shfl_sync(0xffffffffu, sum, 31);
         }
         if (lane == 0) {
+            if (at > most && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+            at = min(at, most);
             ctl->first[p.groups] = at;
             ctl->width = width;
-            ctl->total = (int)min((long long)at * f_tiles, 0x7fffffffLL);
+            ctl->total = at * f_tiles;
         }
     }
     ptx::tc_fence_before_sync();
@@ -891,7 +895,7 @@ static int check_grouped(const void* x, const void* w, const void* bias, const v
     if (activation != REGIONE_ACT_NONE && activation != REGIONE_ACT_GELU_TANH) return REGIONE_INVALID_ARG;
     if (!aligned16(x) || !aligned16(w) || !aligned16(out) || (bias && !aligned16(bias))) return REGIONE_INVALID_ARG;
     if (out_stride < N) return REGIONE_INVALID_ARG;
-    if (N % 8 || out_stride % 8 || groups > kMaxGroups || n_weights > 65536 || K > (1 << 20) || N > (1 << 20) || rows_cap > (1 << 24))
+    if (N % 8 || out_stride % 8 || out_stride > (1LL << 32) || groups > kMaxGroups || n_weights > 65536 || K > (1 << 20) || N > (1 << 20) || rows_cap > (1 << 24))
         return REGIONE_UNSUPPORTED;
     // tiles are counted in 32 bits
     if (((long long)rows_cap / 16 + groups) * ((N + kFeat - 1) / kFeat) >= 0x10000000LL) return REGIONE_UNSUPPORTED;

@@ -261,3 +261,35 @@ def test_refusals_of_the_binding():
                            (u(4, 64), u(4, 3), u(1, 8, 64), u(1, 8, 4))):     # K = 64; scales of another shape
         with pytest.raises(binding.RegionEError):
             binding.mxfp4_grouped_matmul(xq, xs, wq, ws, *r, t(4, 8))
+
+
+@pytest.mark.parametrize("rows,N", [(64, 24), (900, 264)])
+def test_ranges_that_overlap_end_and_are_recorded(rows, N):
+    """Not allowed, and which result stands is not said; no more is run than there can be rows."""
+    import torch
+    x, w, bias, _ = _whole_case(False, [0], [rows], rows, 1, 64, N)
+    G = 512
+    _run(False, x, w, [0] * G, [rows] * G, bias, status=binding.DEV_BOUNDS)
+
+
+def test_first_call_of_a_process_may_be_captured():
+    """Setting the kernels up is no work on a stream."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2510_25590_b200 import binding as b
+t = lambda *s: torch.ones(s, dtype=torch.bfloat16, device="cuda")
+x, w, out = t(3, 64), t(1, 8, 64), torch.zeros((3, 8), dtype=torch.bfloat16, device="cuda")
+r = torch.tensor([0], dtype=torch.int32, device="cuda"), torch.tensor([3], dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    b.grouped_matmul(x, w, *r, out)
+g.replay()
+torch.cuda.synchronize()
+assert bool((out == 64).all()), out
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=root, timeout=120)
