@@ -330,9 +330,15 @@ def _want(t, shape, name):
         raise RegionEError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
+_current_device = None
+
+
 def _here(t, name):
     """The calls below launch on the current device: a tensor of another one is refused."""
-    if t.is_cuda and t.get_device() != _torch()._C._cuda_getDevice():
+    global _current_device
+    if _current_device is None:
+        _current_device = _torch()._C._cuda_getDevice
+    if t.get_device() != _current_device() and t.is_cuda:
         raise RegionEError(f"{name} is on {t.device}, which is not the current device")
 
 

@@ -9,6 +9,18 @@
 // The features of W are the M side of the tensor-core product and the rows of x its N side: D^T = W x^T.  M is fixed by the
 // hardware (128 lanes of tensor memory a CTA), N is any multiple of 16 or 32 up to 256 named in the instruction, so a group
 // of 5 rows costs a tile of 16 or 32 and not one of 128 or 256.
+//
+// Two kernels.  Pairs of CTAs (cta_group::2, 256 features, up to 256 rows, a persistent cluster per pair of SMs, two accumulators so
+// that sums leave while the next tile's products run) for what fills the GPU: 8192^3 in bf16 700 us = 1.57 PFLOP/s with
+// the tensor pipe 92 % busy (the clock is what the power limit leaves), in 4 bits 207 us = 5.3 PFLOP/s; a library product in bf16
+// takes 675.  Lone CTAs (128 features, up to 128 rows, two to an SM) for less, where the start of a launch is what counts: 1024^3
+// 7.9 us, in 4 bits 6.0; two rows against 2 x 6144 x 1024 weights 7.1 us (25 MB, 3.9 us at the copy rate), 5.0 in 4 bits.  Both can
+// split K over the CTAs of a cluster, which add their sums in the order of the slices (225 rows, K 7544, N 80: 29 us whole, 10
+// in eight slices).  The host chooses from the capacities, the width of a pair's tiles is chosen on the device from the rows.
+//
+// What bounds them: bf16 the tensor core; 4 bits, whose operands last a quarter as long, the way from L2 into the SMs (30 KB a
+// chunk in 400 ns of which the products are 272), and with K below 4096 the sums' way out; few rows the weights' way from
+// device memory (64 experts of 2048 x 1408 with 4096 rows: 69 us, 62 at the copy rate).
 #include "common.cuh"
 #include "sm100_ptx.cuh"
 
@@ -37,8 +49,8 @@ struct GroupedArgs {
     int chunks;                                       // of K
     int ring_bytes;                                   // for stages: 128 rows of W and a tile's of x each, and the scales of both
     int tmem_columns, scale_column;
-    int slices;                                       // of K, one per CTA of a cluster (the kernel without pairs)
-    int width;                                        // rows of a tile at most (the kernel without pairs)
+    int slices;                                       // of K, each a CTA or a pair of a cluster (an even number, or 1)
+    int width;                                        // rows of a tile at most (lone CTAs)
     const uint16_t* bias;                             // [n_weights, N] or NULL
     int activation;
     uint16_t* out;
