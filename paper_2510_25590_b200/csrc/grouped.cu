@@ -281,7 +281,7 @@ __device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const Group
 // one and the ring has at least four stages: no phase of a barrier can be mistaken for the one two further on.
 // VEC, rows on 16 bytes: a lane reads its row's 16 bytes, 32 rows in one load.  Else four lanes read a word each, 8 rows in one load: as
 // many lines of the L1 a row (2 x 4992 x 296 for four times 764 rows: 14.9 us, a lane with the four words of its row 20.8).
-// Rows behind the matrices are read as their last one, words behind a row as its last: what they scale is not stored.
+// Rows behind the tile are read as its last one, words behind a row as its last: what they scale is not stored.
 struct ScaleRole {
     GroupedControl* ctl;
     uint8_t* scales;
@@ -308,7 +308,7 @@ __device__ __forceinline__ bool bring_scales(const GroupedArgs& p, const ScaleRo
 #pragma unroll
             for (int i = 0; i < kGroups; ++i) {       // part i: 4 groups of W, then those of x
                 const int row = (i == 0 ? tile.feature + (PAIR ? r.rank & 1 : 0) * kFeat : tile.first) + member * 8 + in_group + (i == 2 ? 128 : 0);
-                const int last = (i == 0 ? p.N : p.rows_cap) - 1;
+                const int last = (i == 0 ? p.N : min(p.rows_cap, tile.first + tile.width)) - 1;
                 src[i] = (i == 0 ? p.w_scale + (size_t)tile.weights * p.N * k32 : p.x_scale) + (size_t)min(row, last) * k32;
                 room[i] = max(last - row, 0);
             }
@@ -412,7 +412,6 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     if (warp == kIssuer) take_tmem<PAIR>(ptx::smem_addr(&ctl->tmem), p.tmem_columns);
     if (warp == kProducer && lane == 0) ptx::prefetch_tensormap(&maps.w);
     grid_dependency_wait();
-    grid_launch_dependents();
 
     // ---- plan: from the groups' row counts, which only the device knows --------------------------------------------
     const int f_tiles = (p.N + (PAIR ? 2 : 1) * kFeat - 1) / ((PAIR ? 2 : 1) * kFeat);
@@ -477,6 +476,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     ptx::tc_fence_before_sync();
     if (cluster > 1) ptx::cluster_sync(); else __syncthreads();
     ptx::tc_fence_after_sync();
+    // (not before this CTA has its tensor memory: a CTA of the next kernel could take it and wait for this kernel's end)
+    grid_launch_dependents();
     const uint32_t tmem = ctl->tmem;
     const int worker = blockIdx.x / cluster, total = ctl->total;
     // The narrower the tiles, the more stages: what bounds the loads is how many bytes are on their way (about 2 us under load).
