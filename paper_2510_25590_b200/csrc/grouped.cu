@@ -679,16 +679,20 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     if (f >= p.N) continue;
                     const uint32_t at = smem + (q * kFeat + 8 * j) * 4;
                     float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    for (int i0 = 0; i0 < p.slices; i0 += 2) {                   // (two at a time, an even number)
-                        float4 lo[2], hi[2];
+                    // (several at a time: a load takes 1000 cycles and more; 4 bits: as many as leave the other roles their registers)
+                    constexpr int kBatch = FP4 ? 2 : PAIR ? 4 : 8;
+                    for (int i0 = 0; i0 < p.slices; i0 += kBatch) {
+                        float4 lo[kBatch], hi[kBatch];
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
+                        for (int i = 0; i < kBatch; ++i) {
+                            if (kBatch > 2 && i0 + i >= p.slices) break;
                             const uint32_t from = ptx::map_rank(at, PAIR ? 2 * (i0 + i) + half : i0 + i);
                             lo[i] = ptx::ld_cluster_f4(from);
                             hi[i] = ptx::ld_cluster_f4(from + 16);
                         }
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
+                        for (int i = 0; i < kBatch; ++i) {
+                            if (kBatch > 2 && i0 + i >= p.slices) break;
                             y[0] += lo[i].x; y[1] += lo[i].y; y[2] += lo[i].z; y[3] += lo[i].w;
                             y[4] += hi[i].x; y[5] += hi[i].y; y[6] += hi[i].z; y[7] += hi[i].w;
                         }
@@ -860,7 +864,8 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
         for (int slices = 1; slices <= 8 && 2 * slices <= std::max(p.chunks, 2); slices *= 2) {
             if (slices > 1 && tiles > sms) break;                               // (the SMs are taken)
             const int rounds = (tiles * slices + sms - 1) / sms, mine = (p.chunks + slices - 1) / slices;
-            const long long cost = (long long)rounds * ((long long)mine * chunk + (slices > 1 ? 2000 + 18 * width : 15 * width)) +
+            const int meet = slices > 1 ? 1500 + (slices == 8 ? 40 : 28) * width : 15 * width;
+            const long long cost = (long long)rounds * ((long long)mine * chunk + meet) +
                                    (rounds - 1) * 800LL + 4300;
             if (cost >= best) continue;
             best = cost;
