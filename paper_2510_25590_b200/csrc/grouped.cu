@@ -535,6 +535,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     const uint32_t d = tmem + (a ? kAcc1 : 0);
                     if (use > 0 && !grouped_wait(ptx::smem_addr(&ctl->acc_empty[a]), (use - 1) & 1, ctl, p.dev_status)) { ok = false; break; }
                     ptx::tc_fence_after_sync();
+                    // (4 bits: E2M1 operands, N, E8M0 scales, M)
                     const uint32_t idesc = FP4 ? (1u << 7) | (1u << 10) | ((uint32_t)(tile.width >> 3) << 17) | (1u << 23) |
                                                      ((PAIR ? 2u : 1u) << 27)
                                                : ptx::idesc_bf16_f32(PAIR ? 256 : 128, tile.width, false);
