@@ -416,21 +416,24 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     // ---- plan: from the groups' row counts, which only the device knows --------------------------------------------
     const int f_tiles = (p.N + (PAIR ? 2 : 1) * kFeat - 1) / ((PAIR ? 2 : 1) * kFeat);
     const int workers = gridDim.x / cluster;
+    int own_begin = 0, own_rows = 0;                  // of group `lane`: read once, 800 cycles
+    bool own_in = true;
+    if (warp < (PAIR ? kMaxWidth / 32 : 1) && lane < p.groups) own_in = rows_of(p, lane, own_begin, own_rows);
     if constexpr (PAIR) {
         // Widths of 32 .. 256 (224) rows: one warp adds up the tiles of one width.  A chunk of a tile takes the tensor core 2 cycles a row;
         // its 128 + width / 2 rows of 128 bytes arrive at about 57 bytes a cycle.  The width with the cheapest rounds of tiles is
         // taken, the larger of equals.  (4096 rows, K 4096, N 4096: rounds counted by width alone take 192, 123 us.)
         if (warp < kMaxWidth / 32) {
             const int width = 32 * (warp + 1);
-            int n = 0;
-            for (int g = lane; g < p.groups; g += 32) {
+            int n = (own_rows + width - 1) / width;
+            for (int g = lane + 32; g < p.groups; g += 32) {
                 int begin, rows;
                 rows_of(p, g, begin, rows);
                 n += (rows + width - 1) / width;
             }
-            n = __reduce_add_sync(0xffffffffu, n);
-            const long long rounds = ((long long)n * f_tiles + workers - 1) / workers;
-            if (lane == 0) ctl->cost[warp] = (int)min(rounds * max(16 * width, 9 * (256 + width)), 0x7fffffffLL);
+            n = min(__reduce_add_sync(0xffffffffu, n), p.rows_cap / width + p.groups);
+            const int rounds = (n * f_tiles + workers - 1) / workers;
+            if (lane == 0) ctl->cost[warp] = (int)min((long long)rounds * max(16 * width, 9 * (256 + width)), 0x7fffffffLL);
         }
         __syncthreads();
     }
@@ -449,8 +452,10 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             const int g = g0 + lane;
             int n = 0;
             if (g < p.groups) {
-                int begin, rows;
-                if (!rows_of(p, g, begin, rows) && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+                int begin = own_begin, rows = own_rows;
+                bool in = own_in;
+                if (g0 > 0) in = rows_of(p, g, begin, rows);
+                if (!in && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
                 n = (rows + width - 1) / width;
                 ctl->begin[g] = begin;
                 ctl->rows[g] = rows;
