@@ -151,11 +151,18 @@ __device__ __forceinline__ void load_x(uint32_t dst, const CUtensorMap* map, uin
                      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
 
-// Arrival on a barrier of this CTA or, through map_rank, of the pair's leader.  What it announces is read by the tensor core of this
-// SM (scales in its shared memory, behind a proxy fence; an accumulator, behind a tcgen05 fence), so that the scope is the CTA: at the
-// cluster's scope the arrival waits for every store of the warp that is on its way.
-__device__ __forceinline__ void arrive_at(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// Arrival on a barrier of this CTA or, in a pair, of its leader: at the cluster's scope where that is another CTA, since a thread of that
+// CTA acts on what is announced.  An ordinary release at that scope waits for all memory operations of the warp that are on their way
+// (16896 x 4096 x 8192 in 4 bits 347 us), which is more than what is announced (in this form 234).  SMEM: the warp's writes to its
+// own CTA's shared memory (scales, behind their proxy fence); the release is restricted to those.  Else an accumulator that was
+// read out: tcgen05 operations are ordered by the fences of their own on both sides, around an arrival that releases nothing.
+template <bool PAIR, bool SMEM> __device__ __forceinline__ void arrive_at(uint32_t bar, int rank) {
+    if (PAIR && (rank & 1)) {
+        if (SMEM) asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(ptx::map_rank(bar, rank & ~1)) : "memory");
+    } else {
+        ptx::mbar_arrive(bar);
+    }
 }
 
 // 16 rows of 32 features from shared memory (64-byte swizzle) to the output; what lies behind the last feature is not written.
@@ -179,9 +186,14 @@ __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t a, uin
 }  // namespace
 
 // ---- waits: bounded; a wait that runs out is recorded and makes the other roles of the CTA give up -----------------
+// In a pair arrivals come from the other CTA as well, so that its waits acquire at the cluster's scope.
+template <bool PAIR> __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    return PAIR ? ptx::mbar_try_wait_cluster(bar, parity) : ptx::mbar_try_wait(bar, parity);
+}
+template <bool PAIR>
 __device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status) {
     const long long t0 = clock64();
-    while (!ptx::mbar_try_wait(bar, parity)) {
+    while (!try_wait<PAIR>(bar, parity)) {
         if (*abort_flag) return false;
         if (clock64() - t0 > kGroupedWait) {
             *abort_flag = 1;
@@ -191,8 +203,8 @@ __device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity,
     }
     return true;
 }
-__device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, GroupedControl* ctl, int32_t* dev_status) {
-    return ptx::mbar_try_wait(bar, parity) || grouped_wait_slow(bar, parity, &ctl->abort_flag, dev_status);
+template <bool PAIR> __device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, GroupedControl* ctl, int32_t* dev_status) {
+    return try_wait<PAIR>(bar, parity) || grouped_wait_slow<PAIR>(bar, parity, &ctl->abort_flag, dev_status);
 }
 
 // Two fp32 operations in one instruction.
@@ -341,7 +353,7 @@ __device__ __forceinline__ bool bring_scales(const GroupedArgs& p, const ScaleRo
         int at = s;
         uint32_t turn = phase;
         for (int k = 0; k < n; ++k) {
-            if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&r.ctl->empty[at]), turn ^ 1, r.ctl, p.dev_status))) return false;
+            if (!__all_sync(0xffffffffu, grouped_wait<PAIR>(ptx::smem_addr(&r.ctl->empty[at]), turn ^ 1, r.ctl, p.dev_status))) return false;
             uint32_t* base = reinterpret_cast<uint32_t*>(r.scales + at * (kScaleA + kScaleB)) + member * 32;
             const bool odd = (first + k) & 1;
 #pragma unroll
@@ -364,7 +376,7 @@ __device__ __forceinline__ bool bring_scales(const GroupedArgs& p, const ScaleRo
             __syncwarp();
             if (lane == 0) {
                 const uint32_t bar = ptx::smem_addr(&r.ctl->full[at]);
-                arrive_at(PAIR ? ptx::map_rank(bar, r.rank & ~1) : bar);
+                arrive_at<PAIR, true>(bar, r.rank);
             }
             if (++at == r.stages) { at = 0; turn ^= 1; }
         }
@@ -514,7 +526,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     const uint32_t bytes = (kTileBytes + rows * kChunkBytes) * (PAIR ? 2 : 1);
                     const int feature = tile.feature + half * kFeat, row = tile.first + half * rows;
                     for (int c = c_begin; c < c_end; ++c) {
-                        if (!grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
+                        if (!grouped_wait<PAIR>(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
                         if (leader) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&ctl->full[s]), bytes);
                         const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * stage_bytes;
                         load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
@@ -538,7 +550,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
                     const int a = it % kAccs, use = it / kAccs;
                     const uint32_t d = tmem + (a ? kAcc1 : 0);
-                    if (use > 0 && !grouped_wait(ptx::smem_addr(&ctl->acc_empty[a]), (use - 1) & 1, ctl, p.dev_status)) { ok = false; break; }
+                    if (use > 0 && !grouped_wait<PAIR>(ptx::smem_addr(&ctl->acc_empty[a]), (use - 1) & 1, ctl, p.dev_status)) { ok = false; break; }
                     ptx::tc_fence_after_sync();
                     // (4 bits: E2M1 operands, N, E8M0 scales, M)
                     const uint32_t idesc = FP4 ? (1u << 7) | (1u << 10) | ((uint32_t)(tile.width >> 3) << 17) | (1u << 23) |
@@ -546,7 +558,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                                                : ptx::idesc_bf16_f32(PAIR ? 256 : 128, tile.width, false);
                     uint32_t accumulate = 0;
                     for (int c = c_begin; c < c_end; ++c) {
-                        if (!grouped_wait(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
+                        if (!grouped_wait<PAIR>(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
                         ptx::tc_fence_after_sync();
                         const uint32_t at = smem + s * stage_bytes;
                         const uint32_t a_lo = ptx::smem_desc_lo(at, 16), b_lo = ptx::smem_desc_lo(at + kTileBytes, 16);
@@ -603,7 +615,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         const float b = __uint_as_float((uint32_t)__ldg(p.bias + (size_t)tile.weights * p.N + f) << 16);
                         bias[i] = pair_of(b, b);
                     }
-                if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->acc_full[a]), use & 1, ctl, p.dev_status)))
+                if (!__all_sync(0xffffffffu, grouped_wait<PAIR>(ptx::smem_addr(&ctl->acc_full[a]), use & 1, ctl, p.dev_status)))
                     break;
                 ptx::tc_fence_after_sync();
                 const uint32_t acc = tmem + (a ? kAcc1 : 0) + ((uint32_t)(32 * sub) << 16);
@@ -670,7 +682,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 }
                 ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) arrive_at(bar_at(&ctl->acc_empty[a]));
+                if (lane == 0) arrive_at<PAIR, false>(ptx::smem_addr(&ctl->acc_empty[a]), rank);
             }
         }
         // ---- the slices of a tile meet --------------------------------------------------------------------------------------
