@@ -643,6 +643,14 @@ int regione_selftest_attention_plan(const int32_t* n_q, const int32_t* n_fresh, 
  */
 int regione_selftest_attention_form(int B, int Nq_cap, int Nf_cap, int Nc_cap, int H, int D, int out_cap, int refreshes);
 
+/*
+ * What a grouped product takes of the ranges it is given: the function that the kernel runs, run on the host.
+ * row_begin, row_end, begin, rows: host int32 [groups]; the rows of group g are [begin[g], begin[g] + rows[g]).
+ * Returns how many of the ranges are not within [0, rows_cap], -1 for invalid arguments.
+ */
+int regione_selftest_group_ranges(const int32_t* row_begin, const int32_t* row_end, int rows_cap, int groups,
+                                  int32_t* begin, int32_t* rows);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,7 @@
 // chunk in 400 ns of which the products are 272), and with K below 4096 the sums' way out; few rows the weights' way from
 // device memory (64 experts of 2048 x 1408 with 4096 rows: 69 us, 62 at the copy rate).
 #include "common.cuh"
+#include "grouped_plan.cuh"
 #include "sm100_ptx.cuh"
 
 #include <algorithm>
@@ -253,10 +254,7 @@ template <int N> __device__ __forceinline__ void gelu_tanh(uint64_t (&x)[N]) {
 
 // A group's rows within the buffer; false: the range as given is not within it.
 __device__ __forceinline__ bool rows_of(const GroupedArgs& p, int g, int& begin, int& rows) {
-    const int b = p.row_begin[g], e = p.row_end[g];
-    begin = min(max(b, 0), p.rows_cap);
-    rows = max(min(e, p.rows_cap) - begin, 0);
-    return b >= 0 && e <= p.rows_cap && b <= e;
+    return cut_range(p.row_begin[g], p.row_end[g], p.rows_cap, begin, rows);
 }
 
 // Rows [first, first + live) of a group against a feature tile; `width` = columns of the product.
@@ -970,4 +968,12 @@ extern "C" int regione_mxfp4_grouped_matmul(const uint8_t* x_q, const uint8_t* x
     p.x_scale = x_scale; p.w_scale = w_scale;
     return K % 512 ? grouped_run<true, false>(x_q, K / 2, w_q, p, (cudaStream_t)stream)
                    : grouped_run<true, true>(x_q, K / 2, w_q, p, (cudaStream_t)stream);
+}
+
+extern "C" int regione_selftest_group_ranges(const int32_t* row_begin, const int32_t* row_end, int rows_cap, int groups,
+                                             int32_t* begin, int32_t* rows) {
+    if (!row_begin || !row_end || !begin || !rows || rows_cap < 0 || groups < 0) return -1;
+    int outside = 0;
+    for (int g = 0; g < groups; ++g) outside += !cut_range(row_begin[g], row_end[g], rows_cap, begin[g], rows[g]);
+    return outside;
 }
