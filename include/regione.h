@@ -319,7 +319,8 @@ int regione_rikv_load_mxfp4(const uint8_t* k_q, const uint8_t* v_q, const uint8_
  * may be in two (which of its results stands, or none, is not said); a range that is not within [0, rows_cap] is cut to it and REGIONE_DEV_BOUNDS recorded.
  * out may not overlap x or w.  K, N and the strides are multiples of 8, groups <= 512, K, N <= 2^20,
  * rows_cap <= 2^24, n_weights <= 65536 (REGIONE_UNSUPPORTED beyond), x, w, bias and out 16-byte aligned.  activation: REGIONE_ACT_NONE, or REGIONE_ACT_GELU_TANH,
- * act(y) = y / 2 (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))).  One kernel launch; nothing is allocated.
+ * act(y) = y / 2 (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))), -0 for y below -10.1, NaN for -infinity (an infinity times 0).
+ * One kernel launch; nothing is allocated.
  *
  * regione_mxfp4_grouped_matmul: the same with x and w in the 4-bit format (rows quantised along K): x_q
  * [rows_cap, K / 2], x_scale [rows_cap, K / 32], w_q [n_weights, N, K / 2], w_scale [n_weights, N, K / 32],

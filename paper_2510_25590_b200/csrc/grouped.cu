@@ -231,21 +231,51 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     return r;
 }
 
+__device__ __forceinline__ float min_or_nan(float x, float y, float z) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // gelu(x) = x / 2 (1 + tanh(u)) = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3), of N pairs of values; the second form keeps its
 // relative accuracy where tanh(u) is near -1.  A pair shares a reciprocal, 1 / a = b / (a b): three results of the special
-// function unit, which sets the pace, in place of four.  exp(-2 u) is held at 2^62 so that a b stays finite: what is lost, from
-// x = -7.3 on, is below |x| 2^-62.  Step by step for all pairs, and the compiler held to it: left to interleave it keeps few in
+// function unit, which sets the pace, in place of four.  a b is below 2^118 where both are above -7.4; where one of the lane's values is
+// not, or is a NaN, each takes a reciprocal of its own.  That is 0 from -10.1 on, where gelu is below 2^-122: -0 there, and NaN for
+// -infinity, as the formula gives.  Step by step for all pairs, and the compiler held to it: left to interleave it keeps few in
 // flight (4 bits, 16896 x 2048 x 8192: 195 us pair by pair, 175 so).
 template <int N> __device__ __forceinline__ void gelu_tanh(uint64_t (&x)[N]) {
     constexpr float c = -2.0f * 1.4426950409f * 0.7978845608f;
-    float e[2 * N], r[N];
+    auto exponent = [&](int i, float& a, float& b) {  // of exp(-2 u), to base 2
+        parts_of(mul2(x[i], fma2(mul2(x[i], x[i]), pair_of(c * 0.044715f, c * 0.044715f), pair_of(c, c))), a, b);
+    };
+    float e[2 * N], r[N], least[2 * N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        parts_of(mul2(x[i], fma2(mul2(x[i], x[i]), pair_of(c * 0.044715f, c * 0.044715f), pair_of(c, c))), e[2 * i], e[2 * i + 1]);
+    for (int i = 0; i < N; ++i) parts_of(x[i], least[2 * i], least[2 * i + 1]);
+#pragma unroll
+    for (int n = 2 * N; n > 1; n = (n + 2) / 3)
+#pragma unroll
+        for (int i = 0; i < (n + 2) / 3; ++i)
+            if (3 * i + 1 < n) least[i] = min_or_nan(least[3 * i], least[3 * i + 1], least[min(3 * i + 2, n - 1)]);
+            else least[i] = least[3 * i];
+    if (!(least[0] > -7.4f)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            exponent(i, e[0], e[1]);
+            x[i] = mul2(x[i], pair_of(reciprocal(1.0f + fast_exp2(e[0])), reciprocal(1.0f + fast_exp2(e[1]))));
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) exponent(i, e[2 * i], e[2 * i + 1]);
 #pragma unroll
     for (int i = 0; i < 2 * N; ++i) asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[i]));
 #pragma unroll
-    for (int i = 0; i < 2 * N; ++i) e[i] = 1.0f + fminf(e[i], 4.611686e18f);
+    for (int i = 0; i < N; ++i) parts_of(add2(pair_of(e[2 * i], e[2 * i + 1]), pair_of(1.0f, 1.0f)), e[2 * i], e[2 * i + 1]);
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("rcp.approx.ftz.f32 %0, %1;" : "=f"(r[i]) : "f"(e[2 * i] * e[2 * i + 1]));
 #pragma unroll
@@ -652,10 +682,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         }
                         // row of the tile t at 64 t, its 16-byte pieces (8 features) turned by t / 2 so that eight rows meet eight banks
                         const int row = (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1, turn = (row >> 1) & 3;
-                        if (PAIR) {                                                  // (the store of the step before)
-                            if (lane == 0) ptx::bulk_wait_read<0>();
-                            __syncwarp();
-                        }
+                        if (PAIR && lane == 0) ptx::bulk_wait_read<0>();             // (the store of the step before)
+                        __syncwarp();
                         stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), z[0], z[1], z[2], z[3]);
                         stmatrix_x4_trans(stage + row * 64 + (((piece + 2) ^ turn) << 4), z[4], z[5], z[6], z[7]);
                         if (PAIR && c + 16 <= tile.live) {
