@@ -334,20 +334,32 @@ def _want(t, shape, name):
 _current_device = None
 
 
-def _here(t, name):
-    """The calls below launch on the current device: a tensor of another one is refused."""
+def _here():
+    """The current device, where the calls below launch."""
     global _current_device
     if _current_device is None:
         _current_device = _torch()._C._cuda_getDevice
-    if t.get_device() != _current_device() and t.is_cuda:
-        raise RegionEError(f"{name} is on {t.device}, which is not the current device")
+    return _current_device()
+
+
+def _on(device, t, dtype, name):
+    """``_ptr`` of a tensor that lies on that device: one of another device is refused."""
+    if t is None:
+        return None
+    try:
+        if t.get_device() == device and t.dtype == dtype and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _ptr(t, dtype, name)
+    raise RegionEError(f"{name} is on {t.device}, which is not the current device")
 
 
 def mxfp4_quantize(x, codes, scales, idx=None, n=None, dev_status=None, stream=None):
     """Rows of bf16 ``x`` [B, rows, K] to 4-bit microscaled ``codes`` [B, cap, K / 2] and ``scales`` [B, cap, K / 32]: row j of
     request b is row idx[b, j] (without ``idx`` row j), j < n[b] (without ``n`` every one)."""
     torch = _torch()
-    _here(x, "x")
+    at = _here()
     u8, i32 = torch.uint8, torch.int32
     B, rows, K = x.shape
     cap = codes.shape[1]
@@ -358,14 +370,15 @@ def mxfp4_quantize(x, codes, scales, idx=None, n=None, dev_status=None, stream=N
     if n is not None:
         _want(n, (B,), "n")
     _check(load().regione_mxfp4_quantize(
-        _ptr(x, torch.bfloat16, "x"), _ptr(idx, i32, "idx"), _ptr(n, i32, "n"), B, rows, cap, K, _ptr(codes, u8, "codes"),
-        _ptr(scales, u8, "scales"), _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_quantize")
+        _on(at, x, torch.bfloat16, "x"), _on(at, idx, i32, "idx"), _on(at, n, i32, "n"), B, rows, cap, K,
+        _on(at, codes, u8, "codes"), _on(at, scales, u8, "scales"), _on(at, dev_status, i32, "dev_status"),
+        _stream(stream)), "regione_mxfp4_quantize")
 
 
 def mxfp4_dequantize(codes, scales, x, n=None, dev_status=None, stream=None):
     """Widens rows j < n[b] of ``mxfp4_quantize`` back to bf16 ``x`` [B, cap, K] (exactly the quantised values)."""
     torch = _torch()
-    _here(x, "x")
+    at = _here()
     u8, i32 = torch.uint8, torch.int32
     B, cap, K = x.shape
     _want(codes, (B, cap, K // 2), "codes")
@@ -373,14 +386,14 @@ def mxfp4_dequantize(codes, scales, x, n=None, dev_status=None, stream=None):
     if n is not None:
         _want(n, (B,), "n")
     _check(load().regione_mxfp4_dequantize(
-        _ptr(codes, u8, "codes"), _ptr(scales, u8, "scales"), _ptr(n, i32, "n"), B, cap, K, _ptr(x, torch.bfloat16, "x"),
-        _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_dequantize")
+        _on(at, codes, u8, "codes"), _on(at, scales, u8, "scales"), _on(at, n, i32, "n"), B, cap, K,
+        _on(at, x, torch.bfloat16, "x"), _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_dequantize")
 
 
 def rikv_store_mxfp4(k_full, v_full, keep_rows, n_keep, k_q, v_q, k_scale, v_scale, dev_status=None, stream=None):
     """``rikv_store`` into a 4-bit microscaled cache: codes [B, cap, H, D / 2], a scale per 32 elements [B, cap, H, D / 32]."""
     torch = _torch()
-    _here(k_full, "k_full")
+    at = _here()
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
     B, n_full, H, D = k_full.shape
     cap = keep_rows.shape[1]
@@ -390,15 +403,16 @@ def rikv_store_mxfp4(k_full, v_full, keep_rows, n_keep, k_q, v_q, k_scale, v_sca
     for t, d, name in ((k_q, 2, "k_q"), (v_q, 2, "v_q"), (k_scale, 32, "k_scale"), (v_scale, 32, "v_scale")):
         _want(t, (B, cap, H, D // d), name)
     _check(load().regione_rikv_store_mxfp4(
-        _ptr(k_full, bf, "k_full"), _ptr(v_full, bf, "v_full"), _ptr(keep_rows, i32, "keep_rows"), _ptr(n_keep, i32, "n_keep"),
-        B, n_full, cap, H, D, _ptr(k_q, u8, "k_q"), _ptr(v_q, u8, "v_q"), _ptr(k_scale, u8, "k_scale"),
-        _ptr(v_scale, u8, "v_scale"), _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_rikv_store_mxfp4")
+        _on(at, k_full, bf, "k_full"), _on(at, v_full, bf, "v_full"), _on(at, keep_rows, i32, "keep_rows"),
+        _on(at, n_keep, i32, "n_keep"), B, n_full, cap, H, D, _on(at, k_q, u8, "k_q"), _on(at, v_q, u8, "v_q"),
+        _on(at, k_scale, u8, "k_scale"), _on(at, v_scale, u8, "v_scale"), _on(at, dev_status, i32, "dev_status"),
+        _stream(stream)), "regione_rikv_store_mxfp4")
 
 
 def rikv_load_mxfp4(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_status=None, stream=None):
     """Widens a 4-bit cache back to bf16 (exactly the quantised values) for the attention."""
     torch = _torch()
-    _here(k_cache, "k_cache")
+    at = _here()
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
     B, cap, H, D = k_cache.shape
     _want(v_cache, k_cache.shape, "v_cache")
@@ -406,19 +420,21 @@ def rikv_load_mxfp4(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_st
     for t, d, name in ((k_q, 2, "k_q"), (v_q, 2, "v_q"), (k_scale, 32, "k_scale"), (v_scale, 32, "v_scale")):
         _want(t, (B, cap, H, D // d), name)
     _check(load().regione_rikv_load_mxfp4(
-        _ptr(k_q, u8, "k_q"), _ptr(v_q, u8, "v_q"), _ptr(k_scale, u8, "k_scale"), _ptr(v_scale, u8, "v_scale"),
-        _ptr(n_keep, i32, "n_keep"), B, cap, H, D, _ptr(k_cache, bf, "k_cache"), _ptr(v_cache, bf, "v_cache"),
-        _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_rikv_load_mxfp4")
+        _on(at, k_q, u8, "k_q"), _on(at, v_q, u8, "v_q"), _on(at, k_scale, u8, "k_scale"), _on(at, v_scale, u8, "v_scale"),
+        _on(at, n_keep, i32, "n_keep"), B, cap, H, D, _on(at, k_cache, bf, "k_cache"), _on(at, v_cache, bf, "v_cache"),
+        _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_rikv_load_mxfp4")
 
 
-def _rows(t, shape, dtype, name):
-    """Device address and row distance of a CUDA matrix of that shape whose rows may lie apart."""
+def _rows(device, t, shape, dtype, name):
+    """Device address and row distance of a matrix of that shape on that device whose rows may lie apart."""
     rows, cols = shape
     try:
-        if t.is_cuda and t.dtype == dtype and t.shape == shape:
+        if t.get_device() == device and t.dtype == dtype and t.shape == shape:
             step, unit = t.stride()
             if unit == 1 and step >= cols:
                 return t.data_ptr(), step if rows > 1 else cols
+        if t.is_cuda and t.get_device() != device:
+            raise RegionEError(f"{name} is on {t.device}, which is not the current device")
     except AttributeError:
         pass
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
@@ -436,7 +452,7 @@ def grouped_matmul(x, w, row_begin, row_end, out, bias=None, activation=ACT_NONE
     i = g % w.shape[0].  ``x`` [rows, K], ``out`` [rows, N] (rows may lie apart), ``w`` [sets, N, K], ``bias`` [sets, N], the
     ranges on the device; rows of no group are left as they are."""
     torch = _torch()
-    _here(x, "x")
+    at = _here()
     bf, i32 = torch.bfloat16, torch.int32
     rows, K = shape = x.shape
     sets, N, k = w.shape
@@ -444,12 +460,12 @@ def grouped_matmul(x, w, row_begin, row_end, out, bias=None, activation=ACT_NONE
         _want(w, (sets, N, K), "w")
         _want(row_end, row_begin.shape, "row_end")
         _want(bias, (sets, N), "bias")
-    xp, xs = _rows(x, shape, bf, "x")
-    op, os_ = _rows(out, (rows, N), bf, "out")
+    xp, xs = _rows(at, x, shape, bf, "x")
+    op, os_ = _rows(at, out, (rows, N), bf, "out")
     _check(load().regione_grouped_matmul(
-        xp, xs, _ptr(w, bf, "w"), _ptr(bias, bf, "bias"), _ptr(row_begin, i32, "row_begin"), _ptr(row_end, i32, "row_end"), rows,
-        row_begin.numel(), sets, K, N, activation, op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)),
-        "regione_grouped_matmul")
+        xp, xs, _on(at, w, bf, "w"), _on(at, bias, bf, "bias"), _on(at, row_begin, i32, "row_begin"),
+        _on(at, row_end, i32, "row_end"), rows, row_begin.numel(), sets, K, N, activation, op, os_,
+        _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_grouped_matmul")
 
 
 def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bias=None, activation=ACT_NONE, dev_status=None,
@@ -457,7 +473,7 @@ def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bi
     """``grouped_matmul`` of rows and weights in the 4-bit format: codes [rows, K / 2] and [sets, N, K / 2], scales
     [rows, K / 32] and [sets, N, K / 32]."""
     torch = _torch()
-    _here(x_q, "x_q")
+    at = _here()
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
     rows, half = x_q.shape
     sets, N, k = w_q.shape
@@ -469,11 +485,12 @@ def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bi
         _want(w_scale, (sets, N, K // 32), "w_scale")
         _want(row_end, row_begin.shape, "row_end")
         _want(bias, (sets, N), "bias")
-    op, os_ = _rows(out, (rows, N), bf, "out")
+    op, os_ = _rows(at, out, (rows, N), bf, "out")
     _check(load().regione_mxfp4_grouped_matmul(
-        _ptr(x_q, u8, "x_q"), _ptr(x_scale, u8, "x_scale"), _ptr(w_q, u8, "w_q"), _ptr(w_scale, u8, "w_scale"),
-        _ptr(bias, bf, "bias"), _ptr(row_begin, i32, "row_begin"), _ptr(row_end, i32, "row_end"), rows, row_begin.numel(), sets, K, N,
-        activation, op, os_, _ptr(dev_status, i32, "dev_status"), _stream(stream)), "regione_mxfp4_grouped_matmul")
+        _on(at, x_q, u8, "x_q"), _on(at, x_scale, u8, "x_scale"), _on(at, w_q, u8, "w_q"), _on(at, w_scale, u8, "w_scale"),
+        _on(at, bias, bf, "bias"), _on(at, row_begin, i32, "row_begin"), _on(at, row_end, i32, "row_end"), rows,
+        row_begin.numel(), sets, K, N, activation, op, os_, _on(at, dev_status, i32, "dev_status"),
+        _stream(stream)), "regione_mxfp4_grouped_matmul")
 
 
 def fresh_qkv(q_src, k_src, v_src, idx, n, q_weight, k_weight, eps, cos_table, sin_table, rope_layout,
