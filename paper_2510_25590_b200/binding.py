@@ -326,8 +326,19 @@ def rikv_load_e4m3(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_sta
         _stream(stream)), "regione_rikv_load_e4m3")
 
 
+def _ranks(**tensors):
+    """Raises for the first tensor that has not that many dimensions (None: any), name=(tensor, dimensions)."""
+    for name, (t, rank) in tensors.items():
+        shape = getattr(t, "shape", None)
+        if shape is None:
+            raise RegionEError(f"{name} must be a CUDA tensor")
+        if rank is not None and len(shape) != rank:
+            raise RegionEError(f"{name} must have {rank} dimensions, got shape {tuple(shape)}")
+
+
 def _want(t, shape, name):
-    if t.shape != shape:
+    if getattr(t, "shape", None) != shape:
+        _ranks(**{name: (t, None)})
         raise RegionEError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
@@ -361,8 +372,12 @@ def mxfp4_quantize(x, codes, scales, idx=None, n=None, dev_status=None, stream=N
     torch = _torch()
     at = _here()
     u8, i32 = torch.uint8, torch.int32
-    B, rows, K = x.shape
-    cap = codes.shape[1]
+    try:
+        B, rows, K = x.shape
+        cap = codes.shape[1]
+    except (AttributeError, ValueError, IndexError):
+        _ranks(x=(x, 3), codes=(codes, 3))
+        raise
     _want(codes, (B, cap, K // 2), "codes")
     _want(scales, (B, cap, K // 32), "scales")
     if idx is not None:
@@ -380,7 +395,11 @@ def mxfp4_dequantize(codes, scales, x, n=None, dev_status=None, stream=None):
     torch = _torch()
     at = _here()
     u8, i32 = torch.uint8, torch.int32
-    B, cap, K = x.shape
+    try:
+        B, cap, K = x.shape
+    except (AttributeError, ValueError, IndexError):
+        _ranks(x=(x, 3))
+        raise
     _want(codes, (B, cap, K // 2), "codes")
     _want(scales, (B, cap, K // 32), "scales")
     if n is not None:
@@ -395,8 +414,12 @@ def rikv_store_mxfp4(k_full, v_full, keep_rows, n_keep, k_q, v_q, k_scale, v_sca
     torch = _torch()
     at = _here()
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
-    B, n_full, H, D = k_full.shape
-    cap = keep_rows.shape[1]
+    try:
+        B, n_full, H, D = k_full.shape
+        cap = keep_rows.shape[1]
+    except (AttributeError, ValueError, IndexError):
+        _ranks(k_full=(k_full, 4), keep_rows=(keep_rows, 2))
+        raise
     _want(v_full, k_full.shape, "v_full")
     _want(keep_rows, (B, cap), "keep_rows")
     _want(n_keep, (B,), "n_keep")
@@ -414,7 +437,11 @@ def rikv_load_mxfp4(k_q, v_q, k_scale, v_scale, n_keep, k_cache, v_cache, dev_st
     torch = _torch()
     at = _here()
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
-    B, cap, H, D = k_cache.shape
+    try:
+        B, cap, H, D = k_cache.shape
+    except (AttributeError, ValueError, IndexError):
+        _ranks(k_cache=(k_cache, 4))
+        raise
     _want(v_cache, k_cache.shape, "v_cache")
     _want(n_keep, (B,), "n_keep")
     for t, d, name in ((k_q, 2, "k_q"), (v_q, 2, "v_q"), (k_scale, 32, "k_scale"), (v_scale, 32, "v_scale")):
@@ -454,12 +481,18 @@ def grouped_matmul(x, w, row_begin, row_end, out, bias=None, activation=ACT_NONE
     torch = _torch()
     at = _here()
     bf, i32 = torch.bfloat16, torch.int32
-    rows, K = shape = x.shape
-    sets, N, k = w.shape
-    if k != K or row_end.shape != row_begin.shape or bias is not None and bias.shape != (sets, N):
+    try:
+        rows, K = shape = x.shape
+        sets, N, k = w.shape
+        fits = k == K and row_end.shape == row_begin.shape and (bias is None or bias.shape == (sets, N))
+    except (AttributeError, ValueError, IndexError):
+        _ranks(x=(x, 2), w=(w, 3), row_begin=(row_begin, None), row_end=(row_end, None), bias=(bias, None))
+        raise
+    if not fits:
         _want(w, (sets, N, K), "w")
         _want(row_end, row_begin.shape, "row_end")
-        _want(bias, (sets, N), "bias")
+        if bias is not None:
+            _want(bias, (sets, N), "bias")
     xp, xs = _rows(at, x, shape, bf, "x")
     op, os_ = _rows(at, out, (rows, N), bf, "out")
     _check(load().regione_grouped_matmul(
@@ -475,16 +508,23 @@ def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bi
     torch = _torch()
     at = _here()
     bf, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
-    rows, half = x_q.shape
-    sets, N, k = w_q.shape
-    K = 2 * half
-    if (k != half or x_scale.shape != (rows, K // 32) or w_scale.shape != (sets, N, K // 32) or
-            row_end.shape != row_begin.shape or bias is not None and bias.shape != (sets, N)):
+    try:
+        rows, half = x_q.shape
+        sets, N, k = w_q.shape
+        K = 2 * half
+        fits = (k == half and x_scale.shape == (rows, K // 32) and w_scale.shape == (sets, N, K // 32) and
+                row_end.shape == row_begin.shape and (bias is None or bias.shape == (sets, N)))
+    except (AttributeError, ValueError, IndexError):
+        _ranks(x_q=(x_q, 2), x_scale=(x_scale, 2), w_q=(w_q, 3), w_scale=(w_scale, 3), row_begin=(row_begin, None), row_end=(row_end, None),
+               bias=(bias, None))
+        raise
+    if not fits:
         _want(x_scale, (rows, K // 32), "x_scale")
         _want(w_q, (sets, N, K // 2), "w_q")
         _want(w_scale, (sets, N, K // 32), "w_scale")
         _want(row_end, row_begin.shape, "row_end")
-        _want(bias, (sets, N), "bias")
+        if bias is not None:
+            _want(bias, (sets, N), "bias")
     op, os_ = _rows(at, out, (rows, N), bf, "out")
     _check(load().regione_mxfp4_grouped_matmul(
         _on(at, x_q, u8, "x_q"), _on(at, x_scale, u8, "x_scale"), _on(at, w_q, u8, "w_q"), _on(at, w_scale, u8, "w_scale"),

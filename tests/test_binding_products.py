@@ -84,3 +84,14 @@ def test_a_tensor_of_another_device_is_refused(called, name, arg):
     with pytest.raises(binding.RegionEError, match=f"^{arg} is on cuda:1"):
         getattr(binding, name)(**_args(name, **{arg: Tensor(shape, dtype, at=1)}))
     assert not called
+
+
+@pytest.mark.parametrize("name,arg", [(name, arg) for name, args in CALLS.items() for arg in args])
+@pytest.mark.parametrize("other", ["fewer dimensions", "more dimensions", "no tensor"])
+def test_other_dimensions_are_refused_by_name(called, name, arg, other):
+    """By the library's own error, whatever is wrong with the argument."""
+    shape, dtype = CALLS[name][arg]
+    t = {"fewer dimensions": Tensor(shape[1:], dtype), "more dimensions": Tensor((1, *shape), dtype), "no tensor": list(range(3))}[other]
+    with pytest.raises(binding.RegionEError, match=rf"^{arg} |row_end must have shape" if arg == "row_begin" else f"^{arg} "):
+        getattr(binding, name)(**_args(name, **{arg: t}))
+    assert not called
