@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(kFp4Threads) mxfp4_dequantize_kernel(const Fp4
 
 // Rows that lie one behind the other and are all live are one long row.
 static int launch_fp4_rows(bool quantize, Fp4Rows p, int B, cudaStream_t st) {
+    if (B * std::max(p.cap, p.src_rows) > (1LL << 50) / p.E) return REGIONE_UNSUPPORTED;   // elements: nothing below passes 64 bits
     if (p.idx == nullptr && p.n == nullptr && p.src_rows == p.cap) {
         p.E *= p.cap * B;
         p.cap = p.src_rows = 1;
