@@ -645,6 +645,15 @@ int regione_selftest_attention_plan(const int32_t* n_q, const int32_t* n_fresh, 
 int regione_selftest_attention_form(int B, int Nq_cap, int Nf_cap, int Nc_cap, int H, int D, int out_cap, int refreshes);
 
 /*
+ * Lets the bounded waits of a grouped product run out, as regione_selftest_bounded_wait does: one thread waits, through the
+ * routines that the kernel's roles wait with, on a barrier that nothing ever arrives on, as a lone block does, as a block
+ * of a pair does (limit_cycles, 1 .. 10^6, each), and once more with a thousand times that and the abort flag raised.
+ * out : dev int64 [3][3], nullable: of each wait {1 if it claimed completion (must be 0), cycles spent, 1 if the abort
+ *       flag is raised behind it (must be 1)}.
+ */
+int regione_selftest_grouped_wait(long long limit_cycles, int32_t* dev_status, long long* out, void* stream);
+
+/*
  * What a grouped product takes of the ranges it is given: the function that the kernel runs, run on the host.
  * row_begin, row_end, begin, rows: host int32 [groups]; the rows of group g are [begin[g], begin[g] + rows[g]).
  * Returns how many of the ranges are not within [0, rows_cap], -1 for invalid arguments.

@@ -88,6 +88,7 @@ SIGNATURES = {
     "regione_selftest_bounded_wait": (c_int, [c_longlong, _P, _P, _P]),
     "regione_selftest_attention_plan": (c_int, [_P, _P, _P] + [c_int] * 8 + [_P, _P, c_int]),
     "regione_selftest_attention_form": (c_int, [c_int] * 8),
+    "regione_selftest_grouped_wait": (c_int, [c_longlong, _P, _P, _P]),
     "regione_selftest_group_ranges": (c_int, [_P, _P, c_int, c_int, _P, _P]),
 }
 
@@ -683,6 +684,14 @@ def selftest_bounded_wait(limit_cycles, dev_status, out=None, stream=None):
     _check(load().regione_selftest_bounded_wait(
         int(limit_cycles), _ptr(dev_status, torch.int32, "dev_status"), _ptr(out, torch.int64, "out"),
         _stream(stream)), "regione_selftest_bounded_wait")
+
+
+def selftest_grouped_wait(limit_cycles, dev_status, out=None, stream=None):
+    """Lets the bounded waits of a grouped product expire (see the header); ``out`` int64 [3, 3], optional."""
+    torch = _torch()
+    _check(load().regione_selftest_grouped_wait(
+        int(limit_cycles), _ptr(dev_status, torch.int32, "dev_status"), _ptr(out, torch.int64, "out"),
+        _stream(stream)), "regione_selftest_grouped_wait")
 
 
 def avd_step(running_product: float, dt: float, gamma: float, delta: float):

@@ -66,7 +66,7 @@ struct GroupedMaps {
 };
 
 struct GroupedControl {
-    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
     uint32_t tmem;
     int abort_flag;
     int width, total;                                 // of the plan: rows of a tile at most, tiles
@@ -192,11 +192,12 @@ template <bool PAIR> __device__ __forceinline__ bool try_wait(uint32_t bar, uint
     return PAIR ? ptx::mbar_try_wait_cluster(bar, parity) : ptx::mbar_try_wait(bar, parity);
 }
 template <bool PAIR>
-__device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status) {
+__device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status,
+                                                  long long limit) {
     const long long t0 = clock64();
     while (!try_wait<PAIR>(bar, parity)) {
         if (*abort_flag) return false;
-        if (clock64() - t0 > kGroupedWait) {
+        if (clock64() - t0 > limit) {
             *abort_flag = 1;
             record_status(dev_status, REGIONE_DEV_TIMEOUT);
             return false;
@@ -204,8 +205,10 @@ __device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity,
     }
     return true;
 }
-template <bool PAIR> __device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, GroupedControl* ctl, int32_t* dev_status) {
-    return try_wait<PAIR>(bar, parity) || grouped_wait_slow<PAIR>(bar, parity, &ctl->abort_flag, dev_status);
+template <bool PAIR>
+__device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, GroupedControl* ctl, int32_t* dev_status,
+                                             long long limit = kGroupedWait) {
+    return try_wait<PAIR>(bar, parity) || grouped_wait_slow<PAIR>(bar, parity, &ctl->abort_flag, dev_status, limit);
 }
 
 // Two fp32 operations in one instruction.
@@ -445,7 +448,6 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             ptx::mbar_init(ptx::smem_addr(&ctl->acc_full[a]), 1);
             ptx::mbar_init(ptx::smem_addr(&ctl->acc_empty[a]), kEpiWarps * (PAIR ? 2 : 1));
         }
-        ptx::mbar_init(ptx::smem_addr(&ctl->drain), 1);
         ctl->abort_flag = 0;
         ptx::fence_barrier_init();
     }
@@ -536,7 +538,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         return PAIR ? ptx::map_rank(a, rank & ~1) : a;
     };
     // What a role keeps from tile to tile: its group, its place in the ring, its tiles so far.
-    int group = 0, s = 0, it = 0, filled = 0, sf = 0;
+    int group = 0, s = 0, it = 0, sf = 0;
     uint32_t phase = 0;
     bool ok = true;
     const bool elected = ptx::elect_one();
@@ -565,7 +567,6 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                                 load_x<PAIR>(dst + kTileBytes + at * kChunkBytes, &maps.x[box], bar, c * (FP4 ? kChunkBytes : kElems), row + at);
                                 at += 16 << box;
                             }
-                        ++filled;
                         if (++s == stages) { s = 0; phase ^= 1; }
                     }
                 }
@@ -764,25 +765,44 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     }
 
     if (PAIR && warp < kEpiWarps && lane == 0) ptx::bulk_wait_all();
-    if (!ok && leader && elected && warp == kProducer) { // copies in flight land before shared memory is given up
-        for (int i = min(filled, stages); i > 0; --i) {
-            int q = s - i;
-            uint32_t ph = phase;
-            if (q < 0) { q += stages; ph ^= 1; }
-            const long long t0 = clock64();
-            while (!ptx::mbar_try_wait(ptx::smem_addr(&ctl->full[q]), ph) && clock64() - t0 < kGroupedWait / 8) {}
+    __syncwarp();
+    if ((PAIR || split) && (threadIdx.x & 31) == 0 && *(volatile int*)&ctl->abort_flag)
+        for (int r = 0; r < (PAIR ? 2 : 1) * p.slices; ++r)
+            asm volatile("st.relaxed.cluster.shared::cluster.s32 [%0], %1;" ::"r"(ptx::map_rank(ptx::smem_addr(&ctl->abort_flag), r)), "r"(1) : "memory");
+    ptx::tc_fence_before_sync();
+    if (PAIR || split) ptx::cluster_sync(); else __syncthreads();
+    ptx::tc_fence_after_sync();
+    // Where any role gave up (every CTA of the cluster sees it), copies and products in flight get a quarter of a second before shared and
+    // tensor memory are given up.
+    if (*(volatile int*)&ctl->abort_flag) {
+        for (const long long t0 = clock64(); clock64() - t0 < kGroupedWait / 8;) {}
+        if (PAIR || split) ptx::cluster_sync(); else __syncthreads();
+    }
+    if (warp == kIssuer) free_tmem<PAIR>(tmem, p.tmem_columns);
+}
+
+// The waits of the roles, run out in the harmless form: on a barrier that nothing arrives on, with no copy and no product in flight.  One
+// of a lone CTA and one of a pair's with the limit, and one with a thousand times that, which sees that another role gave up.
+__global__ void grouped_wait_selftest_kernel(long long limit, int32_t* dev_status, long long* out) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    GroupedControl* ctl = reinterpret_cast<GroupedControl*>(smem_raw);
+    const uint32_t bar = ptx::smem_addr(&ctl->full[0]);
+    if (threadIdx.x > 0) return;
+    ptx::mbar_init(bar, 1);
+    ptx::fence_barrier_init();
+    for (int i = 0; i < 3; ++i) {
+        if (i < 2) *(volatile int*)&ctl->abort_flag = 0;
+        const long long t0 = clock64();
+        const bool done = i == 1 ? grouped_wait<true>(bar, 0, ctl, dev_status, limit)
+                                 : grouped_wait<false>(bar, 0, ctl, dev_status, i == 0 ? limit : 1000 * limit);
+        const long long spent = clock64() - t0;
+        if (out != nullptr) {
+            out[3 * i] = done;
+            out[3 * i + 1] = spent;
+            out[3 * i + 2] = *(volatile int*)&ctl->abort_flag;
         }
     }
-    if (!ok && leader && elected && warp == kIssuer) {  // products in flight end before tensor memory is given up
-        commit<PAIR>(ptx::smem_addr(&ctl->drain), pair_mask);
-        const long long t0 = clock64();
-        while (!ptx::mbar_try_wait(ptx::smem_addr(&ctl->drain), 0) && clock64() - t0 < kGroupedWait / 8) {}
-    }
-    __syncwarp();
-    ptx::tc_fence_before_sync();
-    if (cluster > 1) ptx::cluster_sync(); else __syncthreads();
-    ptx::tc_fence_after_sync();
-    if (warp == kIssuer) free_tmem<PAIR>(tmem, p.tmem_columns);
+    ptx::mbar_inval(bar);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
@@ -1004,4 +1024,10 @@ extern "C" int regione_selftest_group_ranges(const int32_t* row_begin, const int
     int outside = 0;
     for (int g = 0; g < groups; ++g) outside += !cut_range(row_begin[g], row_end[g], rows_cap, begin[g], rows[g]);
     return outside;
+}
+
+extern "C" int regione_selftest_grouped_wait(long long limit_cycles, int32_t* dev_status, long long* out, void* stream) {
+    if (limit_cycles < 1 || limit_cycles > 1000000LL) return REGIONE_INVALID_ARG;
+    grouped_wait_selftest_kernel<<<1, 32, sizeof(GroupedControl), (cudaStream_t)stream>>>(limit_cycles, dev_status, out);
+    return launch_status(cudaGetLastError());
 }
