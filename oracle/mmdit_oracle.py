@@ -20,6 +20,10 @@ A block (weights index s = 0 for text rows, 1 for image and reference rows; all 
     h += gate1 * (attention(q, k, v) @ o_s);  m = LN(h) * (1 + scale2) + shift2
     h += gate2 * (gelu_tanh(m @ fc1_s) @ fc2_s)
 and the velocity of the image tokens is LN(h_image) @ w_out.
+
+In 4 bits (``products="mxfp4"``) the two operands of a @ qkv_s, attention @ o_s, m @ fc1_s and gelu @ fc2_s are replaced by what the
+4-bit microscaled format holds of them: rows, rounded to bf16 before, in blocks of 32 along K, weights in blocks of 32 along K of each
+feature.  ``cache="mxfp4"``: so are the kept rows of K and V, in blocks of 32 along a head, when they are stored.
 """
 from __future__ import annotations
 
@@ -38,10 +42,26 @@ def _gelu_tanh(x):
     return 0.5 * x * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (x + 0.044715 * x ** 3)))
 
 
+def _bf16(x):
+    """Nearest bf16 value, ties to even (finite x)."""
+    m, e = np.frexp(np.asarray(x, np.float64))
+    return np.ldexp(np.round(m * 256.0), e - 8)
+
+
+def _held(x):
+    """What the 4-bit format holds of rows that were rounded to bf16."""
+    return orc.mxfp4_dequantize(*orc.mxfp4_quantize(_bf16(x)))
+
+
 class MMDiTOracle:
     def __init__(self, weights, n_text, n_img, n_ref, heads, head_dim, blocks, cos, sin, ref, planted,
-                 membership="paper"):
+                 membership="paper", products="exact", cache="exact"):
         self.w = {k: np.asarray(v, np.float64) for k, v in weights.items()}
+        self.products, self.cache = products, cache
+        if products == "mxfp4":
+            for k in self.w:
+                if k.startswith(("qkv", "o", "fc")):
+                    self.w[k] = _held(self.w[k].T).T
         self.n_text, self.n_img, self.n_ref = n_text, n_img, n_ref
         self.H, self.D, self.L = heads, head_dim, blocks
         self.cos, self.sin = np.asarray(cos, np.float64), np.asarray(sin, np.float64)
@@ -63,6 +83,8 @@ class MMDiTOracle:
     def _per_stream(self, x, streams, name):
         """Row-wise x @ W_s with the weight set of each row's stream."""
         out = None
+        if self.products == "mxfp4":
+            x = _held(x)
         for s in (0, 1):
             sel = streams == s
             if not sel.any():
@@ -131,6 +153,8 @@ class MMDiTOracle:
 
         def attend(l, q, k, v):
             kc, vc = orc.rikv_store(self.k_full[l], self.v_full[l], cr[None], [nc])
+            if self.cache == "mxfp4":
+                kc, vc = _held(kc), _held(vc)
             return orc.region_attention(q[None], k[None], v[None], kc, vc, [nq], [nq], [nc])[0]
 
         h = self._blocks(h, t, qr, streams, attend)
