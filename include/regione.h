@@ -274,7 +274,7 @@ int regione_rikv_load_e4m3(const uint8_t* k_q, const uint8_t* v_q, const float* 
  * consecutive elements of a row share one power-of-two scale, an element is a 4-bit E2M1 value (1 sign,
  * 2 exponent, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives):
  *     s = 2^k, k the smallest integer with max |x| / 2^k <= 6 over the 32 elements (k = 0 if all are zero;
- *         k >= -127); stored as the byte k + 127 (E8M0)
+ *         k >= -127); stored as the byte k + 127 (E8M0); 255, which no row is given, stands for NaN where it is read
  *     code = nearest E2M1 value of x / s, ties to the even code; elements 2i and 2i + 1 of a row are the low
  *         and the high half of byte i
  *     value(code) * s is exact in bf16 (but for 2^128, to which maxima above 1.75 * 2^127 are rounded: infinite)

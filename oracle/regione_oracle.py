@@ -617,7 +617,8 @@ def mxfp4_quantize(x):
 def mxfp4_dequantize(codes, scales):
     code = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], 2 * codes.shape[-1])
     v = np.where(code & 8, -1.0, 1.0) * E2M1[code & 7]
-    return v * np.repeat(2.0 ** (scales.astype(np.float64) - 127.0), 32, axis=-1)
+    s = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127.0))
+    return v * np.repeat(s, 32, axis=-1)
 
 
 def grouped_matmul(x, w, row_begin, row_end, out, bias=None, gelu=False):

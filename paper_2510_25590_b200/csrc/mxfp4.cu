@@ -74,9 +74,9 @@ __device__ __forceinline__ float2 widen_f16x2(uint32_t h2) {
     return r;
 }
 
-// 2^k, -149 <= k <= 127 (below -126 a subnormal).
-__device__ __forceinline__ float pow2(int k) {
-    return __uint_as_float(k >= -126 ? (uint32_t)(k + 127) << 23 : 1u << (k + 149));
+// What a scale byte stands for: 2^(code - 127) (0: a subnormal), 255 a NaN.
+__device__ __forceinline__ float scale_value(int code) {
+    return __uint_as_float(code == 0 ? 0x00400000u : code < 255 ? (uint32_t)code << 23 : 0x7fc00000u);
 }
 
 // k + 127 of a block's scale from its largest magnitude as bf16 bits without their sign.  With exponent field E and seven mantissa
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kFp4Threads) mxfp4_dequantize_kernel(const Fp4
     const int mine = lane * 32 < live ? scales[lane] : 127;
 #pragma unroll
     for (int u = 0; u < kFp4Unroll; ++u) {
-        const float s = pow2(__shfl_sync(0xffffffffu, mine, u * 8 + (lane >> 2)) - 127);
+        const float s = scale_value(__shfl_sync(0xffffffffu, mine, u * 8 + (lane >> 2)));
         uint32_t h[4];
         unpack_e2m1x8(q[u], h);
         const float2 a = widen_f16x2(h[0]), b = widen_f16x2(h[1]), c = widen_f16x2(h[2]), d = widen_f16x2(h[3]);
