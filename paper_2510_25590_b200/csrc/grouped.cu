@@ -153,17 +153,18 @@ __device__ __forceinline__ void load_x(uint32_t dst, const CUtensorMap* map, uin
 }
 
 // Arrival on a barrier of this CTA or, in a pair, of its leader: at the cluster's scope where that is another CTA, since a thread of that
-// CTA acts on what is announced.  An ordinary release at that scope waits for all memory operations of the warp that are on their way
-// (16896 x 4096 x 8192 in 4 bits 347 us), which is more than what is announced (in this form 234).  SMEM: the warp's writes to its
-// own CTA's shared memory (scales, behind their proxy fence); the release is restricted to those.  Else an accumulator that was
-// read out: tcgen05 operations are ordered by the fences of their own on both sides, around an arrival that releases nothing.
-template <bool PAIR, bool SMEM> __device__ __forceinline__ void arrive_at(uint32_t bar, int rank) {
-    if (PAIR && (rank & 1)) {
-        if (SMEM) asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+// CTA acts on what is announced.  It releases nothing there.  An accumulator that was read out: tcgen05 operations are ordered by the
+// fences of their own on both sides.  Scales: behind release_smem, which is restricted to the warp's writes to its own CTA's shared
+// memory (themselves behind their proxy fence); an ordinary release at that scope waits for all memory operations of the warp that
+// are on their way (16896 x 4096 x 8192 in 4 bits 347 us, in this form 234).
+template <bool PAIR> __device__ __forceinline__ void release_smem(int rank) {
+    if (PAIR && (rank & 1)) asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void arrive_at(uint32_t bar, int rank) {
+    if (PAIR && (rank & 1))
         asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(ptx::map_rank(bar, rank & ~1)) : "memory");
-    } else {
+    else
         ptx::mbar_arrive(bar);
-    }
 }
 
 // 16 rows of 32 features from shared memory (64-byte swizzle) to the output; what lies behind the last feature is not written.
@@ -187,15 +188,16 @@ __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t a, uin
 }  // namespace
 
 // ---- waits: bounded; a wait that runs out is recorded and makes the other roles of the CTA give up -----------------
-// In a pair arrivals come from the other CTA as well, so that its waits acquire at the cluster's scope.
-template <bool PAIR> __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-    return PAIR ? ptx::mbar_try_wait_cluster(bar, parity) : ptx::mbar_try_wait(bar, parity);
+// FAR: a thread of the pair's other CTA is among those that arrive.  (Where only copies and products complete, which the hardware
+// announces, the scope is the CTA whichever CTA issued them; acquiring at the cluster's everywhere takes 8192^3 in 4 bits from 238 to 252 us.)
+template <bool FAR> __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    return FAR ? ptx::mbar_try_wait_cluster(bar, parity) : ptx::mbar_try_wait(bar, parity);
 }
-template <bool PAIR>
+template <bool FAR>
 __device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status,
                                                   long long limit) {
     const long long t0 = clock64();
-    while (!try_wait<PAIR>(bar, parity)) {
+    while (!try_wait<FAR>(bar, parity)) {
         if (*abort_flag) return false;
         if (clock64() - t0 > limit) {
             *abort_flag = 1;
@@ -205,10 +207,10 @@ __device__ __forceinline__ bool grouped_wait_slow(uint32_t bar, uint32_t parity,
     }
     return true;
 }
-template <bool PAIR>
+template <bool FAR = false>
 __device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, GroupedControl* ctl, int32_t* dev_status,
                                              long long limit = kGroupedWait) {
-    return try_wait<PAIR>(bar, parity) || grouped_wait_slow<PAIR>(bar, parity, &ctl->abort_flag, dev_status, limit);
+    return try_wait<FAR>(bar, parity) || grouped_wait_slow<FAR>(bar, parity, &ctl->abort_flag, dev_status, limit);
 }
 
 // Two fp32 operations in one instruction.
@@ -320,7 +322,8 @@ __device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const Group
 // Scales of the tiles [t0, t_end): 8 bytes a row and chunk, from rows that lie K / 32 bytes apart to the places in shared memory that
 // the copy to tensor memory reads.  A team of four warps takes a part of two chunks, 16 bytes a row, a warp every fourth group
 // of 32 rows; a pair of CTAs has two teams that take turns (8192^3: 249 us with one team, 209 with two).  Loads for the next part
-// are not sent ahead: the proxy fence would wait for them.  The stage that a team waits for is at most four chunks behind its last
+// are not sent ahead: the proxy fence would wait for them.  In a pair of CTAs both chunks of a part are announced behind one pair of
+// fences (8192 x 4096 x 8192: 194 000 cycles with a pair each, 186 000 so; lone CTAs have less to wait for and announce each).  The stage that a team waits for is at most four chunks behind its last
 // one and the ring has at least four stages: no phase of a barrier can be mistaken for the one two further on.
 // VEC, rows on 16 bytes: a lane reads its row's 16 bytes, 32 rows in one load.  Else four lanes read a word each, 8 rows in one load: as
 // many lines of the L1 a row (2 x 4992 x 296 for four times 764 rows: 14.9 us, a lane with the four words of its row 20.8).
@@ -384,7 +387,7 @@ __device__ __forceinline__ bool bring_scales(const GroupedArgs& p, const ScaleRo
         int at = s;
         uint32_t turn = phase;
         for (int k = 0; k < n; ++k) {
-            if (!__all_sync(0xffffffffu, grouped_wait<PAIR>(ptx::smem_addr(&r.ctl->empty[at]), turn ^ 1, r.ctl, p.dev_status))) return false;
+            if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&r.ctl->empty[at]), turn ^ 1, r.ctl, p.dev_status))) return false;
             uint32_t* base = reinterpret_cast<uint32_t*>(r.scales + at * (kScaleA + kScaleB)) + member * 32;
             const bool odd = (first + k) & 1;
 #pragma unroll
@@ -403,11 +406,14 @@ __device__ __forceinline__ bool bring_scales(const GroupedArgs& p, const ScaleRo
                     dst[24] = v[i].w;
                 }
             }
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                const uint32_t bar = ptx::smem_addr(&r.ctl->full[at]);
-                arrive_at<PAIR, true>(bar, r.rank);
+            if (!PAIR || k == n - 1) {
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    release_smem<PAIR>(r.rank);
+                    if (PAIR && k > 0) arrive_at<PAIR>(ptx::smem_addr(&r.ctl->full[s]), r.rank);
+                    arrive_at<PAIR>(ptx::smem_addr(&r.ctl->full[at]), r.rank);
+                }
             }
             if (++at == r.stages) { at = 0; turn ^= 1; }
         }
@@ -556,7 +562,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     const uint32_t bytes = (kTileBytes + rows * kChunkBytes) * (PAIR ? 2 : 1);
                     const int feature = tile.feature + half * kFeat, row = tile.first + half * rows;
                     for (int c = c_begin; c < c_end; ++c) {
-                        if (!grouped_wait<PAIR>(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
+                        if (!grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
                         if (leader) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&ctl->full[s]), bytes);
                         const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * stage_bytes;
                         load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
@@ -587,7 +593,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                                                : ptx::idesc_bf16_f32(PAIR ? 256 : 128, tile.width, false);
                     uint32_t accumulate = 0;
                     for (int c = c_begin; c < c_end; ++c) {
-                        if (!grouped_wait<PAIR>(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
+                        if (!grouped_wait<PAIR && FP4>(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
                         ptx::tc_fence_after_sync();
                         const uint32_t at = smem + s * stage_bytes;
                         const uint32_t a_lo = ptx::smem_desc_lo(at, 16), b_lo = ptx::smem_desc_lo(at + kTileBytes, 16);
@@ -644,7 +650,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         const float b = __uint_as_float((uint32_t)__ldg(p.bias + (size_t)tile.weights * p.N + f) << 16);
                         bias[i] = pair_of(b, b);
                     }
-                if (!__all_sync(0xffffffffu, grouped_wait<PAIR>(ptx::smem_addr(&ctl->acc_full[a]), use & 1, ctl, p.dev_status)))
+                if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->acc_full[a]), use & 1, ctl, p.dev_status)))
                     break;
                 ptx::tc_fence_after_sync();
                 const uint32_t acc = tmem + (a ? kAcc1 : 0) + ((uint32_t)(32 * sub) << 16);
@@ -709,7 +715,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 }
                 ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) arrive_at<PAIR, false>(ptx::smem_addr(&ctl->acc_empty[a]), rank);
+                if (lane == 0) arrive_at<PAIR>(ptx::smem_addr(&ctl->acc_empty[a]), rank);
             }
         }
         // ---- the slices of a tile meet --------------------------------------------------------------------------------------
