@@ -12,15 +12,16 @@
 //
 // Two kernels.  Pairs of CTAs (cta_group::2, 256 features, up to 256 rows, a persistent cluster per pair of SMs, two accumulators so
 // that sums leave while the next tile's products run) for what fills the GPU: 8192^3 in bf16 700 us = 1.57 PFLOP/s with
-// the tensor pipe 92 % busy (the clock is what the power limit leaves), in 4 bits 207 us = 5.3 PFLOP/s; a library product in bf16
-// takes 675.  Lone CTAs (128 features, up to 128 rows, two to an SM) for less, where the start of a launch is what counts: 1024^3
-// 7.9 us, in 4 bits 6.0; two rows against 2 x 6144 x 1024 weights 7.1 us (25 MB, 3.9 us at the copy rate), 5.0 in 4 bits.  Both can
-// split K over the CTAs of a cluster, which add their sums in the order of the slices (225 rows, K 7544, N 80: 29 us whole, 10
-// in eight slices).  The host chooses from the capacities, the width of a pair's tiles is chosen on the device from the rows.
+// the tensor pipe 92 % busy (the clock is what the power limit leaves), in 4 bits 228 us = 4.8 PFLOP/s; a library product in bf16
+// takes 670.  Lone CTAs (128 features, up to 128 rows; two to an SM with tiles of up to 64 rows, of 32 in 4 bits) for less, where
+// the start of a launch is what counts: 1024^3 7.9 us, in 4 bits 6.0; two rows against 2 x 6144 x 1024 weights 7.2 us (25 MB, 3.9 us
+// at the copy rate), 5.2 in 4 bits.  Both can split K over the CTAs of a cluster, which add their sums in the order of the
+// slices (225 rows, K 7544, N 80: 29 us whole, 10 in eight slices).  The host chooses from the capacities, the width of a pair's tiles
+// is chosen on the device from the rows.
 //
 // What bounds them: bf16 the tensor core; 4 bits, whose operands last a quarter as long, the way from L2 into the SMs (30 KB a
 // chunk in 400 ns of which the products are 272), and with K below 4096 the sums' way out; few rows the weights' way from
-// device memory (64 experts of 2048 x 1408 with 4096 rows: 69 us, 62 at the copy rate).
+// device memory (64 experts of 2048 x 1408 with 4096 rows: 70 us, 62 at the copy rate).
 #include "common.cuh"
 #include "grouped_plan.cuh"
 #include "sm100_ptx.cuh"
@@ -36,7 +37,7 @@ constexpr int kMaxStages = 12;
 constexpr int kMaxGroups = 512;
 constexpr int kScaleA = 1024, kScaleB = 2048;         // scales of a stage: [2 of 128 elements][1 or 2 of 128 rows][512 bytes]
 // Warps of a CTA: 8 (4) that take sums out of tensor memory, one that loads, one that issues products, and with 4-bit operands 8 (4) that
-// bring the scales: a pair of CTAs fills its SMs, CTAs without a pair leave room for a second one.
+// bring the scales: a pair of CTAs fills its SMs, CTAs without a pair and with narrow tiles leave room for a second one.
 template <bool FP4, bool PAIR> struct Roles {
     static constexpr int kEpi = PAIR ? 8 : 4, kScale = PAIR ? 8 : 4, kThreads = (kEpi + 2 + (FP4 ? kScale : 0)) * 32;
 };
@@ -156,7 +157,7 @@ __device__ __forceinline__ void load_x(uint32_t dst, const CUtensorMap* map, uin
 // CTA acts on what is announced.  It releases nothing there.  An accumulator that was read out: tcgen05 operations are ordered by the
 // fences of their own on both sides.  Scales: behind release_smem, which is restricted to the warp's writes to its own CTA's shared
 // memory (themselves behind their proxy fence); an ordinary release at that scope waits for all memory operations of the warp that
-// are on their way (16896 x 4096 x 8192 in 4 bits 347 us, in this form 234).
+// are on their way (17408 x 4096 x 8192 with GELU in 4 bits 347 us, in this form 234).
 template <bool PAIR> __device__ __forceinline__ void release_smem(int rank) {
     if (PAIR && (rank & 1)) asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
 }
@@ -906,8 +907,8 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
     p.chunks = (p.K + kElems - 1) / kElems;
     const int groups = std::min(p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
     const int f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
-    // What the launch will take, in ns, if every row of the buffer is live and the groups are alike: what a launch takes before and behind
-    // its tiles, and rounds of tiles, each the chunks of a slice times what a chunk takes (no less than 200 by latency; 105 bytes
+    // What the launch will take, in ns, if every row of the buffer is live and the groups are alike (1280 live rows in a buffer of 8704, K 2048,
+    // N 6144: as long as in one of 1280; 205 in 2304 19.4 us, in 205 17.4): what a launch takes before and behind its tiles, and rounds of tiles, each the chunks of a slice times what a chunk takes (no less than 200 by latency; 105 bytes
     // a ns to an SM; the tensor core), and the way of the slices' sums to each other.
     long long best = 0x7fffffffffffffffLL;
     int clusters = 0;
@@ -951,7 +952,7 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
         p.tmem_columns = 512;
         p.scale_column = 448;
     } else {
-        // two CTAs an SM, with a slice's chunks in the ring if they fit; at least four stages (see the scales)
+        // two CTAs an SM where four stages (see the scales) leave room for them, with a slice's chunks in the ring if they fit
         const int stage = kTileBytes + p.width * kChunkBytes + (FP4 ? kScaleA + kScaleB : 0), mine = (p.chunks + p.slices - 1) / p.slices;
         p.ring_bytes = std::max(4 * stage, std::min(grouped_ring<FP4, false>(kSmemHalf), std::min(kMaxStages, mine) * stage));
         p.scale_column = p.width <= 64 ? 64 : 128;
