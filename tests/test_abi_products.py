@@ -52,15 +52,3 @@ def test_mxfp4_cache():
     assert st(D=96) == binding.UNSUPPORTED and st(cap=0) == binding.OK and st(B=0) == binding.OK
     ld = lambda D=64, n=FAKE, cap=8: lib.regione_rikv_load_mxfp4(FAKE, FAKE, FAKE, FAKE, n, 1, cap, 3, D, FAKE, FAKE, NULL, NULL)
     assert ld(D=32) == binding.UNSUPPORTED and ld(n=NULL) == binding.INVALID_ARG and ld(cap=0) == binding.OK
-
-
-def test_mxfp4_sizes_that_pass_64_bits():
-    """Numbers of elements are counted in 64 bits: what does not fit is refused before anything is multiplied."""
-    lib = binding.load()
-    many, wide = (1 << 31) - 1, (1 << 31) - 32
-    assert lib.regione_mxfp4_quantize(FAKE, NULL, NULL, 4, many, many, wide, FAKE, FAKE, NULL, NULL) == binding.UNSUPPORTED
-    assert lib.regione_mxfp4_quantize(FAKE, FAKE, FAKE, many, many, many, wide, FAKE, FAKE, NULL, NULL) == binding.UNSUPPORTED
-    assert lib.regione_mxfp4_dequantize(FAKE, FAKE, NULL, 8, many, wide, FAKE, NULL, NULL) == binding.UNSUPPORTED
-    assert lib.regione_mxfp4_dequantize(FAKE, FAKE, FAKE, many, many, wide, FAKE, NULL, NULL) == binding.UNSUPPORTED
-    assert lib.regione_rikv_store_mxfp4(FAKE, FAKE, FAKE, FAKE, many, 8, many, many, 128, FAKE, FAKE, FAKE, FAKE, NULL, NULL) == binding.UNSUPPORTED
-    assert lib.regione_rikv_load_mxfp4(FAKE, FAKE, FAKE, FAKE, FAKE, many, many, many, 128, FAKE, FAKE, NULL, NULL) == binding.UNSUPPORTED
