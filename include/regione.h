@@ -335,6 +335,71 @@ int regione_mxfp4_grouped_matmul(const uint8_t* x_q, const uint8_t* x_scale, con
                                  int32_t* dev_status, void* stream);
 
 /*
+ * Layer normalisation of ragged groups of rows, behind the gated residual update of a transformer block.  (The paper takes the
+ * model's blocks as given.)  Group g is the rows [row_begin[g], row_end[g]), its parameter set i = g mod n_sets (1: one weight and
+ * bias for all; groups: a modulation per request and stream):
+ *     z = x + gate_i r                       rounded to bf16 and kept in x_out; without r: z = x
+ *     out = (z - mean z) / sqrt(mean (z - mean z)^2 + eps) * w_i + bias_i,   w_i = weight_i, or 1 + weight_i (modulated)
+ * x, r, x_out, out dev bf16 [rows_cap, C], rows their stride apart; gate, weight, bias dev bf16 [n_sets, C], sets set_stride apart
+ * (parts of one modulation may be passed as they lie), each NULL or given: no gate is 1, no weight 1 (0 where modulated), no bias 0;
+ * mean, rstd dev f32 [rows_cap] or NULL, the row's mean and 1 / sqrt(...) for the backward pass; row_begin, row_end dev int32
+ * [groups].  r and x_out are both given or neither.  x_out may be x or r, and out may be x where r is not given or where x is not
+ * needed any more (an output may be an input of the same place, not one that lies elsewhere in it).  Rows of no group are left
+ * untouched and not read; no row may be in two groups; a range not within [0, rows_cap] is cut to it and REGIONE_DEV_BOUNDS recorded.
+ * C and the strides are multiples of 8, C <= 8192, groups <= 512, n_sets <= 65535, rows_cap <= 2^24 (REGIONE_UNSUPPORTED beyond).
+ * One kernel launch; nothing is allocated.
+ *
+ * regione_layer_norm_backward: its gradients.  x is the row that was normalised (x_out where r was given), mean and rstd what the
+ * forward pass wrote, dy the gradient of out, dx_out that of x_out from elsewhere (NULL: none):
+ *     h = (x - mean) rstd,  a = dy w_i,  d = dx_out + rstd (a - mean a - h mean (a h))
+ *     dx = d  (also the gradient of r where the forward pass had no gate),  dr = gate_i d
+ *     dweight_i = sum dy h,  dbias_i = sum dy,  dgate_i = sum d r      over the rows of all groups of set i
+ * r, gate and dr are given together or not at all.  dx, dr dev bf16 [rows_cap, C], rows of no group untouched; dx may be dy or
+ * dx_out.  dweight, dbias, dgate dev f32 [n_sets, C], contiguous, each NULL or given: they are written, not added to, and are zeros
+ * for a set without rows.  workspace: 16-byte aligned, regione_layer_norm_backward_workspace(...) bytes; two calls that may run at
+ * one time need one each.  Sums are added in an order that depends on the sizes and ranges only.  Two kernel launches.
+ */
+int regione_layer_norm(const regione_bf16* x, int64_t x_stride, const regione_bf16* r, int64_t r_stride, const regione_bf16* gate,
+                       const regione_bf16* weight, const regione_bf16* bias, int64_t set_stride, int modulated, float eps,
+                       const int32_t* row_begin, const int32_t* row_end, int rows_cap, int groups, int n_sets, int C,
+                       regione_bf16* x_out, int64_t x_out_stride, regione_bf16* out, int64_t out_stride, float* mean, float* rstd,
+                       int32_t* dev_status, void* stream);
+size_t regione_layer_norm_backward_workspace(int rows_cap, int groups, int C);
+int regione_layer_norm_backward(const regione_bf16* x, int64_t x_stride, const float* mean, const float* rstd, const regione_bf16* dy,
+                                int64_t dy_stride, const regione_bf16* dx_out, int64_t dx_out_stride, const regione_bf16* r,
+                                int64_t r_stride, const regione_bf16* gate, const regione_bf16* weight, int64_t set_stride,
+                                int modulated, const int32_t* row_begin, const int32_t* row_end, int rows_cap, int groups, int n_sets,
+                                int C, regione_bf16* dx, int64_t dx_stride, regione_bf16* dr, int64_t dr_stride, float* dweight,
+                                float* dbias, float* dgate, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                                void* stream);
+
+/*
+ * Rotary positions with several axes (which image or frame, row, column) for rows of Q and K, behind their per-head RMS
+ * normalisation.  (The paper states neither; it fixes that a recomputed token keeps its place: Sec. 4 "Region-Aware Generation".)
+ *     y = x / sqrt(mean_D(x^2) + eps) * weight        where normalise is set, else y = x
+ *     t_i = positions[b, place, axis[i]] * freq[i]    for the D/2 pairs, (a, b) -> (a cos t - b sin t, a sin t + b cos t);
+ *                                                     pair i is elements (2i, 2i+1) or (i, i + D/2) (rope_layout)
+ * for the rows j < n[b] (n NULL: every j < cap) of each request, place = idx[b, j] (idx NULL: j).  Row `place` of the source is
+ * read, or row j (src_compact, as in regione_fresh_qkv), and row j of the output written; rows past n[b] are left untouched.
+ * inverse: turned by -t, which is the gradient of the rotation (with normalise: REGIONE_UNSUPPORTED).
+ * q [B, rows, Hq, D], k [B, rows, Hk, D] (NULL with Hk = 0 and k_out NULL: Q alone) and the outputs [B, cap, H, D] dev bf16,
+ * requests *_batch and rows *_row elements apart (multiples of 8), 16-byte aligned: parts of one projection's rows may be passed as
+ * they lie.  positions dev f32 [B, n_pos, axes], requests positions_batch elements apart (0: the same for all); whole numbers are
+ * exact to 2^24.  The angle is off by no more than 2^-22 turns for positions and frequencies of up to 2^22 turns.  freq host f64 [D/2],
+ * radians a unit of position, 0 for pairs that are not turned; axis host int32 [D/2]; both are read during the call.  q_weight,
+ * k_weight dev bf16 [D] or NULL (ones).  A row may be turned in place (an output that is its source, idx NULL or src_compact);
+ * otherwise sources and outputs must not overlap.  D a multiple of 16 up to 256, axes <= 4.  A count outside [0, cap] is clamped, a
+ * place outside [0, n_pos) skipped, and REGIONE_DEV_BOUNDS recorded.  The sources have as many rows as places (src_compact: cap).
+ * One kernel launch; nothing is allocated.
+ */
+int regione_rotary_axes(const regione_bf16* q, int64_t q_batch, int64_t q_row, const regione_bf16* k, int64_t k_batch, int64_t k_row,
+                        const int32_t* idx, const int32_t* n, const float* positions, int64_t positions_batch, int B, int n_pos,
+                        int cap, int Hq, int Hk, int D, int axes, int src_compact, const double* freq, const int32_t* axis,
+                        int rope_layout, int inverse, int normalise, const regione_bf16* q_weight, const regione_bf16* k_weight,
+                        float eps, regione_bf16* q_out, int64_t q_out_batch, int64_t q_out_row, regione_bf16* k_out,
+                        int64_t k_out_batch, int64_t k_out_row, int32_t* dev_status, void* stream);
+
+/*
  * Region attention with the Region-Instruction KV cache (Sec. 4, "Region-Aware
  * Generation", the attention equation):
  *     out[b,i,h,:] = sum_j softmax_j( scale * q[b,i,h,:] . k_j ) * v_j

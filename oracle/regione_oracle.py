@@ -634,3 +634,60 @@ def grouped_matmul(x, w, row_begin, row_end, out, bias=None, gelu=False):
                 y = 0.5 * y * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (y + 0.044715 * y ** 3)))
             out[r] = y
     return out
+
+
+# ---- layer normalisation, rotary positions with several axes ----------------------------------------------------------------
+def layer_norm(x, weight, bias, ranges, eps, modulated=False, residual=None, gate=None, rounded=lambda z: z):
+    """(z, out, mean, 1 / std) of the rows of ``ranges`` [(begin, end)], zeros elsewhere; ``rounded``: how z is kept."""
+    x = np.asarray(x, np.float64)
+    z, out = np.zeros(x.shape), np.zeros(x.shape)
+    mean, rstd = np.zeros(len(x)), np.zeros(len(x))
+    sets = max(1 if p is None else len(p) for p in (weight, bias, gate))
+    for g, (b, e) in enumerate(ranges):
+        i = g % sets
+        for r in range(b, e):
+            row = x[r]
+            if residual is not None:
+                row = rounded(row + (1.0 if gate is None else np.asarray(gate[i], np.float64)) * np.asarray(residual[r], np.float64))
+            m = row.mean()
+            s = 1.0 / np.sqrt(((row - m) ** 2).mean() + eps)
+            w = (0.0 if modulated else 1.0) if weight is None else np.asarray(weight[i], np.float64)
+            z[r], mean[r], rstd[r] = row, m, s
+            out[r] = (row - m) * s * (w + (1.0 if modulated else 0.0)) + (0.0 if bias is None else np.asarray(bias[i], np.float64))
+    return z, out, mean, rstd
+
+
+def layer_norm_backward(z, mean, rstd, dy, weight, ranges, sets, modulated=False, dz=None, residual=None, gate=None):
+    """(dx, dresidual, dweight, dbias, dgate) of ``layer_norm``, from the row that was normalised."""
+    z, dy = np.asarray(z, np.float64), np.asarray(dy, np.float64)
+    C = z.shape[1]
+    dx, dr = np.zeros(z.shape), np.zeros(z.shape)
+    dweight, dbias, dgate = np.zeros((sets, C)), np.zeros((sets, C)), np.zeros((sets, C))
+    for g, (b, e) in enumerate(ranges):
+        i = g % sets
+        w = (0.0 if modulated else 1.0) if weight is None else np.asarray(weight[i], np.float64)
+        for r in range(b, e):
+            h = (z[r] - mean[r]) * rstd[r]
+            a = dy[r] * (w + (1.0 if modulated else 0.0))
+            dx[r] = rstd[r] * (a - a.mean() - h * (a * h).mean()) + (0.0 if dz is None else np.asarray(dz[r], np.float64))
+            dweight[i] += dy[r] * h
+            dbias[i] += dy[r]
+            if residual is not None:
+                dr[r] = np.asarray(gate[i], np.float64) * dx[r]
+                dgate[i] += dx[r] * np.asarray(residual[r], np.float64)
+    return dx, dr, dweight, dbias, dgate
+
+
+def rotary_axes(x, positions, freq, axis, interleaved, weight=None, eps=None, inverse=False):
+    """Rows x [rows, H, D] at positions [rows, axes], as turns of complex numbers, behind the normalisation where ``eps`` is given."""
+    y = np.asarray(x, np.float64)
+    D = y.shape[-1]
+    if eps is not None:
+        y = y / np.sqrt((y * y).mean(-1, keepdims=True) + eps) * (1.0 if weight is None else np.asarray(weight, np.float64))
+    t = np.asarray(positions, np.float64)[:, list(axis)] * np.asarray(freq, np.float64)
+    turn = np.exp(1j * (-t if inverse else t))[:, None, :]
+    out = np.empty_like(y)
+    first, second = (slice(0, None, 2), slice(1, None, 2)) if interleaved else (slice(0, D // 2), slice(D // 2, None))
+    w = (y[..., first] + 1j * y[..., second]) * turn
+    out[..., first], out[..., second] = w.real, w.imag
+    return out

@@ -68,6 +68,13 @@ SIGNATURES = {
     "regione_rikv_load_mxfp4": (c_int, [_P, _P, _P, _P, _P, c_int, c_int, c_int, c_int, _P, _P, _P, _P]),
     "regione_grouped_matmul": (c_int, [_P, c_int64, _P, _P, _P, _P] + [c_int] * 6 + [_P, c_int64, _P, _P]),
     "regione_mxfp4_grouped_matmul": (c_int, [_P] * 7 + [c_int] * 6 + [_P, c_int64, _P, _P]),
+    "regione_layer_norm": (c_int, [_P, c_int64, _P, c_int64, _P, _P, _P, c_int64, c_int, c_float, _P, _P] + [c_int] * 4 +
+                           [_P, c_int64, _P, c_int64, _P, _P, _P, _P]),
+    "regione_layer_norm_backward_workspace": (c_size_t, [c_int] * 3),
+    "regione_layer_norm_backward": (c_int, [_P, c_int64, _P, _P, _P, c_int64, _P, c_int64, _P, c_int64, _P, _P, c_int64, c_int, _P, _P] +
+                                    [c_int] * 4 + [_P, c_int64, _P, c_int64, _P, _P, _P, _P, c_size_t, _P, _P]),
+    "regione_rotary_axes": (c_int, [_P, c_int64, c_int64, _P, c_int64, c_int64, _P, _P, _P, c_int64] + [c_int] * 8 + [_P, _P] +
+                            [c_int] * 3 + [_P, _P, c_float, _P, c_int64, c_int64, _P, c_int64, c_int64, _P, _P]),
     "regione_region_attention_workspace": (c_size_t, [c_int] * 6),
     "regione_region_attention": (c_int, [_P] * 8 + [c_int] * 6 + [c_float, _P, _P, c_size_t, _P, _P]),
     "regione_region_attention_scatter": (c_int, [_P] * 8 + [c_int] * 6 + [c_float, _P, c_int, _P, _P, c_size_t, _P, _P]),
@@ -532,6 +539,179 @@ def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bi
         _on(at, bias, bf, "bias"), _on(at, row_begin, i32, "row_begin"), _on(at, row_end, i32, "row_end"), rows,
         row_begin.numel(), sets, K, N, activation, op, os_, _on(at, dev_status, i32, "dev_status"),
         _stream(stream)), "regione_mxfp4_grouped_matmul")
+
+
+def _sets(device, tensors, C):
+    """Sets and set distance of the parameters [sets, C] that are given, which have to lie alike, and their addresses."""
+    bf = _torch().bfloat16
+    sets, step, at = None, C, []
+    for t, name in tensors:
+        if t is None:
+            at.append(None)
+            continue
+        if sets is None:
+            _ranks(**{name: (t, 2)})
+            sets = t.shape[0]
+        where, apart = _rows(device, t, (sets, C), bf, name)
+        if sets > 1:
+            if step != apart and any(a is not None for a in at):
+                raise RegionEError(f"the sets of {name} are not as far apart as those of the other parameters")
+            step = apart
+        at.append(where)
+    return sets or 1, step, at
+
+
+def layer_norm(x, weight, bias, row_begin, row_end, out, eps, modulated=False, residual=None, gate=None, x_out=None, mean=None,
+               rstd=None, dev_status=None, stream=None):
+    """out[r] = norm(z[r]) * w + bias[i] for the rows r of group g, row_begin[g] <= r < row_end[g], with the parameter set
+    i = g % sets; w = weight[i], or 1 + weight[i] where ``modulated``.  z = x, or with ``residual`` z = x + gate[i] * residual, rounded
+    and kept in ``x_out`` (which may be ``x``).  ``x``, ``residual``, ``x_out``, ``out`` [rows, C] (rows may lie apart), ``weight``, ``bias``,
+    ``gate`` [sets, C] (sets may lie apart, all alike) or None; ``mean``, ``rstd`` [rows] fp32 for the backward pass; rows of no
+    group are left as they are."""
+    torch = _torch()
+    at = _here()
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    try:
+        rows, C = shape = x.shape
+        fits = row_end.shape == row_begin.shape
+    except (AttributeError, ValueError, IndexError):
+        _ranks(x=(x, 2), row_begin=(row_begin, None), row_end=(row_end, None))
+        raise
+    if not fits:
+        _want(row_end, row_begin.shape, "row_end")
+    if (residual is None) != (x_out is None) or residual is None and gate is not None:
+        raise RegionEError("residual and x_out are given together, and a gate only with them")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if t is not None:
+            _want(t, (rows,), name)
+    xp, xs = _rows(at, x, shape, bf, "x")
+    op, os_ = _rows(at, out, shape, bf, "out")
+    rp, rs = (None, 0) if residual is None else _rows(at, residual, shape, bf, "residual")
+    zp, zs = (None, 0) if x_out is None else _rows(at, x_out, shape, bf, "x_out")
+    sets, step, (wp, bp, gp) = _sets(at, ((weight, "weight"), (bias, "bias"), (gate, "gate")), C)
+    _check(load().regione_layer_norm(
+        xp, xs, rp, rs, gp, wp, bp, step, 1 if modulated else 0, eps, _on(at, row_begin, i32, "row_begin"),
+        _on(at, row_end, i32, "row_end"), rows, row_begin.numel(), sets, C, zp, zs, op, os_, _on(at, mean, f32, "mean"),
+        _on(at, rstd, f32, "rstd"), _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_layer_norm")
+
+
+def layer_norm_backward_workspace(rows, groups, C) -> int:
+    return int(load().regione_layer_norm_backward_workspace(rows, groups, C))
+
+
+def layer_norm_backward(x, mean, rstd, dy, weight, row_begin, row_end, dx, dweight, dbias, workspace, modulated=False, dx_out=None,
+                        residual=None, gate=None, dresidual=None, dgate=None, dev_status=None, stream=None):
+    """Gradients of ``layer_norm``: ``x`` is the row that was normalised (``x_out`` where there was a residual), ``dy`` the gradient
+    of ``out``, ``dx_out`` that of ``x_out`` from elsewhere.  ``dx`` [rows, C]; with ``residual`` and ``gate`` also ``dresidual`` (without a
+    gate the residual's gradient is ``dx``).  ``dweight``, ``dbias``, ``dgate`` [sets, C] fp32, each or None, are written: sums over the
+    rows of all groups of a set, in an order that does not depend on timing."""
+    torch = _torch()
+    at = _here()
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    try:
+        rows, C = shape = x.shape
+        fits = row_end.shape == row_begin.shape
+    except (AttributeError, ValueError, IndexError):
+        _ranks(x=(x, 2), row_begin=(row_begin, None), row_end=(row_end, None))
+        raise
+    if not fits:
+        _want(row_end, row_begin.shape, "row_end")
+    if (residual is None) != (gate is None) or (residual is None) != (dresidual is None) or dgate is not None and residual is None:
+        raise RegionEError("residual, gate and dresidual are given together, and dgate only with them")
+    _want(mean, (rows,), "mean")
+    _want(rstd, (rows,), "rstd")
+    sets, step, (wp, gp) = _sets(at, ((weight, "weight"), (gate, "gate")), C)
+    if weight is None and gate is None and (dweight is not None or dbias is not None):
+        sets = (dweight if dweight is not None else dbias).shape[0]
+    for t, name in ((dweight, "dweight"), (dbias, "dbias"), (dgate, "dgate")):
+        if t is not None:
+            _want(t, (sets, C), name)
+    rows_of = lambda t, name: (None, 0) if t is None else _rows(at, t, shape, bf, name)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().regione_layer_norm_backward(
+        *_rows(at, x, shape, bf, "x"), _on(at, mean, f32, "mean"), _on(at, rstd, f32, "rstd"), *_rows(at, dy, shape, bf, "dy"),
+        *rows_of(dx_out, "dx_out"), *rows_of(residual, "residual"), gp, wp, step, 1 if modulated else 0,
+        _on(at, row_begin, i32, "row_begin"), _on(at, row_end, i32, "row_end"), rows, row_begin.numel(), sets, C,
+        *_rows(at, dx, shape, bf, "dx"), *rows_of(dresidual, "dresidual"), _on(at, dweight, f32, "dweight"),
+        _on(at, dbias, f32, "dbias"), _on(at, dgate, f32, "dgate"), _on(at, workspace, getattr(workspace, "dtype", None), "workspace"),
+        ws_bytes, _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_layer_norm_backward")
+
+
+def rotary_frequencies(widths, theta=10000.0):
+    """(freq, axis) of ``rotary_axes`` for heads whose first widths[0] elements turn with axis 0, the next widths[1] with axis 1 and so
+    on, each axis with the frequencies theta ** (-2 i / width) of its own."""
+    if any(w < 0 or w % 2 for w in widths):
+        raise RegionEError("the elements of an axis come in pairs")
+    return ([float(theta) ** (-2.0 * i / w) for w in widths for i in range(w // 2)],
+            [a for a, w in enumerate(widths) for _ in range(w // 2)])
+
+
+def _heads(device, t, rows, name):
+    """Address, request and row distance of [B, rows, H, D] whose requests and rows may lie apart."""
+    B, n, H, D = t.shape
+    if t.get_device() != device:
+        _ptr(t, t.dtype, name)
+        raise RegionEError(f"{name} is on {t.device}, which is not the current device")
+    if t.dtype != _torch().bfloat16:
+        raise RegionEError(f"{name} must have dtype torch.bfloat16, got {t.dtype}")
+    if rows is not None and n != rows:
+        _want(t, (B, rows, H, D), name)
+    sb, sr, sh, sd = t.stride()
+    if D > 1 and sd != 1 or H > 1 and sh != D:
+        raise RegionEError(f"the heads of a row of {name} must be contiguous")
+    return t.data_ptr(), sb if B > 1 else 0, sr if n > 1 else H * D
+
+
+def rotary_axes(q, k, positions, freq, axis, q_out, k_out, layout, idx=None, n=None, q_weight=None, k_weight=None, eps=None,
+                src_compact=False, inverse=False, dev_status=None, stream=None):
+    """Rows of Q and K turned by the angles positions[b, place, axis[i]] * freq[i] of their places, behind the per-head RMS
+    normalisation where ``eps`` is given.  ``q`` [B, rows, Hq, D], ``k`` [B, rows, Hk, D] or None (requests and rows may lie apart),
+    ``positions`` [B or 1, places, axes] fp32, ``freq`` and ``axis`` D / 2 numbers on the host (``rotary_frequencies``).  Output row j of
+    request b, j < n[b], has place idx[b, j] (without ``idx`` place j) and is read from the row of that number, or from row j
+    (``src_compact``).  ``inverse`` turns the other way, which is the gradient of the rotation."""
+    torch = _torch()
+    at = _here()
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    try:
+        B, src, Hq, D = q.shape
+        Bp, places, axes = positions.shape
+        cap = q_out.shape[1]
+        Hk = 0 if k is None else k.shape[2]
+    except (AttributeError, ValueError, IndexError):
+        _ranks(q=(q, 4), positions=(positions, 3), q_out=(q_out, 4), **({} if k is None else dict(k=(k, 4))))
+        raise
+    if Bp != B and Bp != 1:
+        _want(positions, (B, places, axes), "positions")
+    if (k is None) != (k_out is None):
+        raise RegionEError("k and k_out are given together")
+    _want(q_out, (B, cap, Hq, D), "q_out")
+    if k is not None:
+        _want(k, (B, src, Hk, D), "k")
+        _want(k_out, (B, cap, Hk, D), "k_out")
+    if idx is not None:
+        _want(idx, (B, cap), "idx")
+    if n is not None:
+        _want(n, (B,), "n")
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None:
+            _want(t, (D,), name)
+            if eps is None:
+                raise RegionEError(f"{name} belongs to the normalisation, which eps asks for")
+    if len(freq) != D // 2 or len(axis) != D // 2:
+        raise RegionEError("freq and axis must have D / 2 entries")
+    compact = src_compact or idx is None
+    if src != (cap if compact else places) or (idx is None and cap > places):
+        raise RegionEError("source rows must match the rows to write (compact) or the places (gathered)")
+    rows = src
+    freq_c, axis_c = (c_double * len(freq))(*freq), (ctypes.c_int32 * len(axis))(*axis)
+    qp, kp = _heads(at, q, rows, "q"), (None, 0, 0) if k is None else _heads(at, k, rows, "k")
+    qo, ko = _heads(at, q_out, cap, "q_out"), (None, 0, 0) if k is None else _heads(at, k_out, cap, "k_out")
+    _check(load().regione_rotary_axes(
+        *qp, *kp, _on(at, idx, i32, "idx"), _on(at, n, i32, "n"), _on(at, positions, f32, "positions"),
+        0 if Bp == 1 else places * axes, B, places, cap, Hq, Hk, D, axes, 1 if compact else 0, freq_c, axis_c, int(layout),
+        1 if inverse else 0, 0 if eps is None else 1, _on(at, q_weight, bf, "q_weight"), _on(at, k_weight, bf, "k_weight"),
+        0.0 if eps is None else float(eps), *qo, *ko, _on(at, dev_status, i32, "dev_status"), _stream(stream)),
+        "regione_rotary_axes")
 
 
 def fresh_qkv(q_src, k_src, v_src, idx, n, q_weight, k_weight, eps, cos_table, sin_table, rope_layout,

@@ -1,0 +1,244 @@
+// Rotary positions with several axes for rows of Q and K (regione_rotary_axes), behind their per-head RMS normalisation, and the
+// rotation's gradient.
+//
+// The paper takes the attention layer of the editors as given.  Their tokens have places with several coordinates: which image (the
+// edited one, its reference, the text), which frame, which row and column; a request's own when the images of a batch are not alike,
+// and between whole numbers when an image was resized.  The method fixes that a recomputed token keeps its place (Sec. 4
+// "Region-Aware Generation"), so that the row list of a region step names the places as well as the rows.
+//
+//   y = x / sqrt(mean(x^2) + eps) * weight              over the D elements of a row and head (where asked for)
+//   t_i = position[axis_i] * freq_i                      for the D/2 pairs, (a, b) -> (a cos t - b sin t, a sin t + b cos t)
+//
+// Angles are formed here and not read from a table: frequency in turns as the sum of two fp32 numbers, the product with the position
+// exact in two parts, whole turns taken off before anything is rounded.  The angle is off by about 2^-24 turns however far the
+// position is (one fp32 product at position 10^5 is off by 2^-8 radians, as much as the bf16 output).
+//
+// Bound by device memory: 4 bytes an element.  A warp has a row, or a part of its heads where rows are few; its lanes form the angles
+// of the D/2 pairs once and leave them in shared memory, then go through the heads, 16 bytes a lane and four loads in flight.
+#include "common.cuh"
+
+#include <algorithm>
+#include <cmath>
+
+namespace regione {
+
+constexpr int kRotaryMaxD = 256, kRotaryWarps = 8, kRotaryAxes = 4, kRotaryAhead = 4;
+
+struct RotaryArgs {
+    const uint16_t *q, *k;                            // rows row_stride apart, requests batch_stride apart, heads of a row side by side
+    long long q_batch, q_row, k_batch, k_row;
+    uint16_t *q_out, *k_out;
+    long long q_out_batch, q_out_row, k_out_batch, k_out_row;
+    const int32_t *idx, *n;                           // [B, cap], [B], or NULL
+    const float* positions;                           // [B or 1, n_pos, axes]
+    long long positions_batch;
+    int B, n_pos, cap, Hq, Hk, D, axes;
+    int compact;                                      // row j is read; else row idx[b, j]
+    const uint16_t *q_weight, *k_weight;
+    float eps, sign;                                  // sign: -1 turns back
+    int parts;                                        // warps that share a row
+    int32_t* dev_status;
+    float turns_hi[kRotaryMaxD / 2], turns_lo[kRotaryMaxD / 2];
+    uint8_t axis[kRotaryMaxD / 2];
+};
+
+// LANES: a power of two, at least D / 8; lane g of a head has elements 8 g .. 8 g + 7.
+template <int LANES, bool HALF, bool NORM>
+__global__ void __launch_bounds__(kRotaryWarps * 32) rotary_axes_kernel(const __grid_constant__ RotaryArgs p) {
+    __shared__ __align__(16) float cos_of[kRotaryWarps][LANES * 4], sin_of[kRotaryWarps][LANES * 4];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    constexpr int kHeads = 32 / LANES;                // of a pass of the warp
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = blockIdx.y;
+    const int work = blockIdx.x * kRotaryWarps + warp, j = work / p.parts, part = work - j * p.parts;
+    int live = p.cap;
+    if (p.n != nullptr) {
+        live = p.n[b];
+        if (live < 0 || live > p.cap) {
+            if (work == 0 && lane == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+            live = live < 0 ? 0 : p.cap;
+        }
+    }
+    if (j >= live) return;
+    int place = j;
+    if (p.idx != nullptr) {
+        place = p.idx[(size_t)b * p.cap + j];
+        if (place < 0 || place >= p.n_pos) {
+            if (lane == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+            return;
+        }
+    }
+    const int g = lane & (LANES - 1), pieces = p.D / 8, pairs = p.D / 2;
+    const bool on = g < pieces;
+    const long long from = p.compact ? j : place;
+    const uint16_t* q = p.q + b * p.q_batch + from * p.q_row;
+    const uint16_t* k = p.k == nullptr ? nullptr : p.k + b * p.k_batch + from * p.k_row;
+    uint16_t* q_out = p.q_out + b * p.q_out_batch + j * p.q_out_row;
+    uint16_t* k_out = p.k == nullptr ? nullptr : p.k_out + b * p.k_out_batch + j * p.k_out_row;
+
+    // ---- angles ---------------------------------------------------------------------------------------------------------------
+    float at[kRotaryAxes];
+    const float* position = p.positions + b * p.positions_batch + (long long)place * p.axes;
+#pragma unroll
+    for (int a = 0; a < kRotaryAxes; ++a) at[a] = a < p.axes ? position[a] : 0.f;
+    for (int i = lane; i < pairs; i += 32) {
+        const int axis = p.axis[i];
+        const float x = axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
+        const float hi = p.turns_hi[i], whole = x * hi, rest = fmaf(x, p.turns_lo[i], fmaf(x, hi, -whole));
+        float s, c;
+        sincospif(2.0f * ((whole - rintf(whole)) + rest), &s, &c);
+        cos_of[warp][i] = c;
+        sin_of[warp][i] = s * p.sign;
+    }
+    __syncwarp();
+    constexpr int kAngles = HALF ? 8 : 4;
+    float cs[kAngles], sn[kAngles];
+    const bool second = HALF && 2 * g >= pieces;      // this lane's elements are the second ones of their pairs
+    {
+        const int first = !on ? 0 : HALF ? 8 * (second ? g - pieces / 2 : g) : 4 * g;
+#pragma unroll
+        for (int e = 0; e < kAngles; e += 4) {
+            const float4 c = *reinterpret_cast<const float4*>(&cos_of[warp][first + e]), s = *reinterpret_cast<const float4*>(&sin_of[warp][first + e]);
+            cs[e] = c.x; cs[e + 1] = c.y; cs[e + 2] = c.z; cs[e + 3] = c.w;
+            sn[e] = s.x; sn[e + 1] = s.y; sn[e + 2] = s.z; sn[e + 3] = s.w;
+        }
+        if (HALF && !second)
+#pragma unroll
+            for (int e = 0; e < kAngles; ++e) sn[e] = -sn[e];
+    }
+    const int partner = HALF ? (lane & ~(LANES - 1)) + (!on ? g : second ? g - pieces / 2 : g + pieces / 2) : 0;
+    const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+    uint4 wq = ones, wk = ones;
+    if (NORM && on) {
+        if (p.q_weight != nullptr) wq = ldg128(p.q_weight + 8 * g);
+        if (p.k_weight != nullptr) wk = ldg128(p.k_weight + 8 * g);
+    }
+    const float inv = 1.0f / p.D;
+
+    // ---- heads of Q, then of K: this part's share of the passes ------------------------------------------------------------------
+    const int heads = p.Hq + p.Hk, passes = (heads + kHeads - 1) / kHeads;
+    const int first_pass = (int)((long long)passes * part / p.parts), last_pass = (int)((long long)passes * (part + 1) / p.parts);
+    const int in_pass = lane / LANES;
+    for (int i0 = first_pass; i0 < last_pass; i0 += kRotaryAhead) {
+        uint4 w[kRotaryAhead];
+#pragma unroll
+        for (int u = 0; u < kRotaryAhead; ++u) {
+            const int h = (i0 + u) * kHeads + in_pass;
+            w[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (i0 + u < last_pass && on && h < heads) {
+                const uint16_t* src = h < p.Hq ? q + (long long)h * p.D : k + (long long)(h - p.Hq) * p.D;
+                // (not through the path of read-only data: the row may be turned in place)
+                asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(w[u].x), "=r"(w[u].y), "=r"(w[u].z), "=r"(w[u].w) : "l"(src + 8 * g));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kRotaryAhead; ++u) {
+            if (i0 + u >= last_pass) break;
+            const int h = (i0 + u) * kHeads + in_pass;
+            float y[8] = {bf16_lo(w[u].x), bf16_hi(w[u].x), bf16_lo(w[u].y), bf16_hi(w[u].y),
+                          bf16_lo(w[u].z), bf16_hi(w[u].z), bf16_lo(w[u].w), bf16_hi(w[u].w)}, o[8];
+            if constexpr (NORM) {
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+#pragma unroll
+                for (int d = LANES / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+                const float r = rsqrtf(fmaf(ss, inv, p.eps));
+                const uint4 v = h < p.Hq ? wq : wk;
+                const float m[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] *= r * m[e];
+            }
+            if constexpr (HALF) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = fmaf(__shfl_sync(0xffffffffu, y[e], partner), sn[e], y[e] * cs[e]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    o[2 * t] = fmaf(-y[2 * t + 1], sn[t], y[2 * t] * cs[t]);
+                    o[2 * t + 1] = fmaf(y[2 * t], sn[t], y[2 * t + 1] * cs[t]);
+                }
+            }
+            if (!on || h >= heads) continue;
+            uint16_t* dst = h < p.Hq ? q_out + (long long)h * p.D : k_out + (long long)(h - p.Hq) * p.D;
+            *reinterpret_cast<uint4*>(dst + 8 * g) =
+                make_uint4(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]), pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7]));
+        }
+    }
+}
+
+template <int LANES> static cudaError_t rotary_launch(const RotaryArgs& p, bool half, bool norm, dim3 grid, cudaStream_t st) {
+    const dim3 block(kRotaryWarps * 32);
+    if (half) return norm ? launch_overlapped(rotary_axes_kernel<LANES, true, true>, grid, block, 0, st, p)
+                          : launch_overlapped(rotary_axes_kernel<LANES, true, false>, grid, block, 0, st, p);
+    return norm ? launch_overlapped(rotary_axes_kernel<LANES, false, true>, grid, block, 0, st, p)
+                : launch_overlapped(rotary_axes_kernel<LANES, false, false>, grid, block, 0, st, p);
+}
+
+// Rows of [B, rows, H, D] with requests and rows apart.
+static int check_heads(const void* at, int H, int D, long long batch, long long row) {
+    if (!at || !aligned16(at) || row < (long long)H * D || batch < 0) return REGIONE_INVALID_ARG;
+    return row % 8 || batch % 8 || row > (1LL << 32) || batch > (1LL << 48) ? REGIONE_UNSUPPORTED : REGIONE_OK;
+}
+
+}  // namespace regione
+
+using namespace regione;
+
+extern "C" int regione_rotary_axes(const regione_bf16* q, int64_t q_batch, int64_t q_row, const regione_bf16* k, int64_t k_batch,
+                                   int64_t k_row, const int32_t* idx, const int32_t* n, const float* positions, int64_t positions_batch,
+                                   int B, int n_pos, int cap, int Hq, int Hk, int D, int axes, int src_compact, const double* freq,
+                                   const int32_t* axis, int rope_layout, int inverse, int normalise, const regione_bf16* q_weight,
+                                   const regione_bf16* k_weight, float eps, regione_bf16* q_out, int64_t q_out_batch,
+                                   int64_t q_out_row, regione_bf16* k_out, int64_t k_out_batch, int64_t k_out_row,
+                                   int32_t* dev_status, void* stream) {
+    if (!freq || !axis || B < 0 || n_pos < 0 || cap < 0 || Hq < 1 || Hk < 0 || D < 1 || axes < 1) return REGIONE_INVALID_ARG;
+    if ((k != nullptr) != (Hk > 0) || (k != nullptr) != (k_out != nullptr)) return REGIONE_INVALID_ARG;
+    if (rope_layout != REGIONE_ROPE_INTERLEAVED && rope_layout != REGIONE_ROPE_HALF) return REGIONE_INVALID_ARG;
+    if (normalise ? !(eps >= 0.f) : q_weight || k_weight) return REGIONE_INVALID_ARG;
+    if (inverse && normalise) return REGIONE_UNSUPPORTED;           // (the gradient of the rotation alone)
+    if (!aligned16(q_weight) || !aligned16(k_weight) || positions_batch < 0) return REGIONE_INVALID_ARG;
+    if (!idx && cap > n_pos) return REGIONE_INVALID_ARG;
+    if (D % 16 || D > kRotaryMaxD || axes > kRotaryAxes || Hq > 65536 || Hk > 65536 || B > 65535 || cap > (1 << 24) || n_pos > (1 << 28))
+        return REGIONE_UNSUPPORTED;
+    for (int i = 0; i < D / 2; ++i)
+        if (axis[i] < 0 || axis[i] >= axes || !std::isfinite(freq[i])) return REGIONE_INVALID_ARG;
+    if (B == 0 || cap == 0) return REGIONE_OK;
+    if (!positions) return REGIONE_INVALID_ARG;
+    int rc;
+    if ((rc = check_heads(q, Hq, D, q_batch, q_row)) != REGIONE_OK || (rc = check_heads(q_out, Hq, D, q_out_batch, q_out_row)) != REGIONE_OK) return rc;
+    if (k && ((rc = check_heads(k, Hk, D, k_batch, k_row)) != REGIONE_OK || (rc = check_heads(k_out, Hk, D, k_out_batch, k_out_row)) != REGIONE_OK)) return rc;
+    if (B > 1 && (q_out_batch == 0 || (k && k_out_batch == 0))) return REGIONE_INVALID_ARG;   // (requests would write the same rows)
+    RotaryArgs p = {};
+    p.q = q; p.k = k; p.q_batch = q_batch; p.q_row = q_row; p.k_batch = k_batch; p.k_row = k_row;
+    p.q_out = q_out; p.k_out = k_out; p.q_out_batch = q_out_batch; p.q_out_row = q_out_row; p.k_out_batch = k_out_batch; p.k_out_row = k_out_row;
+    p.idx = idx; p.n = n; p.positions = positions; p.positions_batch = positions_batch;
+    p.B = B; p.n_pos = n_pos; p.cap = cap; p.Hq = Hq; p.Hk = Hk; p.D = D; p.axes = axes; p.compact = src_compact || !idx;
+    p.q_weight = q_weight; p.k_weight = k_weight; p.eps = eps; p.sign = inverse ? -1.0f : 1.0f; p.dev_status = dev_status;
+    for (int i = 0; i < D / 2; ++i) {
+        const double turns = freq[i] * 0.15915494309189533576888;   // 1 / (2 pi)
+        p.turns_hi[i] = (float)turns;
+        p.turns_lo[i] = (float)(turns - (double)p.turns_hi[i]);
+        p.axis[i] = (uint8_t)axis[i];
+    }
+    int lanes = 2;
+    while (lanes < D / 8) lanes *= 2;
+    // Where rows are few their heads are dealt over several warps, until the GPU has some sixteen warps an SM.
+    const int passes = ((Hq + Hk) * lanes + 31) / 32;
+    const long long rows = (long long)B * cap;
+    p.parts = 1;
+    while (p.parts < passes && p.parts < 16 && rows * p.parts < 16LL * sm_count()) p.parts *= 2;
+    const long long blocks = ((long long)cap * p.parts + kRotaryWarps - 1) / kRotaryWarps;
+    const dim3 grid((unsigned)blocks, B);
+    const bool half = rope_layout == REGIONE_ROPE_HALF, norm = normalise != 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    switch (lanes) {
+        case 2: return launch_status(rotary_launch<2>(p, half, norm, grid, st));
+        case 4: return launch_status(rotary_launch<4>(p, half, norm, grid, st));
+        case 8: return launch_status(rotary_launch<8>(p, half, norm, grid, st));
+        case 16: return launch_status(rotary_launch<16>(p, half, norm, grid, st));
+        default: return launch_status(rotary_launch<32>(p, half, norm, grid, st));
+    }
+}
