@@ -691,3 +691,17 @@ def rotary_axes(x, positions, freq, axis, interleaved, weight=None, eps=None, in
     w = (y[..., first] + 1j * y[..., second]) * turn
     out[..., first], out[..., second] = w.real, w.imag
     return out
+
+
+def adapter_matmul(x, w, a, b, adapter, ranges, scale=None, bias=None, gelu=False):
+    """Rows of ``ranges`` times the weight set of their group with the group's low-rank adapter folded into it; zeros elsewhere."""
+    x = np.asarray(x, np.float64)
+    out = np.zeros((len(x), w.shape[1]))
+    for g, ((lo, hi), j) in enumerate(zip(ranges, adapter)):
+        i = g % len(w)
+        whole = np.asarray(w[i], np.float64)
+        if j >= 0:
+            whole = whole + (1.0 if scale is None else float(scale[j])) * (np.asarray(b[j], np.float64) @ np.asarray(a[j], np.float64))
+        y = x[lo:hi] @ whole.T + (0.0 if bias is None else np.asarray(bias[i], np.float64))
+        out[lo:hi] = y / (1.0 + np.exp(-2.0 * np.sqrt(2.0 / np.pi) * (y + 0.044715 * y ** 3))) if gelu else y
+    return out

@@ -68,6 +68,8 @@ SIGNATURES = {
     "regione_rikv_load_mxfp4": (c_int, [_P, _P, _P, _P, _P, c_int, c_int, c_int, c_int, _P, _P, _P, _P]),
     "regione_grouped_matmul": (c_int, [_P, c_int64, _P, _P, _P, _P] + [c_int] * 6 + [_P, c_int64, _P, _P]),
     "regione_mxfp4_grouped_matmul": (c_int, [_P] * 7 + [c_int] * 6 + [_P, c_int64, _P, _P]),
+    "regione_adapter_matmul_workspace": (c_size_t, [c_int] * 5),
+    "regione_adapter_matmul": (c_int, [_P, c_int64] + [_P] * 6 + [c_int, c_int, _P, _P] + [c_int] * 6 + [_P, c_int64, _P, c_size_t, _P, _P]),
     "regione_layer_norm": (c_int, [_P, c_int64, _P, c_int64, _P, _P, _P, c_int64, c_int, c_float, _P, _P] + [c_int] * 4 +
                            [_P, c_int64, _P, c_int64, _P, _P, _P, _P]),
     "regione_layer_norm_backward_workspace": (c_size_t, [c_int] * 3),
@@ -541,6 +543,57 @@ def mxfp4_grouped_matmul(x_q, x_scale, w_q, w_scale, row_begin, row_end, out, bi
         _stream(stream)), "regione_mxfp4_grouped_matmul")
 
 
+def adapter_matmul_workspace(rows, groups, K, N, rank) -> int:
+    return int(load().regione_adapter_matmul_workspace(rows, groups, K, N, rank))
+
+
+def adapter_matmul(x, w, a, b, adapter, row_begin, row_end, out, workspace, scale=None, bias=None, activation=ACT_NONE,
+                   dev_status=None, stream=None):
+    """``grouped_matmul`` with the low-rank adapter of each group beside the shared weights: out[r] = act(x[r] @ w[i].T + bias[i] +
+    scale[j] * (x[r] @ a[j].T) @ b[j].T), j = adapter[g], no adapter where it is -1.  ``a`` [adapters, rank, K], ``b``
+    [adapters, N, rank], ``scale`` [adapters] fp32 or None (1), ``adapter`` [groups] on the device."""
+    torch = _torch()
+    at = _here()
+    bf, i32 = torch.bfloat16, torch.int32
+    try:
+        rows, K = shape = x.shape
+        sets, N, k = w.shape
+        count, rank, ka = a.shape
+        fits = (k == K and ka == K and b.shape == (count, N, rank) and adapter.shape == row_begin.shape == row_end.shape and
+                (bias is None or bias.shape == (sets, N)) and (scale is None or scale.shape == (count,)))
+    except (AttributeError, ValueError, IndexError):
+        _ranks(x=(x, 2), w=(w, 3), a=(a, 3), b=(b, 3), adapter=(adapter, None), row_begin=(row_begin, None), row_end=(row_end, None),
+               **{name: (t, None) for name, t in (("bias", bias), ("scale", scale)) if t is not None})
+        raise
+    if not fits:
+        _want(w, (sets, N, K), "w")
+        _want(a, (count, rank, K), "a")
+        _want(b, (count, N, rank), "b")
+        _want(row_end, row_begin.shape, "row_end")
+        _want(adapter, row_begin.shape, "adapter")
+        if bias is not None:
+            _want(bias, (sets, N), "bias")
+        if scale is not None:
+            _want(scale, (count,), "scale")
+    xp, xs = _rows(at, x, shape, bf, "x")
+    op, os_ = _rows(at, out, (rows, N), bf, "out")
+    wp, ws_bytes = _workspace(at, workspace)
+    _check(load().regione_adapter_matmul(
+        xp, xs, _on(at, w, bf, "w"), _on(at, bias, bf, "bias"), _on(at, a, bf, "a"), _on(at, b, bf, "b"),
+        _on(at, scale, torch.float32, "scale"), _on(at, adapter, i32, "adapter"), count, rank, _on(at, row_begin, i32, "row_begin"),
+        _on(at, row_end, i32, "row_end"), rows, row_begin.numel(), sets, K, N, activation, op, os_, wp, ws_bytes,
+        _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_adapter_matmul")
+
+
+def _workspace(device, t):
+    """Address and bytes of a workspace."""
+    if t is None:
+        return None, 0
+    if not isinstance(getattr(t, "shape", None), _torch().Size):
+        raise RegionEError("workspace must be a CUDA tensor")
+    return _on(device, t, t.dtype, "workspace"), t.nbytes
+
+
 def _sets(device, tensors, C):
     """Sets and set distance of the parameters [sets, C] that are given, which have to lie alike, and their addresses."""
     bf = _torch().bfloat16
@@ -627,14 +680,14 @@ def layer_norm_backward(x, mean, rstd, dy, weight, row_begin, row_end, dx, dweig
         if t is not None:
             _want(t, (sets, C), name)
     rows_of = lambda t, name: (None, 0) if t is None else _rows(at, t, shape, bf, name)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ws, ws_bytes = _workspace(at, workspace)
     _check(load().regione_layer_norm_backward(
         *_rows(at, x, shape, bf, "x"), _on(at, mean, f32, "mean"), _on(at, rstd, f32, "rstd"), *_rows(at, dy, shape, bf, "dy"),
         *rows_of(dx_out, "dx_out"), *rows_of(residual, "residual"), gp, wp, step, 1 if modulated else 0,
         _on(at, row_begin, i32, "row_begin"), _on(at, row_end, i32, "row_end"), rows, row_begin.numel(), sets, C,
         *_rows(at, dx, shape, bf, "dx"), *rows_of(dresidual, "dresidual"), _on(at, dweight, f32, "dweight"),
-        _on(at, dbias, f32, "dbias"), _on(at, dgate, f32, "dgate"), _on(at, workspace, getattr(workspace, "dtype", None), "workspace"),
-        ws_bytes, _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_layer_norm_backward")
+        _on(at, dbias, f32, "dbias"), _on(at, dgate, f32, "dgate"), ws, ws_bytes,
+        _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_layer_norm_backward")
 
 
 def rotary_frequencies(widths, theta=10000.0):

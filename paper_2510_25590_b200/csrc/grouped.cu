@@ -22,11 +22,13 @@
 // What bounds them: bf16 the tensor core; 4 bits, whose operands last a quarter as long, the way from L2 into the SMs (30 KB a
 // chunk in 400 ns of which the products are 272), and with K below 4096 the sums' way out; few rows the weights' way from
 // device memory (64 experts of 2048 x 1408 with 4096 rows: 70 us, 62 at the copy rate).
+#include "adapters.cuh"
 #include "common.cuh"
 #include "grouped_plan.cuh"
 #include "sm100_ptx.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace regione {
 
@@ -59,12 +61,30 @@ struct GroupedArgs {
     long long out_stride;
     const uint8_t *x_scale, *w_scale;                 // [rows_cap, K / 32], [n_weights, N, K / 32]
     int32_t* dev_status;
+    // low-rank adapters (see Product)
+    const int32_t* adapter;                           // [groups], -1: none
+    int n_adapters, rank, tail;                       // tail: chunks of the rank behind those of K
+    const float* adapter_scale;                       // [n_adapters] or NULL
+    const float* addend;                              // [rows_cap, N]
 };
+
+// What a launch multiplies.  kPlain: rows with the weight set of their group.  The others are the parts of a product with low-rank
+// adapters beside it:
+//   kInto    u = s_a x A_a^T, the adapter of the group in place of the weight set; rows of groups without one are left out
+//   kTail    rows with the weight set, and behind the chunks of K those of the rank: u with B_a, into the same accumulators
+//   kJoined  rows with the weight set plus an fp32 row that the adapters' sums are already in; groups of a set whose ranges touch are one
+//            range, so that many groups of a row or two share the tiles, and the weights are read once
+enum class Product { kPlain, kInto, kTail, kJoined };
 struct GroupedMaps {
     CUtensorMap w;                                    // (K, N, n_weights), box 128 bytes x 128 rows
     CUtensorMap x[kMaps];                             // (K, rows), box 128 bytes x 16 << i rows
     CUtensorMap out;                                  // (N, rows), box 32 features x 16 rows
 };
+struct TailMaps : GroupedMaps {
+    CUtensorMap b;                                    // (rank, N, n_adapters), box 128 bytes x 128 rows
+    CUtensorMap u[kMaps];                             // (rank, rows), box 128 bytes x 16 << i rows
+};
+template <Product OP> using MapsOf = std::conditional_t<OP == Product::kTail, TailMaps, GroupedMaps>;
 
 struct GroupedControl {
     uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
@@ -293,15 +313,23 @@ __device__ __forceinline__ bool rows_of(const GroupedArgs& p, int g, int& begin,
     return cut_range(p.row_begin[g], p.row_end[g], p.rows_cap, begin, rows);
 }
 
+// A group's adapter, -1 for none; one that does not exist is none (`in`: false).
+__device__ __forceinline__ int adapter_of(const GroupedArgs& p, int g, bool& in) {
+    const int a = __ldg(p.adapter + g);
+    in = a >= -1 && a < p.n_adapters;
+    return in ? a : -1;
+}
+
 // Rows [first, first + live) of a group against a feature tile; `width` = columns of the product.
 struct GroupedTile {
     int first, live, width, weights, feature;
+    int adapter;                                      // kTail, and with kInto the weight set
 };
 
 // Tile t of the plan, t not smaller than at the last call; `group` is where that one was.  Tiles of a group run through eight feature
 // tiles before they go on to the next rows, so that the tiles in flight at one time share both operands.  PAIR: 256 features,
 // widths in steps of 32.
-template <bool PAIR>
+template <bool PAIR, Product OP = Product::kPlain>
 __device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const GroupedControl* ctl, int t, int f_tiles, int& group) {
     while (ctl->first[group + 1] * f_tiles <= t) ++group;
     const int ahead = ctl->first[group], n = ctl->first[group + 1] - ahead, width = ctl->widths[group];
@@ -317,7 +345,42 @@ __device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const Group
     tile.width = width;
     tile.weights = group < p.n_weights ? group : group % p.n_weights;
     tile.feature = (block * 8 + in - at * wide) * (PAIR ? 2 : 1) * kFeat;
+    tile.adapter = -1;
+    if constexpr (OP == Product::kInto || OP == Product::kTail) {
+        bool exists;
+        tile.adapter = adapter_of(p, group, exists);
+        if (OP == Product::kInto) tile.weights = max(tile.adapter, 0);
+    }
     return tile;
+}
+
+// kJoined: groups of a weight set, in their order, whose ranges touch become one, at the place of the first; the others have no rows.  The
+// last one of a range is found by following links of twice the length in every round.  (All threads; ends with a barrier.)
+__device__ __forceinline__ void join_groups(const GroupedArgs& p, GroupedControl* ctl) {
+    int16_t* last = ctl->widths;
+    bool in = true;
+    for (int g = threadIdx.x; g < p.groups; g += blockDim.x) in = rows_of(p, g, ctl->begin[g], ctl->rows[g]) && in;
+    if (!in && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+    __syncthreads();
+    auto joins = [&](int g) {                         // group g to the set's next one
+        return g + p.n_weights < p.groups && ctl->begin[g] + ctl->rows[g] == ctl->begin[g + p.n_weights];
+    };
+    for (int g = threadIdx.x; g < p.groups; g += blockDim.x) last[g] = (int16_t)(joins(g) ? g + p.n_weights : g);
+    __syncthreads();
+    constexpr int kEach = (kMaxGroups + 191) / 192;   // of a thread (a CTA has 192 at least)
+    for (int reach = p.n_weights; reach < p.groups; reach *= 2) {
+        int16_t further[kEach];
+        for (int i = 0, g = threadIdx.x; i < kEach && g < p.groups; ++i, g += blockDim.x) further[i] = last[last[g]];
+        __syncthreads();
+        for (int i = 0, g = threadIdx.x; i < kEach && g < p.groups; ++i, g += blockDim.x) last[g] = further[i];
+        __syncthreads();
+    }
+    int rows[kEach];
+    for (int i = 0, g = threadIdx.x; i < kEach && g < p.groups; ++i, g += blockDim.x)
+        rows[i] = g >= p.n_weights && joins(g - p.n_weights) ? 0 : ctl->begin[last[g]] + ctl->rows[last[g]] - ctl->begin[g];
+    __syncthreads();
+    for (int i = 0, g = threadIdx.x; i < kEach && g < p.groups; ++i, g += blockDim.x) ctl->rows[g] = rows[i];
+    __syncthreads();
 }
 
 // Scales of the tiles [t0, t_end): 8 bytes a row and chunk, from rows that lie K / 32 bytes apart to the places in shared memory that
@@ -426,9 +489,10 @@ __device__ __forceinline__ bool bring_scales(const GroupedArgs& p, const ScaleRo
 }
 
 // VEC: of 4-bit operands, K is a multiple of 512 (see bring_scales).
-template <bool FP4, bool PAIR, bool VEC>
+template <bool FP4, bool PAIR, bool VEC, Product OP = Product::kPlain>
 __global__ void __launch_bounds__(Roles<FP4, PAIR>::kThreads, PAIR ? 1 : 2)
-grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__ GroupedArgs p) {
+grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ GroupedArgs p) {
+    static_assert(!FP4 || OP == Product::kPlain, "adapters are in bf16");
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     constexpr int kElems = FP4 ? 256 : 64;            // of K in a chunk
     constexpr int kMaxWidth = PAIR ? (FP4 ? 224 : 256) : 128;
@@ -465,9 +529,26 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     // ---- plan: from the groups' row counts, which only the device knows --------------------------------------------
     const int f_tiles = (p.N + (PAIR ? 2 : 1) * kFeat - 1) / ((PAIR ? 2 : 1) * kFeat);
     const int workers = gridDim.x / cluster;
+    if constexpr (OP == Product::kJoined) join_groups(p, ctl);
+    // A group's rows as the plan takes them; false: not a range of the buffer, or not an adapter.
+    auto range = [&](int g, int& begin, int& rows) {
+        if constexpr (OP == Product::kJoined) {
+            begin = ctl->begin[g];
+            rows = ctl->rows[g];
+            return true;
+        } else {
+            bool in = rows_of(p, g, begin, rows);
+            if constexpr (OP == Product::kInto) {
+                bool exists;
+                if (adapter_of(p, g, exists) < 0) rows = 0;
+                in = in && exists;
+            }
+            return in;
+        }
+    };
     int own_begin = 0, own_rows = 0;                  // of group `lane`: read once, 800 cycles
     bool own_in = true;
-    if (warp < (PAIR ? kMaxWidth / 32 : 1) && lane < p.groups) own_in = rows_of(p, lane, own_begin, own_rows);
+    if (warp < (PAIR ? kMaxWidth / 32 : 1) && lane < p.groups) own_in = range(lane, own_begin, own_rows);
     if constexpr (PAIR) {
         // Widths of 32 .. 256 (224) rows: one warp adds up the tiles of one width.  A chunk of a tile takes the tensor core 2 cycles a row;
         // its 128 + width / 2 rows of 128 bytes arrive at about 57 bytes a cycle.  The width with the cheapest rounds of tiles is
@@ -477,7 +558,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             int n = (own_rows + width - 1) / width;
             for (int g = lane + 32; g < p.groups; g += 32) {
                 int begin, rows;
-                rows_of(p, g, begin, rows);
+                range(g, begin, rows);
                 n += (rows + width - 1) / width;
             }
             n = min(__reduce_add_sync(0xffffffffu, n), p.rows_cap / width + p.groups);
@@ -503,7 +584,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             if (g < p.groups) {
                 int begin = own_begin, rows = own_rows;
                 bool in = own_in;
-                if (g0 > 0) in = rows_of(p, g, begin, rows);
+                if (g0 > 0) in = range(g, begin, rows);
                 if (!in && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
                 n = (rows + width - 1) / width;
                 ctl->begin[g] = begin;
@@ -551,6 +632,10 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     const bool elected = ptx::elect_one();
     const uint32_t pair_mask = 3u << (rank & ~1);     // of the cluster's CTAs
     constexpr int kAccs = PAIR ? 2 : 1;
+    // The chunk behind the last one of a tile: the last slice takes those of the rank, where the tile's group has an adapter.
+    auto chunks_end = [&](const GroupedTile& tile) {
+        return OP == Product::kTail && tile.adapter >= 0 && c_end == p.chunks ? c_end + p.tail : c_end;
+    };
 
     // A cluster goes through its tiles without a stop; where slices meet, one tile at a time.
     for (long long t0 = worker; t0 < total; t0 += split ? workers : total) {
@@ -558,16 +643,31 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         if (warp == kProducer) {
             if (elected) {
                 for (long long t = t0; t < t_end && ok; t += workers) {
-                    const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
+                    const GroupedTile tile = tile_at<PAIR, OP>(p, ctl, (int)t, f_tiles, group);
+                    const int c_last = chunks_end(tile);
                     const int rows = PAIR ? tile.width / 2 : tile.width;                     // of x, for this CTA
                     const uint32_t bytes = (kTileBytes + rows * kChunkBytes) * (PAIR ? 2 : 1);
                     const int feature = tile.feature + half * kFeat, row = tile.first + half * rows;
-                    for (int c = c_begin; c < c_end; ++c) {
+                    for (int c = c_begin; c < c_last; ++c) {
                         if (!grouped_wait(ptx::smem_addr(&ctl->empty[s]), phase ^ 1, ctl, p.dev_status)) { ok = false; break; }
                         if (leader) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&ctl->full[s]), bytes);
                         const uint32_t bar = bar_at(&ctl->full[s]), dst = smem + s * stage_bytes;
-                        load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
                         int at = 0;                                                  // boxes that make up the rows, the largest first
+                        if constexpr (OP == Product::kTail) {
+                            if (c >= p.chunks) {
+                                const int j = (c - p.chunks) * kElems;
+                                load_w<PAIR>(dst, &maps.b, bar, j, feature, tile.adapter);
+#pragma unroll
+                                for (int box = kMaps - 1; box >= 0; --box)
+                                    if (rows & (16 << box)) {
+                                        load_x<PAIR>(dst + kTileBytes + at * kChunkBytes, &maps.u[box], bar, j, row + at);
+                                        at += 16 << box;
+                                    }
+                                if (++s == stages) { s = 0; phase ^= 1; }
+                                continue;
+                            }
+                        }
+                        load_w<PAIR>(dst, &maps.w, bar, c * (FP4 ? kChunkBytes : kElems), feature, tile.weights);
 #pragma unroll
                         for (int box = kMaps - 1; box >= 0; --box)
                             if (rows & (16 << box)) {
@@ -583,7 +683,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 constexpr uint32_t hi = ptx::smem_desc_hi_sw128(1024);              // 8-row groups 1024 bytes apart
                 constexpr uint32_t hi_plain = (128u >> 4) | (1u << 14);             // scales: no swizzle, 8 rows of 16 bytes
                 for (long long t = t0; t < t_end && ok; t += workers, ++it) {
-                    const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
+                    const GroupedTile tile = tile_at<PAIR, OP>(p, ctl, (int)t, f_tiles, group);
+                    const int c_last = chunks_end(tile);
                     const int a = it % kAccs, use = it / kAccs;
                     const uint32_t d = tmem + (a ? kAcc1 : 0);
                     if (use > 0 && !grouped_wait<PAIR>(ptx::smem_addr(&ctl->acc_empty[a]), (use - 1) & 1, ctl, p.dev_status)) { ok = false; break; }
@@ -593,7 +694,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                                                      ((PAIR ? 2u : 1u) << 27)
                                                : ptx::idesc_bf16_f32(PAIR ? 256 : 128, tile.width, false);
                     uint32_t accumulate = 0;
-                    for (int c = c_begin; c < c_end; ++c) {
+                    for (int c = c_begin; c < c_last; ++c) {
                         if (!grouped_wait<PAIR && FP4>(ptx::smem_addr(&ctl->full[s]), phase, ctl, p.dev_status)) { ok = false; break; }
                         ptx::tc_fence_after_sync();
                         const uint32_t at = smem + s * stage_bytes;
@@ -612,7 +713,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                             }
                         }
                         // 32 bytes of K to an instruction; what lies behind K is zero and left out
-                        const int left = (p.K - c * kElems + kElems / 4 - 1) / (kElems / 4);
+                        const int behind = OP == Product::kTail && c >= p.chunks ? p.rank - (c - p.chunks) * kElems : p.K - c * kElems;
+                        const int left = (behind + kElems / 4 - 1) / (kElems / 4);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             if (k >= left) break;
@@ -640,7 +742,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             const int sub = warp & 3, part = warp >> 2;
             const uint32_t stage = ptx::smem_addr(staging) + warp * kStagingBytes;
             for (long long t = t0; t < t_end; t += workers, ++it) {
-                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t, f_tiles, group);
+                const GroupedTile tile = tile_at<PAIR, OP>(p, ctl, (int)t, f_tiles, group);
                 const int a = it % kAccs, use = it / kAccs;
                 const int feature = tile.feature + half * kFeat + 32 * sub;
                 uint64_t bias[4] = {0, 0, 0, 0};          // of features lane / 4 + {0, 8, 16, 24}, twice each
@@ -651,6 +753,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         const float b = __uint_as_float((uint32_t)__ldg(p.bias + (size_t)tile.weights * p.N + f) << 16);
                         bias[i] = pair_of(b, b);
                     }
+                const float scale = OP == Product::kInto && p.adapter_scale != nullptr ? __ldg(p.adapter_scale + tile.weights) : 1.0f;
                 if (!__all_sync(0xffffffffu, grouped_wait(ptx::smem_addr(&ctl->acc_full[a]), use & 1, ctl, p.dev_status)))
                     break;
                 ptx::tc_fence_after_sync();
@@ -680,6 +783,17 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         for (int i = 0; i < 8; ++i)
                             y[i] = add2(pair_of(__uint_as_float(ahead[2 * i]), __uint_as_float(ahead[2 * i + 1])), bias[(i >> 2) * 2 + (i & 1)]);
                         if (c + kEpiCols < tile.live) fetch(c + kEpiCols);
+                        if constexpr (OP == Product::kInto)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) y[i] = mul2(y[i], pair_of(scale, scale));
+                        if constexpr (OP == Product::kJoined)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                // (as the sums lie: rows 2 (l % 4) + {0, 1} of eight, features l / 4 of eight)
+                                const int q = c + 8 * ((i >> 1) & 1) + 2 * (lane & 3), f = feature + (lane >> 2) + 8 * ((i >> 2) * 2 + (i & 1));
+                                const float* from = p.addend + (size_t)(tile.first + q) * p.N + f;
+                                y[i] = add2(y[i], pair_of(f < p.N && q < tile.live ? from[0] : 0.f, f < p.N && q + 1 < tile.live ? from[p.N] : 0.f));
+                            }
                         if (p.activation == REGIONE_ACT_GELU_TANH) gelu_tanh(y);
                         uint32_t z[8];
 #pragma unroll
@@ -724,7 +838,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         if (split) {
             ptx::cluster_sync();
             if (warp < kEpiWarps && !ctl->abort_flag) {
-                const GroupedTile tile = tile_at<PAIR>(p, ctl, (int)t0, f_tiles, group);
+                const GroupedTile tile = tile_at<PAIR, OP>(p, ctl, (int)t0, f_tiles, group);
+                const float scale = OP == Product::kInto && p.adapter_scale != nullptr ? __ldg(p.adapter_scale + tile.weights) : 1.0f;
                 // pieces of 8 features of a row, dealt over the slices' threads; slices are added in their order
                 for (int u = threadIdx.x * p.slices + slice; u < tile.live * (kFeat / 8); u += kEpiWarps * 32 * p.slices) {
                     const int q = u / (kFeat / 8), j = u % (kFeat / 8), f = tile.feature + half * kFeat + 8 * j;
@@ -753,6 +868,15 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         const uint4 b = ldg128(p.bias + (size_t)tile.weights * p.N + f);
                         y[0] += bf16_lo(b.x); y[1] += bf16_hi(b.x); y[2] += bf16_lo(b.y); y[3] += bf16_hi(b.y);
                         y[4] += bf16_lo(b.z); y[5] += bf16_hi(b.z); y[6] += bf16_lo(b.w); y[7] += bf16_hi(b.w);
+                    }
+                    if constexpr (OP == Product::kInto)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] *= scale;
+                    if constexpr (OP == Product::kJoined) {
+                        const float4* from = reinterpret_cast<const float4*>(p.addend + (size_t)(tile.first + q) * p.N + f);
+                        const float4 lo = from[0], hi = from[1];
+                        y[0] += lo.x; y[1] += lo.y; y[2] += lo.z; y[3] += lo.w;
+                        y[4] += hi.x; y[5] += hi.y; y[6] += hi.z; y[7] += hi.w;
                     }
                     if (p.activation == REGIONE_ACT_GELU_TANH) {
                         uint64_t z[4] = {pair_of(y[0], y[1]), pair_of(y[2], y[3]), pair_of(y[4], y[5]), pair_of(y[6], y[7])};
@@ -866,20 +990,20 @@ template <bool FP4, bool PAIR> static void grouped_config(cudaLaunchConfig_t& cf
 }
 
 // Clusters of pairs that the device holds at one time, by their slices of K (1, 2, 4); 0 where the kernel cannot be set up.
-template <bool FP4, bool VEC> static const int* grouped_pairs(int dev) {
+template <bool FP4, bool VEC, Product OP> static const int* grouped_pairs(int dev) {
     static int held[kMaxDevices][4] = {};
     int* h = held[dev];
     if (__atomic_load_n(&h[3], __ATOMIC_ACQUIRE)) return h;
     const size_t smem = grouped_smem<FP4, true>(grouped_ring<FP4, true>(kSmemCta));
-    if (cudaFuncSetAttribute(grouped_kernel<FP4, true, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess ||
-        cudaFuncSetAttribute(grouped_kernel<FP4, false, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess)
+    if (cudaFuncSetAttribute(grouped_kernel<FP4, true, VEC, OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess ||
+        cudaFuncSetAttribute(grouped_kernel<FP4, false, VEC, OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess)
         return nullptr;
     for (int i = 0; i < 3; ++i) {
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attr[2];
         grouped_config<FP4, true>(cfg, attr, 2u << i, 2 << i, smem, nullptr);
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, grouped_kernel<FP4, true, VEC>, &cfg) != cudaSuccess) {
+        if (cudaOccupancyMaxActiveClusters(&n, grouped_kernel<FP4, true, VEC, OP>, &cfg) != cudaSuccess) {
             cudaGetLastError();
             n = 0;
         }
@@ -889,23 +1013,26 @@ template <bool FP4, bool VEC> static const int* grouped_pairs(int dev) {
     return h;
 }
 
-template <bool FP4, bool PAIR, bool VEC>
-static int grouped_launch(const GroupedMaps& maps, const GroupedArgs& p, int clusters, cudaStream_t st) {
+template <bool FP4, bool PAIR, bool VEC, Product OP>
+static int grouped_launch(const MapsOf<OP>& maps, const GroupedArgs& p, int clusters, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     const int cluster = (PAIR ? 2 : 1) * p.slices;
     grouped_config<FP4, PAIR>(cfg, attr, (unsigned)(clusters * cluster), cluster, grouped_smem<FP4, PAIR>(p.ring_bytes), st);
-    return launch_status(launch_counted(&cfg, grouped_kernel<FP4, PAIR, VEC>, maps, p));
+    return launch_status(launch_counted(&cfg, grouped_kernel<FP4, PAIR, VEC, OP>, maps, p));
 }
 
-template <bool FP4, bool VEC>
-static int grouped_run(const void* x, long long x_row_bytes, const void* w, GroupedArgs p, cudaStream_t st) {
+// `b`, `u`: the adapters' second factors [n_adapters, N, rank] and the rows' products with the first [rows_cap, rank] (kTail).
+template <bool FP4, bool VEC, Product OP = Product::kPlain>
+static int grouped_run(const void* x, long long x_row_bytes, const void* w, GroupedArgs p, cudaStream_t st, const void* b = nullptr,
+                       const void* u = nullptr) {
     constexpr int kElems = FP4 ? 256 : 64;
     const int dev = current_device(), sms = sm_count();
-    const int* held = dev < 0 ? nullptr : grouped_pairs<FP4, VEC>(dev);
+    const int* held = dev < 0 ? nullptr : grouped_pairs<FP4, VEC, OP>(dev);
     if (!held) return REGIONE_CUDA_ERROR;
     p.chunks = (p.K + kElems - 1) / kElems;
-    const int groups = std::min(p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
+    // (joined groups: as if all of a set were)
+    const int groups = std::min(OP == Product::kJoined ? std::min(p.groups, p.n_weights) : p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
     const int f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
     // What the launch will take, in ns, if every row of the buffer is live and the groups are alike (1280 live rows in a buffer of 8704, K 2048,
     // N 6144: as long as in one of 1280; 205 in 2304 19.4 us, in 205 17.4): what a launch takes before and behind its tiles, and rounds of tiles, each the chunks of a slice times what a chunk takes (no less than 200 by latency; 105 bytes
@@ -958,10 +1085,16 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
         p.scale_column = p.width <= 64 ? 64 : 128;
         p.tmem_columns = FP4 ? 2 * p.scale_column : std::max(32, p.width);
     }
-    GroupedMaps maps;
-    bool ok = grouped_map(&maps.w, FP4, 3, w, p.K, p.N, p.n_weights, FP4 ? p.K / 2 : 2LL * p.K, 128);
+    MapsOf<OP> maps;
+    bool ok = grouped_map(&maps.w, FP4, 3, w, p.K, p.N, OP == Product::kInto ? p.n_adapters : p.n_weights, FP4 ? p.K / 2 : 2LL * p.K, 128);
     for (int i = 0; i < kMaps && ok && (pair || (16 << i) <= p.width); ++i)
         ok = grouped_map(&maps.x[i], FP4, 2, x, p.K, p.rows_cap, 1, x_row_bytes, 16 << i);
+    if constexpr (OP == Product::kTail) {
+        p.tail = (p.rank + kElems - 1) / kElems;
+        ok = ok && grouped_map(&maps.b, false, 3, b, p.rank, p.N, p.n_adapters, 2LL * p.rank, 128);
+        for (int i = 0; i < kMaps && ok && (pair || (16 << i) <= p.width); ++i)
+            ok = grouped_map(&maps.u[i], false, 2, u, p.rank, p.rows_cap, 1, 2LL * p.rank, 16 << i);
+    }
     if (ok && pair) {
         const cuuint64_t dims[2] = {(cuuint64_t)p.N, (cuuint64_t)p.rows_cap}, strides[1] = {(cuuint64_t)(2 * p.out_stride)};
         const cuuint32_t box[2] = {32u, 16u}, ones[2] = {1u, 1u};
@@ -970,15 +1103,39 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     }
     if (!ok) return REGIONE_CUDA_ERROR;
-    return pair ? grouped_launch<FP4, true, VEC>(maps, p, clusters, st) : grouped_launch<FP4, false, VEC>(maps, p, clusters, st);
+    return pair ? grouped_launch<FP4, true, VEC, OP>(maps, p, clusters, st) : grouped_launch<FP4, false, VEC, OP>(maps, p, clusters, st);
+}
+
+static GroupedArgs adapter_args(const AdapterCall& c) {
+    GroupedArgs p = {};
+    p.row_begin = c.row_begin; p.row_end = c.row_end; p.groups = c.groups; p.n_weights = c.n_weights; p.rows_cap = c.rows_cap;
+    p.K = c.K; p.N = c.N; p.bias = c.bias; p.activation = c.activation; p.out = c.out; p.out_stride = c.out_stride; p.dev_status = c.dev_status;
+    p.adapter = c.adapter; p.n_adapters = c.n_adapters; p.rank = c.rank; p.adapter_scale = c.scale;
+    return p;
+}
+
+int adapters_into(const AdapterCall& c, uint16_t* u, cudaStream_t st) {
+    GroupedArgs p = adapter_args(c);
+    p.N = c.rank; p.bias = nullptr; p.activation = REGIONE_ACT_NONE; p.out = u; p.out_stride = c.rank;
+    return grouped_run<false, false, Product::kInto>(c.x, 2 * c.x_stride, c.a, p, st);
+}
+
+int adapters_tail(const AdapterCall& c, const uint16_t* u, cudaStream_t st) {
+    return grouped_run<false, false, Product::kTail>(c.x, 2 * c.x_stride, c.w, adapter_args(c), st, c.b, u);
+}
+
+int adapters_joined(const AdapterCall& c, const float* addend, cudaStream_t st) {
+    GroupedArgs p = adapter_args(c);
+    p.addend = addend;
+    return grouped_run<false, false, Product::kJoined>(c.x, 2 * c.x_stride, c.w, p, st);
 }
 
 }  // namespace regione
 
 using namespace regione;
 
-static int check_grouped(const void* x, const void* w, const void* bias, const void* begin, const void* end, int rows_cap, int groups,
-                         int n_weights, int K, int N, int activation, const void* out, long long out_stride) {
+int regione::check_grouped(const void* x, const void* w, const void* bias, const void* begin, const void* end, int rows_cap, int groups,
+                           int n_weights, int K, int N, int activation, const void* out, long long out_stride) {
     if (!w || (rows_cap && (!x || !out)) || (groups && (!begin || !end))) return REGIONE_INVALID_ARG;
     if (rows_cap < 0 || groups < 0 || n_weights < 1 || K < 1 || N < 1) return REGIONE_INVALID_ARG;
     if (activation != REGIONE_ACT_NONE && activation != REGIONE_ACT_GELU_TANH) return REGIONE_INVALID_ARG;
