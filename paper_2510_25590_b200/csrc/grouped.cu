@@ -24,6 +24,7 @@
 // device memory (64 experts of 2048 x 1408 with 4096 rows: 70 us, 62 at the copy rate).
 #include "adapters.cuh"
 #include "common.cuh"
+#include "f32x2.cuh"
 #include "grouped_plan.cuh"
 #include "sm100_ptx.cuh"
 
@@ -232,29 +233,6 @@ template <bool FAR = false>
 __device__ __forceinline__ bool grouped_wait(uint32_t bar, uint32_t parity, GroupedControl* ctl, int32_t* dev_status,
                                              long long limit = kGroupedWait) {
     return try_wait<FAR>(bar, parity) || grouped_wait_slow<FAR>(bar, parity, &ctl->abort_flag, dev_status, limit);
-}
-
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ uint64_t pair_of(float x, float y) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void parts_of(uint64_t p, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
 }
 
 __device__ __forceinline__ float min_or_nan(float x, float y, float z) {

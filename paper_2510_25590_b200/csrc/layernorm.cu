@@ -18,6 +18,7 @@
 // registers; two sums a row cross the block (one barrier), the next row's loads are on their way meanwhile.  Where a share
 // passes from one group to the next the sums go to a slot of the workspace, and a second kernel adds the slots of a set in the
 // order of the rows: results do not depend on timing.  All arithmetic in fp32.
+#include "f32x2.cuh"
 #include "row_groups.cuh"
 
 #include <algorithm>
@@ -59,13 +60,6 @@ __device__ __forceinline__ uint4 ld_once128(const void* p) {
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
     return r;
 }
-__device__ __forceinline__ void widen8(const uint4& w, float (&x)[8]) {
-    x[0] = bf16_lo(w.x); x[1] = bf16_hi(w.x); x[2] = bf16_lo(w.y); x[3] = bf16_hi(w.y);
-    x[4] = bf16_lo(w.z); x[5] = bf16_hi(w.z); x[6] = bf16_lo(w.w); x[7] = bf16_hi(w.w);
-}
-__device__ __forceinline__ uint4 round8(const float (&x)[8]) {
-    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-}
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
@@ -85,7 +79,7 @@ template <int W> __device__ __forceinline__ float row_sum(float x, float* part) 
     return x;
 }
 
-// W warps to a row (1: eight rows to a block), P pieces of 8 columns to a thread.
+// W warps to a row (1: eight rows to a block), P pieces of 8 columns to a thread, of which only the last may lie behind the row.
 template <int W, int P, bool RES>
 __global__ void __launch_bounds__(W == 1 ? 256 : W * 32) layer_norm_kernel(const __grid_constant__ NormArgs p) {
     __shared__ RowGroups table;
@@ -96,75 +90,77 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 32) layer_norm_kernel(const
     const int total = fill_row_groups(&table, p.row_begin, p.row_end, p.groups, p.rows_cap, blockIdx.x == 0, p.dev_status);
     const int team = W == 1 ? threadIdx.x >> 5 : 0, t = W == 1 ? threadIdx.x & 31 : threadIdx.x;
     const float inv = 1.0f / p.C;
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    const uint64_t one = pair_of(p.one, p.one);
+    const bool whole = ((P - 1) * kThreads + t) * 8 < p.C;
     int g = 0;
     for (int v = blockIdx.x * kTeams + team; v < total; v += gridDim.x * kTeams) {
         g = group_of(&table, v, g);
         const size_t row = (size_t)(table.begin[g] + v - table.first[g]);
         const size_t set = (size_t)(g % p.n_sets) * p.set_stride;
-        uint4 z[P];
+        uint4 x[P], r[P];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int c = (i * kThreads + t) * 8;
-            z[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (c < p.C) z[i] = ld_once128(p.x + row * p.x_stride + c);
-        }
-        float sum = 0.f;
-        if constexpr (RES) {
-            uint4 r[P];
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                const int c = (i * kThreads + t) * 8;
-                r[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (c < p.C) r[i] = ld_once128(p.r + row * p.r_stride + c);
-            }
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                const int c = (i * kThreads + t) * 8;
-                if (c >= p.C) continue;
-                uint4 gate = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);      // ones
-                if (p.gate != nullptr) gate = ldg128(p.gate + set + c);
-                float a[8], b[8], q[8];
-                widen8(z[i], a); widen8(r[i], b); widen8(gate, q);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = fmaf(q[e], b[e], a[e]);
-                z[i] = round8(a);
-                *reinterpret_cast<uint4*>(p.x_out + row * p.x_out_stride + c) = z[i];
+            x[i] = r[i] = none;
+            if (i < P - 1 || whole) {
+                x[i] = ld_once128(p.x + row * p.x_stride + (i * kThreads + t) * 8);
+                if (RES) r[i] = ld_once128(p.r + row * p.r_stride + (i * kThreads + t) * 8);
             }
         }
+        uint64_t z[P][4], sum = 0;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            float a[8];
-            widen8(z[i], a);
-            sum += ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+            widen8(x[i], z[i]);
+            if (RES && (i < P - 1 || whole)) {
+                uint64_t b[4], q[4];
+                widen8(r[i], b);
+                if (p.gate != nullptr) {
+                    widen8(ldg128(p.gate + set + (i * kThreads + t) * 8), q);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[i][e] = fma2(q[e], b[e], z[i][e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[i][e] = add2(b[e], z[i][e]);
+                }
+                x[i] = round8(z[i]);
+                *reinterpret_cast<uint4*>(p.x_out + row * p.x_out_stride + (i * kThreads + t) * 8) = x[i];
+                widen8(x[i], z[i]);
+            }
+            sum = add2(sum, add2(add2(z[i][0], z[i][1]), add2(z[i][2], z[i][3])));
         }
-        const float mean = row_sum<W>(sum, part[0]) * inv;
-        float sq = 0.f;
+        const float mean = row_sum<W>(sum2(sum), part[0]) * inv;
+        const uint64_t minus = pair_of(-mean, -mean);
+        uint64_t sq = 0;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            if ((i * kThreads + t) * 8 >= p.C) continue;
-            float a[8];
-            widen8(z[i], a);
+            if (i == P - 1 && !whole) break;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sq = fmaf(a[e] - mean, a[e] - mean, sq);
+            for (int e = 0; e < 4; ++e) {
+                z[i][e] = add2(z[i][e], minus);
+                sq = fma2(z[i][e], z[i][e], sq);
+            }
         }
-        const float rstd = rsqrtf(fmaf(row_sum<W>(sq, part[W > 1]), inv, p.eps));
+        const float rstd = rsqrtf(fmaf(row_sum<W>(sum2(sq), part[1]), inv, p.eps));
         if (t == 0) {
             if (p.mean != nullptr) p.mean[row] = mean;
             if (p.rstd != nullptr) p.rstd[row] = rstd;
         }
+        const uint64_t scale = pair_of(rstd, rstd);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int c = (i * kThreads + t) * 8;
-            if (c >= p.C) continue;
-            float a[8], w[8], b[8];
-            widen8(z[i], a);
-            if (p.weight != nullptr) widen8(ldg128(p.weight + set + c), w);
-            else for (int e = 0; e < 8; ++e) w[e] = 1.0f - p.one;
-            if (p.bias != nullptr) widen8(ldg128(p.bias + set + c), b);
-            else for (int e = 0; e < 8; ++e) b[e] = 0.f;
+            if (i == P - 1 && !whole) break;
+            uint64_t w[4], b[4] = {0, 0, 0, 0};
+            const size_t at = set + (i * kThreads + t) * 8;
+            if (p.bias != nullptr) widen8(ldg128(p.bias + at), b);
+            if (p.weight != nullptr) {
+                widen8(ldg128(p.weight + at), w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] = fmaf((a[e] - mean) * rstd, w[e] + p.one, b[e]);
-            *reinterpret_cast<uint4*>(p.out + row * p.out_stride + c) = round8(a);
+                for (int e = 0; e < 4; ++e) z[i][e] = fma2(mul2(z[i][e], scale), add2(w[e], one), b[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[i][e] = fma2(z[i][e], scale, b[e]);
+            }
+            *reinterpret_cast<uint4*>(p.out + row * p.out_stride + (i * kThreads + t) * 8) = round8(z[i]);
         }
     }
 }
@@ -172,140 +168,264 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 32) layer_norm_kernel(const
 // Rows to a block's share: the same in both kernels of the backward pass.
 __host__ __device__ __forceinline__ int norm_share(int total, int blocks) { return total > 0 ? (total + blocks - 1) / blocks : 1; }
 
-template <int T, bool RES>
-__global__ void __launch_bounds__(T, T <= 256 ? 2 : 1) layer_norm_backward_kernel(const __grid_constant__ NormGradArgs p) {
+constexpr int kNormThreads = 512, kNormMaxTeams = 8;
+
+// 16 bytes to shared memory on their own; a thread waits for its own copies only, and reads what it copied itself.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+// `teams` of `width` threads to a block, a row to a team; AHEAD rows of every team are on their way or at hand, each thread's columns at
+// places of its own: no barrier, and the bytes in flight do not depend on registers.
+template <bool RES, int EACH, int AHEAD>
+__global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(const __grid_constant__ NormGradArgs p, int width, int teams) {
+    extern __shared__ __align__(16) uint8_t ring[];   // [AHEAD][x, dy, dx_out, r][piece][threads] of 16 bytes
     __shared__ RowGroups table;
-    __shared__ float2 part[2][T / 32];
-    constexpr bool kAhead = T < 1024;                 // room for the next row's loads in registers
+    __shared__ __align__(16) uint64_t part[2][kNormThreads / 32 + kNormMaxTeams];    // of a warp: the two sums; an even number to a team
+    __shared__ float4 stage[kNormThreads];
     grid_dependency_wait();
     grid_launch_dependents();
     const int total = fill_row_groups(&table, p.row_begin, p.row_end, p.groups, p.rows_cap, blockIdx.x == 0, p.dev_status);
     const int share = norm_share(total, gridDim.x);
     const long long v0 = (long long)blockIdx.x * share;
-    if (v0 >= total) return;
     const int v1 = (int)min((long long)total, v0 + share);
-    const int c = threadIdx.x * 8, warps = blockDim.x >> 5;
-    const bool live = c < p.C;
+    if (v0 >= v1) return;
+    const int team = threadIdx.x / width, t = threadIdx.x - team * width;
+    const int warps = width >> 5, places = (warps + 1) & ~1;
+    const bool from_elsewhere = p.dz != nullptr;
     const float inv = 1.0f / p.C;
-    int g = group_of(&table, (int)v0, 0), ahead_g = g;
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-    uint4 x, dy, dz = none, r = none;
-    float mean, rstd;
-    auto fetch = [&](int v, uint4& x, uint4& dy, uint4& dz, uint4& r, float& mean, float& rstd) {
-        ahead_g = group_of(&table, v, ahead_g);
-        const size_t row = (size_t)(table.begin[ahead_g] + v - table.first[ahead_g]);
-        x = dy = none;
-        mean = p.mean[row];
-        rstd = p.rstd[row];
-        if (!live) return;
-        x = ld_once128(p.x + row * p.x_stride + c);
-        dy = ld_once128(p.dy + row * p.dy_stride + c);
-        if constexpr (RES) {
-            if (p.dz != nullptr) dz = ld_once128(p.dz + row * p.dz_stride + c);
-            r = ld_once128(p.r + row * p.r_stride + c);
-        } else {
-            if (p.dz != nullptr) dz = ld_once128(p.dz + row * p.dz_stride + c);
-        }
-    };
-    float dw[8], db[8], dg[8];
-    uint4 weight = none, gate = none;
-    auto enter = [&] {                                // a new group: its parameters, no sums yet
-        const size_t set = (size_t)(g % p.n_sets) * p.set_stride;
-        const uint32_t one = p.one != 0.f ? 0u : 0x3f803f80u;
-        weight = make_uint4(one, one, one, one);
-        if (p.weight != nullptr && live) weight = ldg128(p.weight + set + c);
-        if (RES && live) gate = ldg128(p.gate + set + c);
+    const uint64_t one = pair_of(p.one, p.one);
+    const uint32_t piece_bytes = blockDim.x * 16, array_bytes = EACH * piece_bytes, slot_bytes = (RES ? 4 : 3) * array_bytes;
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
+    int col[EACH];
+    bool live[EACH];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dw[e] = db[e] = dg[e] = 0.f;
-    };
-    auto leave = [&] {
-        if (!live) return;
-        float* to = p.sums + (size_t)(blockIdx.x + g) * 3 * p.C + c;
-        auto put = [&](float* at, const float (&s)[8]) {
-            reinterpret_cast<float4*>(at)[0] = make_float4(s[0], s[1], s[2], s[3]);
-            reinterpret_cast<float4*>(at)[1] = make_float4(s[4], s[5], s[6], s[7]);
-        };
-        put(to, dw);
-        put(to + p.C, db);
-        if (RES) put(to + 2 * p.C, dg);
-    };
-    enter();
-    fetch((int)v0, x, dy, dz, r, mean, rstd);
-    for (int v = (int)v0; v < v1; ++v) {
-        if (v >= table.first[g + 1]) {
-            leave();
-            g = group_of(&table, v, g);
-            enter();
-        }
-        if (!kAhead && v > v0) fetch(v, x, dy, dz, r, mean, rstd);
-        float h[8], d[8], w[8], s1 = 0.f, s2 = 0.f;
-        widen8(x, h); widen8(dy, d); widen8(weight, w);
-        const float m = mean, s = rstd;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            h[e] = live ? (h[e] - m) * s : 0.f;
-            dw[e] = fmaf(d[e], h[e], dw[e]);
-            db[e] += d[e];
-            d[e] *= w[e] + p.one;
-            s1 += d[e];
-            s2 = fmaf(d[e], h[e], s2);
-        }
-        const uint4 dz_now = dz, r_now = r;
-        const size_t row = (size_t)(table.begin[g] + v - table.first[g]);
-        if (kAhead && v + 1 < v1) fetch(v + 1, x, dy, dz, r, mean, rstd);
-        s1 = warp_sum(s1);
-        s2 = warp_sum(s2);
-        float2* at = part[v & 1];
-        if ((threadIdx.x & 31) == 0) at[threadIdx.x >> 5] = make_float2(s1, s2);
-        __syncthreads();
-        s1 = s2 = 0.f;
-        for (int i = 0; i < warps; ++i) {
-            s1 += at[i].x;
-            s2 += at[i].y;
-        }
-        s1 *= inv;
-        s2 *= inv;
-        if (!live) continue;
-        float q[8];
-        widen8(dz_now, q);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = fmaf(d[e] - s1 - h[e] * s2, s, q[e]);
-        *reinterpret_cast<uint4*>(p.dx + row * p.dx_stride + c) = round8(d);
-        if constexpr (RES) {
-            float b[8];
-            widen8(r_now, b);
-            widen8(gate, q);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                dg[e] = fmaf(d[e], b[e], dg[e]);
-                d[e] *= q[e];
-            }
-            *reinterpret_cast<uint4*>(p.dr + row * p.dr_stride + c) = round8(d);
-        }
+    for (int i = 0; i < EACH; ++i) {
+        col[i] = (i * width + t) * 8;
+        live[i] = col[i] < p.C;
     }
-    leave();
+    if ((warps & 1) && t == 0) part[0][team * places + warps] = part[1][team * places + warps] = 0;
+    int g = group_of(&table, (int)v0, 0), turn = 0;
+    // the rows to fetch: where their group ends, and where they lie
+    int next = (int)v0 + team, next_g = g, next_end = 0;
+    uint32_t next_slot = 0, slot = 0;
+    const uint16_t *x_at = nullptr, *dy_at = nullptr, *dz_at = nullptr, *r_at = nullptr;
+    auto fetch = [&] {
+        if (next < v1) {
+            if (next >= next_end) {
+                next_g = group_of(&table, next, next_g);
+                next_end = table.first[next_g + 1];
+                const size_t row = (size_t)(table.begin[next_g] + next - table.first[next_g]);
+                x_at = p.x + row * p.x_stride + col[0];
+                dy_at = p.dy + row * p.dy_stride + col[0];
+                dz_at = p.dz + row * p.dz_stride + col[0];
+                r_at = p.r + row * p.r_stride + col[0];
+            }
+            uint32_t to = base + next_slot;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i, to += piece_bytes) {
+                if (!live[i]) break;
+                copy16(to, x_at + i * width * 8);
+                copy16(to + array_bytes, dy_at + i * width * 8);
+                if (from_elsewhere) copy16(to + 2 * array_bytes, dz_at + i * width * 8);
+                if (RES) copy16(to + 3 * array_bytes, r_at + i * width * 8);
+            }
+            x_at += teams * p.x_stride;
+            dy_at += teams * p.dy_stride;
+            if (from_elsewhere) dz_at += teams * p.dz_stride;
+            if (RES) r_at += teams * p.r_stride;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        next += teams;
+        next_slot += slot_bytes;
+        if (next_slot == AHEAD * slot_bytes) next_slot = 0;
+    };
+#pragma unroll 1
+    for (int i = 0; i < AHEAD - 1; ++i) fetch();
+    int u = (int)v0 + team;
+    for (int v = (int)v0; v < v1;) {
+        // the share's rows of one group
+        g = group_of(&table, v, g);
+        const int end = min(v1, table.first[g + 1]);
+        const size_t set = (size_t)(g % p.n_sets) * p.set_stride;
+        const uint32_t unit = p.one != 0.f ? 0u : 0x3f803f80u;
+        uint64_t w[EACH][4], gate[EACH][4];
+        uint64_t dw[EACH][4], db[EACH][4], dg[EACH][4];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            uint4 weight = make_uint4(unit, unit, unit, unit), of = make_uint4(0u, 0u, 0u, 0u);
+            if (p.weight != nullptr && live[i]) weight = ldg128(p.weight + set + col[i]);
+            if (RES && live[i]) of = ldg128(p.gate + set + col[i]);
+            widen8(weight, w[i]);
+            widen8(of, gate[i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[i][e] = add2(w[i][e], one);
+                dw[i][e] = db[i][e] = dg[i][e] = 0;
+            }
+        }
+        size_t row = (size_t)(table.begin[g] + u - table.first[g]);
+        float mean = 0.f, rstd = 0.f;
+        if (u < end) {
+            mean = p.mean[row];
+            rstd = p.rstd[row];
+        }
+        uint16_t *dx_at = p.dx + row * p.dx_stride + col[0], *dr_at = p.dr + row * p.dr_stride + col[0];
+        for (; u < end; u += teams) {
+            fetch();                                  // (into the place of the row before this one)
+            asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
+            const uint32_t at = base + slot;
+            slot += slot_bytes;
+            if (slot == AHEAD * slot_bytes) slot = 0;
+            const uint64_t minus = pair_of(-mean, -mean), scale = pair_of(rstd, rstd);
+            row += teams;
+            if (u + teams < end) {                    // (of the next row)
+                mean = p.mean[row];
+                rstd = p.rstd[row];
+            }
+            constexpr bool kKeep = !(RES && EACH > 1);           // room for a row's h and a between the two passes
+            uint64_t h[EACH][4], a[EACH][4], sum_a = 0, sum_ah = 0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                if (!live[i]) break;
+                widen8(lds128(at + i * piece_bytes), h[i]);
+                widen8(lds128(at + i * piece_bytes + array_bytes), a[i]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    h[i][e] = mul2(add2(h[i][e], minus), scale);
+                    dw[i][e] = fma2(a[i][e], h[i][e], dw[i][e]);
+                    db[i][e] = add2(a[i][e], db[i][e]);
+                    a[i][e] = mul2(a[i][e], w[i][e]);
+                    sum_a = add2(sum_a, a[i][e]);
+                    sum_ah = fma2(a[i][e], h[i][e], sum_ah);
+                }
+            }
+            uint64_t sums = pair_of(sum2(sum_a), sum2(sum_ah));
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) {
+                float x, y;
+                parts_of(sums, x, y);
+                sums = add2(sums, pair_of(__shfl_xor_sync(0xffffffffu, x, d), __shfl_xor_sync(0xffffffffu, y, d)));
+            }
+            if (warps > 1) {
+                const uint64_t* mine = &part[turn][team * places];
+                if ((threadIdx.x & 31) == 0) part[turn][team * places + (t >> 5)] = sums;
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(width) : "memory");
+                sums = 0;
+#pragma unroll 4
+                for (int i = 0; i < places; i += 2) {
+                    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(mine + i);
+                    sums = add2(add2(sums, two.x), two.y);
+                }
+                turn ^= 1;                            // (a place is written again two rows on, behind the next one's barrier)
+            }
+            float s1, s2;
+            parts_of(mul2(sums, pair_of(-inv, -inv)), s1, s2);
+            const uint64_t mean_a = pair_of(s1, s1), mean_ah = pair_of(s2, s2);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                if (!live[i]) break;
+                uint64_t d[4], q[4] = {0, 0, 0, 0};
+                if (!kKeep) {
+                    widen8(lds128(at + i * piece_bytes), h[i]);
+                    widen8(lds128(at + i * piece_bytes + array_bytes), a[i]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        h[i][e] = mul2(add2(h[i][e], minus), scale);
+                        a[i][e] = mul2(a[i][e], w[i][e]);
+                    }
+                }
+                if (from_elsewhere) widen8(lds128(at + i * piece_bytes + 2 * array_bytes), q);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[e] = fma2(fma2(h[i][e], mean_ah, add2(a[i][e], mean_a)), scale, q[e]);
+                *reinterpret_cast<uint4*>(dx_at + i * width * 8) = round8(d);
+                if constexpr (RES) {
+                    widen8(lds128(at + i * piece_bytes + 3 * array_bytes), q);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        dg[i][e] = fma2(d[e], q[e], dg[i][e]);
+                        d[e] = mul2(d[e], gate[i][e]);
+                    }
+                    *reinterpret_cast<uint4*>(dr_at + i * width * 8) = round8(d);
+                }
+            }
+            dx_at += teams * p.dx_stride;
+            if (RES) dr_at += teams * p.dr_stride;
+        }
+        // the teams' sums, in their order, to the slot of this share and group
+        float* to = p.sums + (size_t)(blockIdx.x + g) * 3 * p.C;
+        auto gather = [&](const uint64_t (&s)[4], float* to, bool live) {
+            float4 f[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                parts_of(s[2 * i], f[i].x, f[i].y);
+                parts_of(s[2 * i + 1], f[i].z, f[i].w);
+            }
+            if (teams > 1) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    __syncthreads();
+                    if (team > 0) stage[threadIdx.x] = f[i];
+                    __syncthreads();
+                    if (team == 0)
+                        for (int k = 1; k < teams; ++k) {
+                            const float4 other = stage[k * width + t];
+                            f[i].x += other.x; f[i].y += other.y; f[i].z += other.z; f[i].w += other.w;
+                        }
+                }
+            }
+            if (team != 0 || !live) return;
+            reinterpret_cast<float4*>(to)[0] = f[0];
+            reinterpret_cast<float4*>(to)[1] = f[1];
+        };
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            gather(dw[i], to + col[i], live[i]);
+            gather(db[i], to + p.C + col[i], live[i]);
+            if (RES) gather(dg[i], to + 2 * p.C + col[i], live[i]);
+        }
+        v = end;
+    }
 }
 
-// The slots of a set, added in the order of the rows: a warp takes every eighth, the eight sums are added in their order.  blockIdx.z:
-// which of the three.
-__global__ void __launch_bounds__(256) layer_norm_sums_kernel(const __grid_constant__ NormGradArgs p, int blocks) {
+// The slots of a set, added in the order of the rows: a warp takes every sixteenth, the sixteen sums are added in their order.  64 columns to
+// a block, so that few sets still make some blocks; ten loads of a warp are on their way at one time, which is all it has where there is
+// a block to an SM.  blockIdx.z: which of the three.
+constexpr int kSumWarps = 16, kSumColumns = 64;
+__global__ void __launch_bounds__(kSumWarps * 32) layer_norm_sums_kernel(const __grid_constant__ NormGradArgs p, int blocks) {
     __shared__ RowGroups table;
-    __shared__ float4 part[8][32];
+    __shared__ float2 part[kSumWarps][32];
+    // (the ranges were written ahead of the kernel in front of this one, which had waited for them before it let this one in)
+    const int total = fill_row_groups(&table, p.row_begin, p.row_end, p.groups, p.rows_cap, false, nullptr);
     grid_dependency_wait();
     grid_launch_dependents();
-    const int total = fill_row_groups(&table, p.row_begin, p.row_end, p.groups, p.rows_cap, false, nullptr);
     const int share = norm_share(total, blocks), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int c = (blockIdx.x * 32 + lane) * 4, kind = blockIdx.z;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int c = blockIdx.x * kSumColumns + lane * 2, kind = blockIdx.z;
+    float2 sum = make_float2(0.f, 0.f);
     if (c < p.C)
         for (int g = blockIdx.y; g < p.groups; g += p.n_sets) {
             const int begin = table.first[g], end = table.first[g + 1];
             if (begin >= end) continue;
             const int last = (end - 1) / share;
-#pragma unroll 4
-            for (int b = begin / share + warp; b <= last; b += 8) {
-                const float4 s = *reinterpret_cast<const float4*>(p.sums + ((size_t)(b + g) * 3 + kind) * p.C + c);
-                sum.x += s.x; sum.y += s.y; sum.z += s.z; sum.w += s.w;
+            constexpr int kBatch = 10;
+            for (int b = begin / share + warp; b <= last; b += kBatch * kSumWarps) {
+                float2 s[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const float* from = p.sums + ((size_t)(b + i * kSumWarps + g) * 3 + kind) * p.C + c;
+                    s[i] = make_float2(0.f, 0.f);
+                    if (b + i * kSumWarps <= last) asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(s[i].x), "=f"(s[i].y) : "l"(from));
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    sum.x += s[i].x;
+                    sum.y += s[i].y;
+                }
             }
         }
     part[warp][lane] = sum;
@@ -313,11 +433,11 @@ __global__ void __launch_bounds__(256) layer_norm_sums_kernel(const __grid_const
     float* to = kind == 0 ? p.dweight : kind == 1 ? p.dbias : p.dgate;
     if (warp == 0 && c < p.C && to != nullptr) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) {
-            const float4 s = part[i][lane];
-            sum.x += s.x; sum.y += s.y; sum.z += s.z; sum.w += s.w;
+        for (int i = 1; i < kSumWarps; ++i) {
+            sum.x += part[i][lane].x;
+            sum.y += part[i][lane].y;
         }
-        *reinterpret_cast<float4*>(to + (size_t)blockIdx.y * p.C + c) = sum;
+        *reinterpret_cast<float2*>(to + (size_t)blockIdx.y * p.C + c) = sum;
     }
 }
 
@@ -327,35 +447,56 @@ template <int W, int P> static cudaError_t norm_launch(const NormArgs& p, int bl
     return p.r != nullptr ? launch_overlapped(layer_norm_kernel<W, P, true>, grid, block, 0, st, p)
                           : launch_overlapped(layer_norm_kernel<W, P, false>, grid, block, 0, st, p);
 }
-
-static cudaError_t norm_run(const NormArgs& p, cudaStream_t st) {
-    const int sms = sm_count();
-    // Rows that fill the warps of the GPU a few times over: a warp each.  Fewer: four warps, the latency of a row counts.
-    if (p.C > 4096) return norm_launch<8, 4>(p, std::min(p.rows_cap, 8 * sms), st);
-    if (p.rows_cap < 16 * sms) {
-        const int blocks = std::min(p.rows_cap, 16 * sms);
-        if (p.C <= 1024) return norm_launch<4, 1>(p, blocks, st);
-        if (p.C <= 2048) return norm_launch<4, 2>(p, blocks, st);
-        return norm_launch<4, 4>(p, blocks, st);
+template <int W> static cudaError_t norm_launch(const NormArgs& p, int blocks, cudaStream_t st) {
+    switch ((p.C + W * 256 - 1) / (W * 256)) {
+        case 1: return norm_launch<W, 1>(p, blocks, st);
+        case 2: return norm_launch<W, 2>(p, blocks, st);
+        case 3: return norm_launch<W, 3>(p, blocks, st);
+        default: return norm_launch<W, 4>(p, blocks, st);
     }
-    const int blocks = std::min((p.rows_cap + 7) / 8, 8 * sms);
-    if (p.C <= 256) return norm_launch<1, 1>(p, blocks, st);
-    if (p.C <= 512) return norm_launch<1, 2>(p, blocks, st);
-    if (p.C <= 1024) return norm_launch<1, 4>(p, blocks, st);
-    if (p.C <= 2048) return norm_launch<1, 8>(p, blocks, st);
-    return norm_launch<1, 16>(p, blocks, st);
 }
 
-// Blocks of the backward pass: as many as are resident at one time, with two rows each at least.
-static int norm_blocks(int rows_cap, int C) {
-    const int threads = (C / 8 + 31) & ~31;
-    return std::max(1, std::min((rows_cap + 1) / 2, sm_count() * std::max(1, std::min(8, 640 / threads))));
+// Warps to a row: what measured fastest.  Few rows: eight or four, the latency of a row counts (300 x 2048: 3.2 us with eight, 3.6 with
+// four, 4.8 with two; 1075 x 2048: 5.9, 5.2, 5.6).  Many: one for short rows (17000 x 1024: 13.2 us, four 21; 40000 x 512 with a
+// residual 31 and 49), two or four up to 2048 (17000 x 2048: two 26, four 31; with a residual, whose loads are twice as many, 59 and
+// 51), four up to 4096 (34000 x 4096 with a residual: 191 us, 0.90 of the copy rate; eight 203).
+static cudaError_t norm_run(const NormArgs& p, cudaStream_t st) {
+    const int rows = p.rows_cap, sms = sm_count();
+    if (p.C > 4096) return norm_launch<8>(p, std::min(rows, 4 * sms), st);
+    if (rows < 4 * sms) return norm_launch<8>(p, rows, st);
+    if (rows < 16 * sms || p.C > 2048) return norm_launch<4>(p, std::min(rows, 8 * sms), st);
+    if (p.C <= 1024) return norm_launch<1>(p, std::min((rows + 7) / 8, 8 * sms), st);
+    return p.r != nullptr ? norm_launch<4>(p, std::min(rows, 64 * sms), st) : norm_launch<2>(p, std::min(rows, 16 * sms), st);
 }
 
-template <int T> static cudaError_t norm_grad_launch(const NormGradArgs& p, int blocks, cudaStream_t st) {
-    const dim3 grid(blocks), block((p.C / 8 + 31) & ~31);
-    return p.r != nullptr ? launch_overlapped(layer_norm_backward_kernel<T, true>, grid, block, 0, st, p)
-                          : launch_overlapped(layer_norm_backward_kernel<T, false>, grid, block, 0, st, p);
+// Of the backward pass: threads of a team, teams of a block, blocks.
+struct NormShape {
+    int each, width, teams, blocks;                   // pieces of 8 columns of a thread, threads of a team, teams of a block
+};
+// Eight columns to a thread and up to eight teams; sixteen for rows of more than 4096 columns, which need it, and for many rows without a
+// gated residual, where the sums of two pieces still fit in registers and a row's reduction costs half as much (17408 x 2048: 62 us
+// with eight, 55 with sixteen; 1101 x 1536: 10.7 and 14; with the residual, 17408 x 2048: 85 and 133, as registers are spilled).
+static NormShape norm_shape(int rows_cap, int C, bool residual) {
+    NormShape n;
+    n.each = C > 4096 || (!residual && rows_cap > 16 * sm_count()) ? 2 : 1;
+    n.width = (C / 8 + 32 * n.each - 1) / (32 * n.each) * 32;
+    n.teams = std::min(kNormMaxTeams, kNormThreads / n.width);
+    n.blocks = std::max(1, std::min((rows_cap + n.teams - 1) / n.teams, sm_count()));
+    return n;
+}
+template <bool RES, int EACH, int AHEAD> static cudaError_t norm_grad_launch(const NormGradArgs& p, const NormShape& n, cudaStream_t st) {
+    constexpr int kEach = AHEAD * (RES ? 4 : 3) * EACH * 16;           // bytes of a thread
+    static int ready[kMaxDevices] = {};
+    const int dev = current_device();
+    if (dev < 0) return cudaErrorInvalidDevice;
+    if (!__atomic_load_n(&ready[dev], __ATOMIC_ACQUIRE)) {
+        const cudaError_t e = cudaFuncSetAttribute(layer_norm_backward_kernel<RES, EACH, AHEAD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   kEach * kNormThreads);
+        if (e != cudaSuccess) return e;
+        __atomic_store_n(&ready[dev], 1, __ATOMIC_RELEASE);
+    }
+    const int threads = n.width * n.teams;
+    return launch_overlapped(layer_norm_backward_kernel<RES, EACH, AHEAD>, dim3(n.blocks), dim3(threads), kEach * threads, st, p, n.width, n.teams);
 }
 
 static int check_norm(int rows_cap, int groups, int n_sets, int C, long long set_stride, const void* begin, const void* end) {
@@ -399,7 +540,7 @@ extern "C" int regione_layer_norm(const regione_bf16* x, int64_t x_stride, const
 
 extern "C" size_t regione_layer_norm_backward_workspace(int rows_cap, int groups, int C) {
     if (rows_cap < 0 || groups < 0 || C < 1 || C % 8 || C > kNormMaxC || groups > kMaxRowGroups || rows_cap > (1 << 24)) return 0;
-    return (size_t)(norm_blocks(rows_cap, C) + groups) * 3 * C * sizeof(float);
+    return (size_t)(norm_shape(rows_cap, C, true).blocks + groups) * 3 * C * sizeof(float);
 }
 
 extern "C" int regione_layer_norm_backward(const regione_bf16* x, int64_t x_stride, const float* mean, const float* rstd,
@@ -431,13 +572,13 @@ extern "C" int regione_layer_norm_backward(const regione_bf16* x, int64_t x_stri
     p.dx = dx; p.dr = dr; p.dx_stride = dx_stride; p.dr_stride = dr_stride;
     p.sums = (float*)workspace; p.dweight = dweight; p.dbias = dbias; p.dgate = dgate; p.dev_status = dev_status;
     const cudaStream_t st = (cudaStream_t)stream;
-    const int blocks = norm_blocks(rows_cap, C);
+    const NormShape n = norm_shape(rows_cap, C, r != nullptr);
     if (!empty) {
-        const cudaError_t e = C <= 2048 ? norm_grad_launch<256>(p, blocks, st) : C <= 4096 ? norm_grad_launch<512>(p, blocks, st)
-                                                                                           : norm_grad_launch<1024>(p, blocks, st);
+        const cudaError_t e = n.each == 2 ? (r ? norm_grad_launch<true, 2, 3>(p, n, st) : norm_grad_launch<false, 2, 3>(p, n, st))
+                                          : (r ? norm_grad_launch<true, 1, 4>(p, n, st) : norm_grad_launch<false, 1, 4>(p, n, st));
         if (e != cudaSuccess) return launch_status(e);
     }
     if (!dweight && !dbias && !dgate) return REGIONE_OK;
-    const dim3 grid((C + 127) / 128, n_sets, dgate ? 3 : 2);
-    return launch_status(launch_overlapped(layer_norm_sums_kernel, grid, dim3(256), 0, st, p, blocks));
+    const dim3 grid((C + kSumColumns - 1) / kSumColumns, n_sets, dgate ? 3 : 2);
+    return launch_status(launch_overlapped(layer_norm_sums_kernel, grid, dim3(kSumWarps * 32), 0, st, p, n.blocks));
 }

@@ -44,58 +44,99 @@ struct RotaryArgs {
 
 // LANES: a power of two, at least D / 8; lane g of a head has elements 8 g .. 8 g + 7.
 template <int LANES, bool HALF, bool NORM>
-__global__ void __launch_bounds__(kRotaryWarps * 32) rotary_axes_kernel(const __grid_constant__ RotaryArgs p) {
+__global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const __grid_constant__ RotaryArgs p) {
     __shared__ __align__(16) float cos_of[kRotaryWarps][LANES * 4], sin_of[kRotaryWarps][LANES * 4];
+    __shared__ float2 turns_of[LANES * 4];
+    __shared__ int axis_of[LANES * 4];
+    constexpr int kHeads = 32 / LANES;                // of a pass of the warp
+    constexpr int kPairs = (LANES * 4 + 31) / 32;     // of a lane
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pairs = p.D / 2;
+    // The pairs' frequencies: from the launch's parameters once a block, since 32 addresses of them take a warp 32 turns, then a lane keeps
+    // those of the pairs whose angles it forms.
+    if (threadIdx.x < LANES * 4) {
+        turns_of[threadIdx.x] = make_float2(p.turns_hi[threadIdx.x], p.turns_lo[threadIdx.x]);
+        axis_of[threadIdx.x] = p.axis[threadIdx.x];
+    }
+    __syncthreads();
+    float2 turns[kPairs];
+    int axis[kPairs];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        const int at = min(lane + 32 * i, LANES * 4 - 1);
+        turns[i] = turns_of[at];
+        axis[i] = axis_of[at];
+    }
     grid_dependency_wait();
     grid_launch_dependents();
-    constexpr int kHeads = 32 / LANES;                // of a pass of the warp
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = blockIdx.y;
-    const int work = blockIdx.x * kRotaryWarps + warp, j = work / p.parts, part = work - j * p.parts;
-    int live = p.cap;
-    if (p.n != nullptr) {
-        live = p.n[b];
-        if (live < 0 || live > p.cap) {
-            if (work == 0 && lane == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
-            live = live < 0 ? 0 : p.cap;
-        }
-    }
-    if (j >= live) return;
-    int place = j;
-    if (p.idx != nullptr) {
-        place = p.idx[(size_t)b * p.cap + j];
-        if (place < 0 || place >= p.n_pos) {
-            if (lane == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
-            return;
-        }
-    }
-    const int g = lane & (LANES - 1), pieces = p.D / 8, pairs = p.D / 2;
+    const int g = lane & (LANES - 1), pieces = p.D / 8, in_pass = lane / LANES;
     const bool on = g < pieces;
-    const long long from = p.compact ? j : place;
-    const uint16_t* q = p.q + b * p.q_batch + from * p.q_row;
-    const uint16_t* k = p.k == nullptr ? nullptr : p.k + b * p.k_batch + from * p.k_row;
-    uint16_t* q_out = p.q_out + b * p.q_out_batch + j * p.q_out_row;
-    uint16_t* k_out = p.k == nullptr ? nullptr : p.k_out + b * p.k_out_batch + j * p.k_out_row;
-
-    // ---- angles ---------------------------------------------------------------------------------------------------------------
-    float at[kRotaryAxes];
-    const float* position = p.positions + b * p.positions_batch + (long long)place * p.axes;
-#pragma unroll
-    for (int a = 0; a < kRotaryAxes; ++a) at[a] = a < p.axes ? position[a] : 0.f;
-    for (int i = lane; i < pairs; i += 32) {
-        const int axis = p.axis[i];
-        const float x = axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
-        const float hi = p.turns_hi[i], whole = x * hi, rest = fmaf(x, p.turns_lo[i], fmaf(x, hi, -whole));
-        float s, c;
-        sincospif(2.0f * ((whole - rintf(whole)) + rest), &s, &c);
-        cos_of[warp][i] = c;
-        sin_of[warp][i] = s * p.sign;
-    }
-    __syncwarp();
-    constexpr int kAngles = HALF ? 8 : 4;
-    float cs[kAngles], sn[kAngles];
     const bool second = HALF && 2 * g >= pieces;      // this lane's elements are the second ones of their pairs
-    {
+    const int partner = HALF ? (lane & ~(LANES - 1)) + (!on ? g : second ? g - pieces / 2 : g + pieces / 2) : 0;
+    const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+    uint4 wq = ones, wk = ones;
+    if (NORM && on) {
+        if (p.q_weight != nullptr) wq = ldg128(p.q_weight + 8 * g);
+        if (p.k_weight != nullptr) wk = ldg128(p.k_weight + 8 * g);
+    }
+    const float inv = 1.0f / p.D;
+    const int heads = p.Hq + p.Hk, passes = (heads + kHeads - 1) / kHeads;
+    const long long total = (long long)p.B * p.cap * p.parts;
+    for (long long item = (long long)blockIdx.x * kRotaryWarps + warp; item < total; item += (long long)gridDim.x * kRotaryWarps) {
+        const int row = (int)(item / p.parts), part = (int)(item - (long long)row * p.parts);
+        const int b = row / p.cap, j = row - b * p.cap;
+        int live = p.cap;
+        if (p.n != nullptr) {
+            live = p.n[b];
+            if (live < 0 || live > p.cap) {
+                if (j == 0 && part == 0 && lane == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+                live = live < 0 ? 0 : p.cap;
+            }
+        }
+        if (j >= live) continue;
+        int place = j;
+        if (p.idx != nullptr) {
+            place = p.idx[row];
+            if (place < 0 || place >= p.n_pos) {
+                if (lane == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+                continue;
+            }
+        }
+        const long long from = p.compact ? j : place;
+        const uint16_t* q = p.q + b * p.q_batch + from * p.q_row + 8 * g;
+        const uint16_t* k = p.k + b * p.k_batch + from * p.k_row + 8 * g - (long long)p.Hq * p.D;
+        uint16_t* q_out = p.q_out + b * p.q_out_batch + j * p.q_out_row + 8 * g;
+        uint16_t* k_out = p.k_out + b * p.k_out_batch + j * p.k_out_row + 8 * g - (long long)p.Hq * p.D;
+        const int first_pass = (int)((long long)passes * part / p.parts), last_pass = (int)((long long)passes * (part + 1) / p.parts);
+        uint4 w[kRotaryAhead];
+        auto fetch = [&](int i0) {
+#pragma unroll
+            for (int u = 0; u < kRotaryAhead; ++u) {
+                const int h = (i0 + u) * kHeads + in_pass;
+                w[u] = make_uint4(0u, 0u, 0u, 0u);
+                // (not through the path of read-only data: the row may be turned in place)
+                if (i0 + u < last_pass && on && h < heads)
+                    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(w[u].x), "=r"(w[u].y), "=r"(w[u].z), "=r"(w[u].w) : "l"((h < p.Hq ? q : k) + h * p.D));
+            }
+        };
+        fetch(first_pass);
+        // the angles, while the first heads are on their way: lane a has the position on axis a
+        const float at = lane < p.axes ? p.positions[b * p.positions_batch + (long long)place * p.axes + lane] : 0.f;
+        __syncwarp();                                 // (the row before has read its angles)
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            const float x = __shfl_sync(0xffffffffu, at, axis[i]);
+            if (lane + 32 * i < pairs) {
+                const float whole = x * turns[i].x, rest = fmaf(x, turns[i].y, fmaf(x, turns[i].x, -whole));
+                float s, c;
+                sincospif(2.0f * ((whole - rintf(whole)) + rest), &s, &c);
+                cos_of[warp][lane + 32 * i] = c;
+                sin_of[warp][lane + 32 * i] = s * p.sign;
+            }
+        }
+        __syncwarp();
+        constexpr int kAngles = HALF ? 8 : 4;
+        float cs[kAngles], sn[kAngles];
         const int first = !on ? 0 : HALF ? 8 * (second ? g - pieces / 2 : g) : 4 * g;
 #pragma unroll
         for (int e = 0; e < kAngles; e += 4) {
@@ -106,65 +147,42 @@ __global__ void __launch_bounds__(kRotaryWarps * 32) rotary_axes_kernel(const __
         if (HALF && !second)
 #pragma unroll
             for (int e = 0; e < kAngles; ++e) sn[e] = -sn[e];
-    }
-    const int partner = HALF ? (lane & ~(LANES - 1)) + (!on ? g : second ? g - pieces / 2 : g + pieces / 2) : 0;
-    const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-    uint4 wq = ones, wk = ones;
-    if (NORM && on) {
-        if (p.q_weight != nullptr) wq = ldg128(p.q_weight + 8 * g);
-        if (p.k_weight != nullptr) wk = ldg128(p.k_weight + 8 * g);
-    }
-    const float inv = 1.0f / p.D;
 
-    // ---- heads of Q, then of K: this part's share of the passes ------------------------------------------------------------------
-    const int heads = p.Hq + p.Hk, passes = (heads + kHeads - 1) / kHeads;
-    const int first_pass = (int)((long long)passes * part / p.parts), last_pass = (int)((long long)passes * (part + 1) / p.parts);
-    const int in_pass = lane / LANES;
-    for (int i0 = first_pass; i0 < last_pass; i0 += kRotaryAhead) {
-        uint4 w[kRotaryAhead];
+        // ---- heads of Q, then of K: this part's share of the passes ------------------------------------------------------------
+        for (int i0 = first_pass; i0 < last_pass; i0 += kRotaryAhead) {
+            if (i0 > first_pass) fetch(i0);
 #pragma unroll
-        for (int u = 0; u < kRotaryAhead; ++u) {
-            const int h = (i0 + u) * kHeads + in_pass;
-            w[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (i0 + u < last_pass && on && h < heads) {
-                const uint16_t* src = h < p.Hq ? q + (long long)h * p.D : k + (long long)(h - p.Hq) * p.D;
-                // (not through the path of read-only data: the row may be turned in place)
-                asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                             : "=r"(w[u].x), "=r"(w[u].y), "=r"(w[u].z), "=r"(w[u].w) : "l"(src + 8 * g));
-            }
-        }
+            for (int u = 0; u < kRotaryAhead; ++u) {
+                if (i0 + u >= last_pass) break;
+                const int h = (i0 + u) * kHeads + in_pass;
+                float y[8] = {bf16_lo(w[u].x), bf16_hi(w[u].x), bf16_lo(w[u].y), bf16_hi(w[u].y),
+                              bf16_lo(w[u].z), bf16_hi(w[u].z), bf16_lo(w[u].w), bf16_hi(w[u].w)}, o[8];
+                if constexpr (NORM) {
+                    float ss = 0.f;
 #pragma unroll
-        for (int u = 0; u < kRotaryAhead; ++u) {
-            if (i0 + u >= last_pass) break;
-            const int h = (i0 + u) * kHeads + in_pass;
-            float y[8] = {bf16_lo(w[u].x), bf16_hi(w[u].x), bf16_lo(w[u].y), bf16_hi(w[u].y),
-                          bf16_lo(w[u].z), bf16_hi(w[u].z), bf16_lo(w[u].w), bf16_hi(w[u].w)}, o[8];
-            if constexpr (NORM) {
-                float ss = 0.f;
+                    for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+                    for (int d = LANES / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+                    const float r = rsqrtf(fmaf(ss, inv, p.eps));
+                    const uint4 v = h < p.Hq ? wq : wk;
+                    const float m[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
 #pragma unroll
-                for (int d = LANES / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-                const float r = rsqrtf(fmaf(ss, inv, p.eps));
-                const uint4 v = h < p.Hq ? wq : wk;
-                const float m[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] *= r * m[e];
-            }
-            if constexpr (HALF) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = fmaf(__shfl_sync(0xffffffffu, y[e], partner), sn[e], y[e] * cs[e]);
-            } else {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    o[2 * t] = fmaf(-y[2 * t + 1], sn[t], y[2 * t] * cs[t]);
-                    o[2 * t + 1] = fmaf(y[2 * t], sn[t], y[2 * t + 1] * cs[t]);
+                    for (int e = 0; e < 8; ++e) y[e] *= r * m[e];
                 }
+                if constexpr (HALF) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = fmaf(__shfl_sync(0xffffffffu, y[e], partner), sn[e], y[e] * cs[e]);
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        o[2 * t] = fmaf(-y[2 * t + 1], sn[t], y[2 * t] * cs[t]);
+                        o[2 * t + 1] = fmaf(y[2 * t], sn[t], y[2 * t + 1] * cs[t]);
+                    }
+                }
+                if (!on || h >= heads) continue;
+                *reinterpret_cast<uint4*>((h < p.Hq ? q_out : k_out) + h * p.D) =
+                    make_uint4(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]), pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7]));
             }
-            if (!on || h >= heads) continue;
-            uint16_t* dst = h < p.Hq ? q_out + (long long)h * p.D : k_out + (long long)(h - p.Hq) * p.D;
-            *reinterpret_cast<uint4*>(dst + 8 * g) =
-                make_uint4(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]), pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7]));
         }
     }
 }
@@ -201,6 +219,7 @@ extern "C" int regione_rotary_axes(const regione_bf16* q, int64_t q_batch, int64
     if (inverse && normalise) return REGIONE_UNSUPPORTED;           // (the gradient of the rotation alone)
     if (!aligned16(q_weight) || !aligned16(k_weight) || positions_batch < 0) return REGIONE_INVALID_ARG;
     if (!idx && cap > n_pos) return REGIONE_INVALID_ARG;
+    if ((long long)B * cap > 0x7fffffffLL) return REGIONE_UNSUPPORTED;
     if (D % 16 || D > kRotaryMaxD || axes > kRotaryAxes || Hq > 65536 || Hk > 65536 || B > 65535 || cap > (1 << 24) || n_pos > (1 << 28))
         return REGIONE_UNSUPPORTED;
     for (int i = 0; i < D / 2; ++i)
@@ -230,8 +249,8 @@ extern "C" int regione_rotary_axes(const regione_bf16* q, int64_t q_batch, int64
     const long long rows = (long long)B * cap;
     p.parts = 1;
     while (p.parts < passes && p.parts < 16 && rows * p.parts < 16LL * sm_count()) p.parts *= 2;
-    const long long blocks = ((long long)cap * p.parts + kRotaryWarps - 1) / kRotaryWarps;
-    const dim3 grid((unsigned)blocks, B);
+    const long long blocks = std::min((rows * p.parts + kRotaryWarps - 1) / kRotaryWarps, 64LL * sm_count());
+    const dim3 grid((unsigned)blocks);
     const bool half = rope_layout == REGIONE_ROPE_HALF, norm = normalise != 0;
     cudaStream_t st = (cudaStream_t)stream;
     switch (lanes) {
