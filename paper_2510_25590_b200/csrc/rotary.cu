@@ -15,7 +15,7 @@
 //
 // Bound by device memory: 4 bytes an element.  A warp has a row, or a part of its heads where rows are few; its lanes form the angles
 // of the D/2 pairs once and leave them in shared memory, then go through the heads, 16 bytes a lane and four loads in flight.
-#include "common.cuh"
+#include "f32x2.cuh"
 
 #include <algorithm>
 #include <cmath>
@@ -36,11 +36,16 @@ struct RotaryArgs {
     int compact;                                      // row j is read; else row idx[b, j]
     const uint16_t *q_weight, *k_weight;
     float eps, sign;                                  // sign: -1 turns back
-    int parts;                                        // warps that share a row
+    int parts_log;                                    // 1 << this warps share a row
     int32_t* dev_status;
     float turns_hi[kRotaryMaxD / 2], turns_lo[kRotaryMaxD / 2];
     uint8_t axis[kRotaryMaxD / 2];
 };
+
+__device__ __forceinline__ uint4 of_lane(const uint4& v, int lane) {
+    return make_uint4(__shfl_sync(0xffffffffu, v.x, lane), __shfl_sync(0xffffffffu, v.y, lane), __shfl_sync(0xffffffffu, v.z, lane),
+                      __shfl_sync(0xffffffffu, v.w, lane));
+}
 
 // LANES: a power of two, at least D / 8; lane g of a head has elements 8 g .. 8 g + 7.
 template <int LANES, bool HALF, bool NORM>
@@ -72,18 +77,13 @@ __global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const
     const bool on = g < pieces;
     const bool second = HALF && 2 * g >= pieces;      // this lane's elements are the second ones of their pairs
     const int partner = HALF ? (lane & ~(LANES - 1)) + (!on ? g : second ? g - pieces / 2 : g + pieces / 2) : 0;
-    const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-    uint4 wq = ones, wk = ones;
-    if (NORM && on) {
-        if (p.q_weight != nullptr) wq = ldg128(p.q_weight + 8 * g);
-        if (p.k_weight != nullptr) wk = ldg128(p.k_weight + 8 * g);
-    }
+    const int partner_g = partner & (LANES - 1);
     const float inv = 1.0f / p.D;
     const int heads = p.Hq + p.Hk, passes = (heads + kHeads - 1) / kHeads;
-    const long long total = (long long)p.B * p.cap * p.parts;
-    for (long long item = (long long)blockIdx.x * kRotaryWarps + warp; item < total; item += (long long)gridDim.x * kRotaryWarps) {
-        const int row = (int)(item / p.parts), part = (int)(item - (long long)row * p.parts);
-        const int b = row / p.cap, j = row - b * p.cap;
+    const uint32_t total = ((uint32_t)p.B * p.cap) << p.parts_log;
+    for (uint32_t item = blockIdx.x * kRotaryWarps + warp; item < total; item += gridDim.x * kRotaryWarps) {
+        const int row = (int)(item >> p.parts_log), part = (int)(item & ((1u << p.parts_log) - 1));
+        const int b = (int)((uint32_t)row / (uint32_t)p.cap), j = row - b * p.cap;
         int live = p.cap;
         if (p.n != nullptr) {
             live = p.n[b];
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const
         const uint16_t* k = p.k + b * p.k_batch + from * p.k_row + 8 * g - (long long)p.Hq * p.D;
         uint16_t* q_out = p.q_out + b * p.q_out_batch + j * p.q_out_row + 8 * g;
         uint16_t* k_out = p.k_out + b * p.k_out_batch + j * p.k_out_row + 8 * g - (long long)p.Hq * p.D;
-        const int first_pass = (int)((long long)passes * part / p.parts), last_pass = (int)((long long)passes * (part + 1) / p.parts);
+        const int first_pass = (passes * part) >> p.parts_log, last_pass = (passes * (part + 1)) >> p.parts_log;
         uint4 w[kRotaryAhead];
         auto fetch = [&](int i0) {
 #pragma unroll
@@ -128,25 +128,60 @@ __global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const
             const float x = __shfl_sync(0xffffffffu, at, axis[i]);
             if (lane + 32 * i < pairs) {
                 const float whole = x * turns[i].x, rest = fmaf(x, turns[i].y, fmaf(x, turns[i].x, -whole));
-                float s, c;
-                sincospif(2.0f * ((whole - rintf(whole)) + rest), &s, &c);
-                cos_of[warp][lane + 32 * i] = c;
-                sin_of[warp][lane + 32 * i] = s * p.sign;
+                float turn = (whole - rintf(whole)) + rest;
+                turn = (turn - rintf(turn)) * 6.283185307179586f;
+                // (the fast forms: 2^-21 off within half a turn, a hundredth of the output's rounding)
+                cos_of[warp][lane + 32 * i] = __cosf(turn);
+                sin_of[warp][lane + 32 * i] = __sinf(turn) * p.sign;
             }
         }
         __syncwarp();
-        constexpr int kAngles = HALF ? 8 : 4;
-        float cs[kAngles], sn[kAngles];
+        // What the lane's elements are multiplied with, weights and angles in one: the same for all heads of Q, and of K.
+        //   halves: out[e] = r (x[e] own[e] + partner[e] other[e]);   pairs: (a, b) -> r (a own.x + b other.x, a own.y + b other.y)
+        uint64_t own[4], other[4];
         const int first = !on ? 0 : HALF ? 8 * (second ? g - pieces / 2 : g) : 4 * g;
+        auto factors = [&](const uint16_t* weight) {
+            const float *c = &cos_of[warp][first], *s = &sin_of[warp][first];
 #pragma unroll
-        for (int e = 0; e < kAngles; e += 4) {
-            const float4 c = *reinterpret_cast<const float4*>(&cos_of[warp][first + e]), s = *reinterpret_cast<const float4*>(&sin_of[warp][first + e]);
-            cs[e] = c.x; cs[e + 1] = c.y; cs[e + 2] = c.z; cs[e + 3] = c.w;
-            sn[e] = s.x; sn[e + 1] = s.y; sn[e + 2] = s.z; sn[e + 3] = s.w;
-        }
-        if (HALF && !second)
+            for (int e = 0; e < 4; e += 2) {
+                if constexpr (HALF) {
+                    const float4 cs = *reinterpret_cast<const float4*>(c + 2 * e), sn = *reinterpret_cast<const float4*>(s + 2 * e);
+                    const float sign = second ? 1.f : -1.f;
+                    own[e] = pair_of(cs.x, cs.y);
+                    own[e + 1] = pair_of(cs.z, cs.w);
+                    other[e] = pair_of(sign * sn.x, sign * sn.y);
+                    other[e + 1] = pair_of(sign * sn.z, sign * sn.w);
+                } else {
+                    const float2 cs = *reinterpret_cast<const float2*>(c + e), sn = *reinterpret_cast<const float2*>(s + e);
+                    own[e] = pair_of(cs.x, sn.x);
+                    own[e + 1] = pair_of(cs.y, sn.y);
+                    other[e] = pair_of(-sn.x, cs.x);
+                    other[e + 1] = pair_of(-sn.y, cs.y);
+                }
+            }
+            if (NORM && weight != nullptr && on) {    // (from L1: there are no registers to keep them in)
+                uint64_t a[4], b[4];
+                if constexpr (HALF) {
+                    widen8(ldg128(weight + 8 * g), a);
+                    widen8(ldg128(weight + 8 * partner_g), b);
+                } else {
+                    const uint4 v = ldg128(weight + 8 * g);
+                    const uint32_t of[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int e = 0; e < kAngles; ++e) sn[e] = -sn[e];
+                    for (int e = 0; e < 4; ++e) {
+                        a[e] = pair_of(bf16_lo(of[e]), bf16_lo(of[e]));
+                        b[e] = pair_of(bf16_hi(of[e]), bf16_hi(of[e]));
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    own[e] = mul2(own[e], a[e]);
+                    other[e] = mul2(other[e], b[e]);
+                }
+            }
+        };
+        bool of_k = first_pass * kHeads + in_pass >= p.Hq;
+        factors(of_k ? p.k_weight : p.q_weight);
 
         // ---- heads of Q, then of K: this part's share of the passes ------------------------------------------------------------
         for (int i0 = first_pass; i0 < last_pass; i0 += kRotaryAhead) {
@@ -155,33 +190,37 @@ __global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const
             for (int u = 0; u < kRotaryAhead; ++u) {
                 if (i0 + u >= last_pass) break;
                 const int h = (i0 + u) * kHeads + in_pass;
-                float y[8] = {bf16_lo(w[u].x), bf16_hi(w[u].x), bf16_lo(w[u].y), bf16_hi(w[u].y),
-                              bf16_lo(w[u].z), bf16_hi(w[u].z), bf16_lo(w[u].w), bf16_hi(w[u].w)}, o[8];
+                if (NORM && !of_k && h >= p.Hq) {                    // (once a row)
+                    of_k = true;
+                    factors(p.k_weight);
+                }
+                uint64_t x[4], o[4];
+                widen8(w[u], x);
+                float r = 1.f;
                 if constexpr (NORM) {
-                    float ss = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+                    float ss = sum2(fma2(x[0], x[0], fma2(x[1], x[1], fma2(x[2], x[2], mul2(x[3], x[3])))));
 #pragma unroll
                     for (int d = LANES / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-                    const float r = rsqrtf(fmaf(ss, inv, p.eps));
-                    const uint4 v = h < p.Hq ? wq : wk;
-                    const float m[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= r * m[e];
+                    r = rsqrtf(fmaf(ss, inv, p.eps));
                 }
                 if constexpr (HALF) {
+                    uint64_t y[4];
+                    widen8(of_lane(w[u], partner), y);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = fmaf(__shfl_sync(0xffffffffu, y[e], partner), sn[e], y[e] * cs[e]);
+                    for (int e = 0; e < 4; ++e) o[e] = fma2(y[e], other[e], mul2(x[e], own[e]));
                 } else {
+                    const uint32_t v[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        o[2 * t] = fmaf(-y[2 * t + 1], sn[t], y[2 * t] * cs[t]);
-                        o[2 * t + 1] = fmaf(y[2 * t], sn[t], y[2 * t + 1] * cs[t]);
+                    for (int e = 0; e < 4; ++e) {
+                        const float a = bf16_lo(v[e]), b = bf16_hi(v[e]);
+                        o[e] = fma2(pair_of(b, b), other[e], mul2(pair_of(a, a), own[e]));
                     }
                 }
+                if constexpr (NORM)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = mul2(o[e], pair_of(r, r));
                 if (!on || h >= heads) continue;
-                *reinterpret_cast<uint4*>((h < p.Hq ? q_out : k_out) + h * p.D) =
-                    make_uint4(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]), pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7]));
+                *reinterpret_cast<uint4*>((h < p.Hq ? q_out : k_out) + h * p.D) = round8(o);
             }
         }
     }
@@ -219,7 +258,7 @@ extern "C" int regione_rotary_axes(const regione_bf16* q, int64_t q_batch, int64
     if (inverse && normalise) return REGIONE_UNSUPPORTED;           // (the gradient of the rotation alone)
     if (!aligned16(q_weight) || !aligned16(k_weight) || positions_batch < 0) return REGIONE_INVALID_ARG;
     if (!idx && cap > n_pos) return REGIONE_INVALID_ARG;
-    if ((long long)B * cap > 0x7fffffffLL) return REGIONE_UNSUPPORTED;
+    if ((long long)B * cap > 0x3fffffffLL) return REGIONE_UNSUPPORTED;
     if (D % 16 || D > kRotaryMaxD || axes > kRotaryAxes || Hq > 65536 || Hk > 65536 || B > 65535 || cap > (1 << 24) || n_pos > (1 << 28))
         return REGIONE_UNSUPPORTED;
     for (int i = 0; i < D / 2; ++i)
@@ -247,9 +286,8 @@ extern "C" int regione_rotary_axes(const regione_bf16* q, int64_t q_batch, int64
     // Where rows are few their heads are dealt over several warps, until the GPU has some sixteen warps an SM.
     const int passes = ((Hq + Hk) * lanes + 31) / 32;
     const long long rows = (long long)B * cap;
-    p.parts = 1;
-    while (p.parts < passes && p.parts < 16 && rows * p.parts < 16LL * sm_count()) p.parts *= 2;
-    const long long blocks = std::min((rows * p.parts + kRotaryWarps - 1) / kRotaryWarps, 64LL * sm_count());
+    while ((1 << p.parts_log) < passes && p.parts_log < 4 && (rows << p.parts_log) < 16LL * sm_count()) ++p.parts_log;
+    const long long blocks = std::min(((rows << p.parts_log) + kRotaryWarps - 1) / kRotaryWarps, 3LL * sm_count());
     const dim3 grid((unsigned)blocks);
     const bool half = rope_layout == REGIONE_ROPE_HALF, norm = normalise != 0;
     cudaStream_t st = (cudaStream_t)stream;
