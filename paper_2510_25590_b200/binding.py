@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+from array import array
 from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int64, c_longlong, c_size_t, c_ulonglong, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -594,24 +595,24 @@ def _workspace(device, t):
     return _on(device, t, t.dtype, "workspace"), t.nbytes
 
 
-def _sets(device, tensors, C):
-    """Sets and set distance of the parameters [sets, C] that are given, which have to lie alike, and their addresses."""
+def _sets(device, C, *tensors):
+    """Sets, set distance and addresses of the parameters [sets, C] that are given, which have to lie alike: (tensor, name)."""
     bf = _torch().bfloat16
-    sets, step, at = None, C, []
+    sets, step, at = 0, C, []
     for t, name in tensors:
         if t is None:
             at.append(None)
             continue
-        if sets is None:
+        if not sets:
             _ranks(**{name: (t, 2)})
             sets = t.shape[0]
-        where, apart = _rows(device, t, (sets, C), bf, name)
-        if sets > 1:
-            if step != apart and any(a is not None for a in at):
+            where, step = _rows(device, t, (sets, C), bf, name)
+        else:
+            where, apart = _rows(device, t, (sets, C), bf, name)
+            if apart != step:
                 raise RegionEError(f"the sets of {name} are not as far apart as those of the other parameters")
-            step = apart
         at.append(where)
-    return sets or 1, step, at
+    return (sets or 1, step, *at)
 
 
 def layer_norm(x, weight, bias, row_begin, row_end, out, eps, modulated=False, residual=None, gate=None, x_out=None, mean=None,
@@ -626,26 +627,33 @@ def layer_norm(x, weight, bias, row_begin, row_end, out, eps, modulated=False, r
     bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
     try:
         rows, C = shape = x.shape
-        fits = row_end.shape == row_begin.shape
+        groups = row_begin.shape
+        fits = row_end.shape == groups
     except (AttributeError, ValueError, IndexError):
         _ranks(x=(x, 2), row_begin=(row_begin, None), row_end=(row_end, None))
         raise
     if not fits:
-        _want(row_end, row_begin.shape, "row_end")
-    if (residual is None) != (x_out is None) or residual is None and gate is not None:
-        raise RegionEError("residual and x_out are given together, and a gate only with them")
-    for t, name in ((mean, "mean"), (rstd, "rstd")):
-        if t is not None:
-            _want(t, (rows,), name)
+        _want(row_end, groups, "row_end")
     xp, xs = _rows(at, x, shape, bf, "x")
     op, os_ = _rows(at, out, shape, bf, "out")
-    rp, rs = (None, 0) if residual is None else _rows(at, residual, shape, bf, "residual")
-    zp, zs = (None, 0) if x_out is None else _rows(at, x_out, shape, bf, "x_out")
-    sets, step, (wp, bp, gp) = _sets(at, ((weight, "weight"), (bias, "bias"), (gate, "gate")), C)
+    rp, rs, zp, zs = None, 0, None, 0
+    if residual is not None and x_out is not None:
+        rp, rs = _rows(at, residual, shape, bf, "residual")
+        zp, zs = _rows(at, x_out, shape, bf, "x_out")
+    elif residual is not None or x_out is not None or gate is not None:
+        raise RegionEError("residual and x_out are given together, and a gate only with them")
+    mp = sp = None
+    if mean is not None:
+        _want(mean, (rows,), "mean")
+        mp = _on(at, mean, f32, "mean")
+    if rstd is not None:
+        _want(rstd, (rows,), "rstd")
+        sp = _on(at, rstd, f32, "rstd")
+    sets, step, wp, bp, gp = _sets(at, C, (weight, "weight"), (bias, "bias"), (gate, "gate"))
     _check(load().regione_layer_norm(
         xp, xs, rp, rs, gp, wp, bp, step, 1 if modulated else 0, eps, _on(at, row_begin, i32, "row_begin"),
-        _on(at, row_end, i32, "row_end"), rows, row_begin.numel(), sets, C, zp, zs, op, os_, _on(at, mean, f32, "mean"),
-        _on(at, rstd, f32, "rstd"), _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_layer_norm")
+        _on(at, row_end, i32, "row_end"), rows, groups.numel(), sets, C, zp, zs, op, os_, mp, sp,
+        _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_layer_norm")
 
 
 def layer_norm_backward_workspace(rows, groups, C) -> int:
@@ -671,22 +679,31 @@ def layer_norm_backward(x, mean, rstd, dy, weight, row_begin, row_end, dx, dweig
         _want(row_end, row_begin.shape, "row_end")
     if (residual is None) != (gate is None) or (residual is None) != (dresidual is None) or dgate is not None and residual is None:
         raise RegionEError("residual, gate and dresidual are given together, and dgate only with them")
+    sets, step, wp, gp = _sets(at, C, (weight, "weight"), (gate, "gate"))
+    if weight is None and gate is None:
+        first = dweight if dweight is not None else dbias
+        if first is not None:
+            _ranks(**{"dweight" if dweight is not None else "dbias": (first, 2)})
+            sets = first.shape[0]
     _want(mean, (rows,), "mean")
     _want(rstd, (rows,), "rstd")
-    sets, step, (wp, gp) = _sets(at, ((weight, "weight"), (gate, "gate")), C)
-    if weight is None and gate is None and (dweight is not None or dbias is not None):
-        sets = (dweight if dweight is not None else dbias).shape[0]
+    each = (sets, C)
     for t, name in ((dweight, "dweight"), (dbias, "dbias"), (dgate, "dgate")):
         if t is not None:
-            _want(t, (sets, C), name)
-    rows_of = lambda t, name: (None, 0) if t is None else _rows(at, t, shape, bf, name)
+            _want(t, each, name)
+    xp, xs = _rows(at, x, shape, bf, "x")
+    yp, ys = _rows(at, dy, shape, bf, "dy")
+    dp, ds = _rows(at, dx, shape, bf, "dx")
+    zp, zs = (None, 0) if dx_out is None else _rows(at, dx_out, shape, bf, "dx_out")
+    rp, rs, qp, qs = None, 0, None, 0
+    if residual is not None:
+        rp, rs = _rows(at, residual, shape, bf, "residual")
+        qp, qs = _rows(at, dresidual, shape, bf, "dresidual")
     ws, ws_bytes = _workspace(at, workspace)
     _check(load().regione_layer_norm_backward(
-        *_rows(at, x, shape, bf, "x"), _on(at, mean, f32, "mean"), _on(at, rstd, f32, "rstd"), *_rows(at, dy, shape, bf, "dy"),
-        *rows_of(dx_out, "dx_out"), *rows_of(residual, "residual"), gp, wp, step, 1 if modulated else 0,
-        _on(at, row_begin, i32, "row_begin"), _on(at, row_end, i32, "row_end"), rows, row_begin.numel(), sets, C,
-        *_rows(at, dx, shape, bf, "dx"), *rows_of(dresidual, "dresidual"), _on(at, dweight, f32, "dweight"),
-        _on(at, dbias, f32, "dbias"), _on(at, dgate, f32, "dgate"), ws, ws_bytes,
+        xp, xs, _on(at, mean, f32, "mean"), _on(at, rstd, f32, "rstd"), yp, ys, zp, zs, rp, rs, gp, wp, step, 1 if modulated else 0,
+        _on(at, row_begin, i32, "row_begin"), _on(at, row_end, i32, "row_end"), rows, row_begin.numel(), sets, C, dp, ds, qp, qs,
+        _on(at, dweight, f32, "dweight"), _on(at, dbias, f32, "dbias"), _on(at, dgate, f32, "dgate"), ws, ws_bytes,
         _on(at, dev_status, i32, "dev_status"), _stream(stream)), "regione_layer_norm_backward")
 
 
@@ -699,20 +716,26 @@ def rotary_frequencies(widths, theta=10000.0):
             [a for a, w in enumerate(widths) for _ in range(w // 2)])
 
 
-def _heads(device, t, rows, name):
-    """Address, request and row distance of [B, rows, H, D] whose requests and rows may lie apart."""
-    B, n, H, D = t.shape
-    if t.get_device() != device:
-        _ptr(t, t.dtype, name)
-        raise RegionEError(f"{name} is on {t.device}, which is not the current device")
-    if t.dtype != _torch().bfloat16:
-        raise RegionEError(f"{name} must have dtype torch.bfloat16, got {t.dtype}")
-    if rows is not None and n != rows:
-        _want(t, (B, rows, H, D), name)
-    sb, sr, sh, sd = t.stride()
-    if D > 1 and sd != 1 or H > 1 and sh != D:
-        raise RegionEError(f"the heads of a row of {name} must be contiguous")
-    return t.data_ptr(), sb if B > 1 else 0, sr if n > 1 else H * D
+def _heads(device, t, shape, dtype, name):
+    """Address, request and row distance of [B, rows, H, D] of that shape on that device whose requests and rows may lie apart."""
+    B, rows, H, D = shape
+    try:
+        if t.get_device() == device and t.dtype == dtype and t.shape == shape:
+            sb, sr, sh, sd = t.stride()
+            if (sd == 1 or D == 1) and (sh == D or H == 1):
+                return t.data_ptr(), sb if B > 1 else 0, sr if rows > 1 else H * D
+            raise RegionEError(f"the heads of a row of {name} must be contiguous")
+        if t.is_cuda and t.get_device() != device:
+            raise RegionEError(f"{name} is on {t.device}, which is not the current device")
+    except AttributeError:
+        pass
+    if not isinstance(getattr(t, "shape", None), _torch().Size) or not t.is_cuda:
+        raise RegionEError(f"{name} must be a CUDA tensor")
+    _ranks(**{name: (t, 4)})
+    if t.dtype != dtype:
+        raise RegionEError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    _want(t, shape, name)
+    raise RegionEError(f"{name} cannot be used")
 
 
 def rotary_axes(q, k, positions, freq, axis, q_out, k_out, layout, idx=None, n=None, q_weight=None, k_weight=None, eps=None,
@@ -724,9 +747,9 @@ def rotary_axes(q, k, positions, freq, axis, q_out, k_out, layout, idx=None, n=N
     (``src_compact``).  ``inverse`` turns the other way, which is the gradient of the rotation."""
     torch = _torch()
     at = _here()
-    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    bf, i32 = torch.bfloat16, torch.int32
     try:
-        B, src, Hq, D = q.shape
+        B, src, Hq, D = shape = q.shape
         Bp, places, axes = positions.shape
         cap = q_out.shape[1]
         Hk = 0 if k is None else k.shape[2]
@@ -737,34 +760,43 @@ def rotary_axes(q, k, positions, freq, axis, q_out, k_out, layout, idx=None, n=N
         _want(positions, (B, places, axes), "positions")
     if (k is None) != (k_out is None):
         raise RegionEError("k and k_out are given together")
-    _want(q_out, (B, cap, Hq, D), "q_out")
-    if k is not None:
-        _want(k, (B, src, Hk, D), "k")
-        _want(k_out, (B, cap, Hk, D), "k_out")
-    if idx is not None:
-        _want(idx, (B, cap), "idx")
-    if n is not None:
-        _want(n, (B,), "n")
-    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if t is not None:
-            _want(t, (D,), name)
-            if eps is None:
-                raise RegionEError(f"{name} belongs to the normalisation, which eps asks for")
-    if len(freq) != D // 2 or len(axis) != D // 2:
-        raise RegionEError("freq and axis must have D / 2 entries")
     compact = src_compact or idx is None
     if src != (cap if compact else places) or (idx is None and cap > places):
         raise RegionEError("source rows must match the rows to write (compact) or the places (gathered)")
-    rows = src
-    freq_c, axis_c = (c_double * len(freq))(*freq), (ctypes.c_int32 * len(axis))(*axis)
-    qp, kp = _heads(at, q, rows, "q"), (None, 0, 0) if k is None else _heads(at, k, rows, "k")
-    qo, ko = _heads(at, q_out, cap, "q_out"), (None, 0, 0) if k is None else _heads(at, k_out, cap, "k_out")
+    qp, qb, qr = _heads(at, q, shape, bf, "q")
+    op, ob, or_ = _heads(at, q_out, (B, cap, Hq, D), bf, "q_out")
+    kp, kb, kr, lp, lb, lr = None, 0, 0, None, 0, 0
+    if k is not None:
+        kp, kb, kr = _heads(at, k, (B, src, Hk, D), bf, "k")
+        lp, lb, lr = _heads(at, k_out, (B, cap, Hk, D), bf, "k_out")
+    ip = np_ = qw = kw = None
+    if idx is not None:
+        _want(idx, (B, cap), "idx")
+        ip = _on(at, idx, i32, "idx")
+    if n is not None:
+        _want(n, (B,), "n")
+        np_ = _on(at, n, i32, "n")
+    if eps is None:
+        if q_weight is not None or k_weight is not None:
+            raise RegionEError("q_weight and k_weight belong to the normalisation, which eps asks for")
+    else:
+        if q_weight is not None:
+            _want(q_weight, (D,), "q_weight")
+            qw = _on(at, q_weight, bf, "q_weight")
+        if k_weight is not None:
+            _want(k_weight, (D,), "k_weight")
+            kw = _on(at, k_weight, bf, "k_weight")
+    try:
+        freq, axis = array("d", freq), array("i", axis)
+    except TypeError:
+        raise RegionEError("freq and axis must be sequences of numbers, axis of whole ones") from None
+    if len(freq) != D // 2 or len(axis) != D // 2:
+        raise RegionEError("freq and axis must have D / 2 entries")
     _check(load().regione_rotary_axes(
-        *qp, *kp, _on(at, idx, i32, "idx"), _on(at, n, i32, "n"), _on(at, positions, f32, "positions"),
-        0 if Bp == 1 else places * axes, B, places, cap, Hq, Hk, D, axes, 1 if compact else 0, freq_c, axis_c, int(layout),
-        1 if inverse else 0, 0 if eps is None else 1, _on(at, q_weight, bf, "q_weight"), _on(at, k_weight, bf, "k_weight"),
-        0.0 if eps is None else float(eps), *qo, *ko, _on(at, dev_status, i32, "dev_status"), _stream(stream)),
-        "regione_rotary_axes")
+        qp, qb, qr, kp, kb, kr, ip, np_, _on(at, positions, torch.float32, "positions"), 0 if Bp == 1 else places * axes, B, places, cap,
+        Hq, Hk, D, axes, 1 if compact else 0, freq.buffer_info()[0], axis.buffer_info()[0], layout, 1 if inverse else 0,
+        0 if eps is None else 1, qw, kw, 0.0 if eps is None else eps, op, ob, or_, lp, lb, lr, _on(at, dev_status, i32, "dev_status"),
+        _stream(stream)), "regione_rotary_axes")
 
 
 def fresh_qkv(q_src, k_src, v_src, idx, n, q_weight, k_weight, eps, cos_table, sin_table, rope_layout,
