@@ -98,6 +98,19 @@ struct GroupedControl {
     int16_t widths[kMaxGroups];                       // rows of its tiles, which are even
 };
 
+struct AdapterControl : GroupedControl {
+    int adapter[kMaxGroups];                          // of a group, -1: none
+};
+template <Product OP> constexpr bool kAdapters = OP == Product::kInto || OP == Product::kTail;
+template <Product OP> using ControlOf = std::conditional_t<kAdapters<OP>, AdapterControl, GroupedControl>;
+// The second launch of a product with adapters, which starts ahead of the first one's end (see the kernel).  What it reads before it has
+// waited comes from L2: lines of L1 may be older than the launch in front of the first.
+template <Product OP> constexpr bool kLate = OP == Product::kTail || OP == Product::kJoined;
+template <Product OP, typename T> __device__ __forceinline__ T ld_input(const T* p) {
+    if constexpr (kLate<OP>) return __ldcg(p);
+    else return __ldg(p);
+}
+
 // ---- instructions that the pair of CTAs and the scaled product need -------------------------------------------
 namespace {
 
@@ -287,13 +300,15 @@ template <int N> __device__ __forceinline__ void gelu_tanh(uint64_t (&x)[N]) {
 }
 
 // A group's rows within the buffer; false: the range as given is not within it.
+template <Product OP = Product::kPlain>
 __device__ __forceinline__ bool rows_of(const GroupedArgs& p, int g, int& begin, int& rows) {
-    return cut_range(p.row_begin[g], p.row_end[g], p.rows_cap, begin, rows);
+    if constexpr (kLate<OP>) return cut_range(__ldcg(p.row_begin + g), __ldcg(p.row_end + g), p.rows_cap, begin, rows);
+    else return cut_range(p.row_begin[g], p.row_end[g], p.rows_cap, begin, rows);
 }
 
 // A group's adapter, -1 for none; one that does not exist is none (`in`: false).
-__device__ __forceinline__ int adapter_of(const GroupedArgs& p, int g, bool& in) {
-    const int a = __ldg(p.adapter + g);
+template <Product OP> __device__ __forceinline__ int adapter_of(const GroupedArgs& p, int g, bool& in) {
+    const int a = ld_input<OP>(p.adapter + g);
     in = a >= -1 && a < p.n_adapters;
     return in ? a : -1;
 }
@@ -324,9 +339,8 @@ __device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const Group
     tile.weights = group < p.n_weights ? group : group % p.n_weights;
     tile.feature = (block * 8 + in - at * wide) * (PAIR ? 2 : 1) * kFeat;
     tile.adapter = -1;
-    if constexpr (OP == Product::kInto || OP == Product::kTail) {
-        bool exists;
-        tile.adapter = adapter_of(p, group, exists);
+    if constexpr (kAdapters<OP>) {
+        tile.adapter = static_cast<const AdapterControl*>(ctl)->adapter[group];
         if (OP == Product::kInto) tile.weights = max(tile.adapter, 0);
     }
     return tile;
@@ -337,7 +351,7 @@ __device__ __forceinline__ GroupedTile tile_at(const GroupedArgs& p, const Group
 __device__ __forceinline__ void join_groups(const GroupedArgs& p, GroupedControl* ctl) {
     int16_t* last = ctl->widths;
     bool in = true;
-    for (int g = threadIdx.x; g < p.groups; g += blockDim.x) in = rows_of(p, g, ctl->begin[g], ctl->rows[g]) && in;
+    for (int g = threadIdx.x; g < p.groups; g += blockDim.x) in = rows_of<Product::kJoined>(p, g, ctl->begin[g], ctl->rows[g]) && in;
     if (!in && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
     __syncthreads();
     auto joins = [&](int g) {                         // group g to the set's next one
@@ -480,7 +494,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
     const uint32_t smem = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
     uint8_t* base = smem_raw + (smem - ptx::smem_addr(smem_raw));
     uint8_t* staging = base + p.ring_bytes;
-    GroupedControl* ctl = reinterpret_cast<GroupedControl*>(staging + kEpiWarps * kStagingBytes);
+    ControlOf<OP>* ctl = reinterpret_cast<ControlOf<OP>*>(staging + kEpiWarps * kStagingBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // a cluster has a tile's slices of K, a slice is a CTA or a pair; `half`: which of the pair
     const int cluster = (PAIR ? 2 : 1) * p.slices;
@@ -502,7 +516,10 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
     }
     if (warp == kIssuer) take_tmem<PAIR>(ptx::smem_addr(&ctl->tmem), p.tmem_columns);
     if (warp == kProducer && lane == 0) ptx::prefetch_tensormap(&maps.w);
-    grid_dependency_wait();
+    // The second launch of a product with adapters takes one thing from the first, and waits for it where it is read: the thread that
+    // loads, ahead of the first chunk of the rank, or the threads that add.  Everything else was there before the first launch began,
+    // which waited for it before it let this one in.  (Every CTA waits somewhere: what follows this launch counts on both.)
+    if (!kLate<OP>) grid_dependency_wait();
 
     // ---- plan: from the groups' row counts, which only the device knows --------------------------------------------
     const int f_tiles = (p.N + (PAIR ? 2 : 1) * kFeat - 1) / ((PAIR ? 2 : 1) * kFeat);
@@ -515,10 +532,10 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
             rows = ctl->rows[g];
             return true;
         } else {
-            bool in = rows_of(p, g, begin, rows);
+            bool in = rows_of<OP>(p, g, begin, rows);
             if constexpr (OP == Product::kInto) {
                 bool exists;
-                if (adapter_of(p, g, exists) < 0) rows = 0;
+                if (adapter_of<OP>(p, g, exists) < 0) rows = 0;
                 in = in && exists;
             }
             return in;
@@ -567,6 +584,10 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
                 n = (rows + width - 1) / width;
                 ctl->begin[g] = begin;
                 ctl->rows[g] = rows;
+                if constexpr (kAdapters<OP>) {
+                    bool exists;
+                    ctl->adapter[g] = adapter_of<OP>(p, g, exists);
+                }
                 constexpr int kStep = PAIR ? 32 : 16;
                 if (n > 0) ctl->widths[g] = (int16_t)(((rows + n - 1) / n + kStep - 1) & ~(kStep - 1));
             }
@@ -620,6 +641,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
         const long long t_end = split ? t0 + 1 : total;
         if (warp == kProducer) {
             if (elected) {
+                bool waited = false;
                 for (long long t = t0; t < t_end && ok; t += workers) {
                     const GroupedTile tile = tile_at<PAIR, OP>(p, ctl, (int)t, f_tiles, group);
                     const int c_last = chunks_end(tile);
@@ -633,6 +655,11 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
                         int at = 0;                                                  // boxes that make up the rows, the largest first
                         if constexpr (OP == Product::kTail) {
                             if (c >= p.chunks) {
+                                if (!waited) {
+                                    grid_dependency_wait();
+                                    asm volatile("fence.proxy.async.global;" ::: "memory");
+                                    waited = true;
+                                }
                                 const int j = (c - p.chunks) * kElems;
                                 load_w<PAIR>(dst, &maps.b, bar, j, feature, tile.adapter);
 #pragma unroll
@@ -728,7 +755,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int f = min(feature + (lane >> 2) + 8 * i, p.N - 1);
-                        const float b = __uint_as_float((uint32_t)__ldg(p.bias + (size_t)tile.weights * p.N + f) << 16);
+                        const float b = __uint_as_float((uint32_t)ld_input<OP>(p.bias + (size_t)tile.weights * p.N + f) << 16);
                         bias[i] = pair_of(b, b);
                     }
                 const float scale = OP == Product::kInto && p.adapter_scale != nullptr ? __ldg(p.adapter_scale + tile.weights) : 1.0f;
@@ -754,6 +781,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
                         tmem_ld_16x256b_x2(acc + (16u << 16) + c, ahead + 8);
                     };
                     if (part * 16 < tile.live) fetch(part * 16);
+                    if (OP == Product::kJoined) grid_dependency_wait();
                     for (int c = part * 16; c < tile.live; c += kEpiCols) {
                         uint64_t y[8];                                               // two rows of one feature
                         ptx::tmem_wait_ld();
@@ -818,6 +846,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
             if (warp < kEpiWarps && !ctl->abort_flag) {
                 const GroupedTile tile = tile_at<PAIR, OP>(p, ctl, (int)t0, f_tiles, group);
                 const float scale = OP == Product::kInto && p.adapter_scale != nullptr ? __ldg(p.adapter_scale + tile.weights) : 1.0f;
+                if (OP == Product::kJoined) grid_dependency_wait();
                 // pieces of 8 features of a row, dealt over the slices' threads; slices are added in their order
                 for (int u = threadIdx.x * p.slices + slice; u < tile.live * (kFeat / 8); u += kEpiWarps * 32 * p.slices) {
                     const int q = u / (kFeat / 8), j = u % (kFeat / 8), f = tile.feature + half * kFeat + 8 * j;
@@ -843,7 +872,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
                         }
                     }
                     if (p.bias != nullptr) {
-                        const uint4 b = ldg128(p.bias + (size_t)tile.weights * p.N + f);
+                        const uint4 b = ld_input<OP>(reinterpret_cast<const uint4*>(p.bias + (size_t)tile.weights * p.N + f));
                         y[0] += bf16_lo(b.x); y[1] += bf16_hi(b.x); y[2] += bf16_lo(b.y); y[3] += bf16_hi(b.y);
                         y[4] += bf16_lo(b.z); y[5] += bf16_hi(b.z); y[6] += bf16_lo(b.w); y[7] += bf16_hi(b.w);
                     }
@@ -873,6 +902,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
         }
     }
 
+    if (kLate<OP>) grid_dependency_wait();
     if (PAIR && warp < kEpiWarps && lane == 0) ptx::bulk_wait_all();
     __syncwarp();
     if ((PAIR || split) && (threadIdx.x & 31) == 0 && *(volatile int*)&ctl->abort_flag)
@@ -944,12 +974,12 @@ static bool grouped_map(CUtensorMap* map, bool fp4, int rank, const void* at, lo
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool FP4, bool PAIR> static size_t grouped_smem(int ring_bytes) {
-    return 1024 + ring_bytes + Roles<FP4, PAIR>::kEpi * kStagingBytes + sizeof(GroupedControl);
+template <bool FP4, bool PAIR, Product OP> static size_t grouped_smem(int ring_bytes) {
+    return 1024 + ring_bytes + Roles<FP4, PAIR>::kEpi * kStagingBytes + sizeof(ControlOf<OP>);
 }
 // One CTA on an SM of a pair, two without.
 constexpr int kSmemCta = 232448, kSmemHalf = 113 * 1024;
-template <bool FP4, bool PAIR> static int grouped_ring(int smem) { return (smem - (int)grouped_smem<FP4, PAIR>(0)) & ~1023; }
+template <bool FP4, bool PAIR, Product OP> static int grouped_ring(int smem) { return (smem - (int)grouped_smem<FP4, PAIR, OP>(0)) & ~1023; }
 
 template <bool FP4, bool PAIR> static void grouped_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, unsigned blocks, int cluster,
                                                           size_t smem, cudaStream_t st) {
@@ -972,7 +1002,7 @@ template <bool FP4, bool VEC, Product OP> static const int* grouped_pairs(int de
     static int held[kMaxDevices][4] = {};
     int* h = held[dev];
     if (__atomic_load_n(&h[3], __ATOMIC_ACQUIRE)) return h;
-    const size_t smem = grouped_smem<FP4, true>(grouped_ring<FP4, true>(kSmemCta));
+    const size_t smem = grouped_smem<FP4, true, OP>(grouped_ring<FP4, true, OP>(kSmemCta));
     if (cudaFuncSetAttribute(grouped_kernel<FP4, true, VEC, OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess ||
         cudaFuncSetAttribute(grouped_kernel<FP4, false, VEC, OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta) != cudaSuccess)
         return nullptr;
@@ -996,7 +1026,7 @@ static int grouped_launch(const MapsOf<OP>& maps, const GroupedArgs& p, int clus
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     const int cluster = (PAIR ? 2 : 1) * p.slices;
-    grouped_config<FP4, PAIR>(cfg, attr, (unsigned)(clusters * cluster), cluster, grouped_smem<FP4, PAIR>(p.ring_bytes), st);
+    grouped_config<FP4, PAIR>(cfg, attr, (unsigned)(clusters * cluster), cluster, grouped_smem<FP4, PAIR, OP>(p.ring_bytes), st);
     return launch_status(launch_counted(&cfg, grouped_kernel<FP4, PAIR, VEC, OP>, maps, p));
 }
 
@@ -1053,13 +1083,13 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
     }
     if (pair && clusters == 0) return REGIONE_CUDA_ERROR;
     if (pair) {
-        p.ring_bytes = grouped_ring<FP4, true>(kSmemCta);
+        p.ring_bytes = grouped_ring<FP4, true, OP>(kSmemCta);
         p.tmem_columns = 512;
         p.scale_column = 448;
     } else {
         // two CTAs an SM where four stages (see the scales) leave room for them, with a slice's chunks in the ring if they fit
         const int stage = kTileBytes + p.width * kChunkBytes + (FP4 ? kScaleA + kScaleB : 0), mine = (p.chunks + p.slices - 1) / p.slices;
-        p.ring_bytes = std::max(4 * stage, std::min(grouped_ring<FP4, false>(kSmemHalf), std::min(kMaxStages, mine) * stage));
+        p.ring_bytes = std::max(4 * stage, std::min(grouped_ring<FP4, false, OP>(kSmemHalf), std::min(kMaxStages, mine) * stage));
         p.scale_column = p.width <= 64 ? 64 : 128;
         p.tmem_columns = FP4 ? 2 * p.scale_column : std::max(32, p.width);
     }

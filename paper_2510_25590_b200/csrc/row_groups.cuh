@@ -14,7 +14,8 @@ struct RowGroups {
     int begin[kMaxRowGroups];
 };
 
-// Fills the table (one warp adds up, then a barrier of the block).  No more rows are counted than the buffer has, which ranges without a
+// Fills the table (one warp adds up, then a barrier of the block), from L2, since a kernel may do so before it has waited for the one
+// in front of it.  No more rows are counted than the buffer has, which ranges without a
 // common row do not reach: numbers stay within 32 bits, whatever the ranges are.
 __device__ __forceinline__ int fill_row_groups(RowGroups* t, const int32_t* row_begin, const int32_t* row_end, int groups, int cap,
                                                bool reports, int32_t* dev_status) {
@@ -25,7 +26,7 @@ __device__ __forceinline__ int fill_row_groups(RowGroups* t, const int32_t* row_
             const int g = g0 + lane;
             int begin = 0, rows = 0;
             bool in = true;
-            if (g < groups) in = cut_range(row_begin[g], row_end[g], cap, begin, rows);
+            if (g < groups) in = cut_range(__ldcg(row_begin + g), __ldcg(row_end + g), cap, begin, rows);
             int sum = rows;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
