@@ -11,9 +11,10 @@
 // accumulators: the adapter's part is never rounded, written or read on its own.
 //
 // Groups of a row or two (a token each): tiles of their own would read W once per group.  The adapters' part comes first here, in
-// fp32, by this file's kernel: a cluster of eight CTAs has a group, each CTA an eighth of K for the first factor (partial sums
-// meet over distributed shared memory, added in the order of the CTAs) and an eighth of N for the second.  It is bound by reading A and B.  The
-// product with W then takes groups that lie side by side as one and adds that part in its epilogue.
+// fp32, by this file's kernel: a cluster of eight CTAs has eight rows with the same adapter, each CTA an eighth of K for the first factor
+// (partial sums meet over distributed shared memory, added in the order of the CTAs) and an eighth of N for the second.  It is
+// bound by the latency of its steps and by reading A and B.  The product with W, which runs beside it, takes groups that lie side by
+// side as one and adds that part in its epilogue.
 #include "adapters.cuh"
 #include "grouped_plan.cuh"
 #include "sm100_ptx.cuh"
@@ -22,22 +23,44 @@
 
 namespace regione {
 
-constexpr int kMaxRank = 256;
-constexpr int kPartCtas = 8, kPartThreads = 256, kPartRows = 4;
+constexpr int kMaxRank = 256, kMaxAdapterGroups = 512;
+constexpr int kPartCtas = 8, kPartThreads = 256, kPartWarps = kPartThreads / 32, kPartRows = 8;
 
-__device__ __forceinline__ void fma8(const uint4& a, const uint4& b, float& sum) {
-    sum = fmaf(bf16_lo(a.x), bf16_lo(b.x), sum); sum = fmaf(bf16_hi(a.x), bf16_hi(b.x), sum);
-    sum = fmaf(bf16_lo(a.y), bf16_lo(b.y), sum); sum = fmaf(bf16_hi(a.y), bf16_hi(b.y), sum);
-    sum = fmaf(bf16_lo(a.z), bf16_lo(b.z), sum); sum = fmaf(bf16_hi(a.z), bf16_hi(b.z), sum);
-    sum = fmaf(bf16_lo(a.w), bf16_lo(b.w), sum); sum = fmaf(bf16_hi(a.w), bf16_hi(b.w), sum);
+// D = A B + D of 16 x 16 by 16 x 8 bf16 numbers.  (Eight rows at a time: the tensor core's large tiles would stand almost empty.)
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 32 elements of the contraction, of which a lane has the eight of its place among four in one load: in which order they are added does not
+// matter as long as both operands have the same.  lo, hi: rows l / 4 and l / 4 + 8 of A; b: row l / 4 of B.
+__device__ __forceinline__ void mma_32(float (&d)[4], const uint4& lo, const uint4& hi, const uint4& b) {
+    mma_16x8x16(d, lo.x, hi.x, lo.y, hi.y, b.x, b.y);
+    mma_16x8x16(d, lo.z, hi.z, lo.w, hi.w, b.z, b.w);
 }
 
-// addend[r, :] = s_a (x[r] A_a^T) B_a^T for the rows of every group, zeros without an adapter.
-__global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid_constant__ AdapterCall p, float* __restrict__ addend) {
-    __shared__ __align__(16) float partial[2][kPartRows][kMaxRank], u[kPartRows][kMaxRank];
+// What two numbers are above those that they were rounded to.  (Infinite ones: nothing.)
+__device__ __forceinline__ uint32_t rest_of(float x, float y, uint32_t rounded) {
+    const float a = bf16_lo(rounded), b = bf16_hi(rounded);
+    return pack_bf16x2(isinf(a) ? 0.f : x - a, isinf(b) ? 0.f : y - b);
+}
+
+struct PartMemory {
+    float sums[2][kPartRows][kMaxRank];               // this CTA's part of u = x A^T, in turns
+    float parts[kPartWarps * 16][kPartRows + 1];      // of a warp, before the warps with the same ranks are added
+    uint16_t u_hi[kPartRows][kMaxRank + 8], u_lo[kPartRows][kMaxRank + 8];
+    int begin[kMaxAdapterGroups], first[kMaxAdapterGroups + 1];      // the adapter's groups: their rows, numbered through
+    int warp_rows[kPartWarps], warp_groups[kPartWarps];
+    int place, groups;                                // of this cluster's group among them, how many
+};
+
+// addend[r, :] = s_a (x[r] A_a^T) B_a^T for the rows of every group, zeros without an adapter.  A cluster to a group, or `subs`; the clusters
+// of all groups with an adapter deal its rows out eight at a time, so that A and B are read once for eight rows wherever those are.
+__global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid_constant__ AdapterCall p, float* __restrict__ addend, int subs) {
+    __shared__ __align__(16) PartMemory m;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int g = blockIdx.x / kPartCtas, cta = blockIdx.x % kPartCtas, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cluster = blockIdx.x / kPartCtas, cta = blockIdx.x % kPartCtas, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = cluster / subs, sub = cluster - g * subs;
     int begin, rows;
     const bool in = cut_range(p.row_begin[g], p.row_end[g], p.rows_cap, begin, rows);
     int a = p.adapter[g];
@@ -46,62 +69,140 @@ __global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid
     if (!exists) a = -1;
     const int n0 = p.N / 8 * cta / kPartCtas * 8, n1 = p.N / 8 * (cta + 1) / kPartCtas * 8;       // features of this CTA
     if (a < 0) {                                      // (the whole cluster)
-        for (int r = 0; r < rows; ++r)
+        for (int r = sub; r < rows; r += subs)
             for (int f = n0 + threadIdx.x * 4; f < n1; f += kPartThreads * 4)
                 *reinterpret_cast<float4*>(addend + (size_t)(begin + r) * p.N + f) = make_float4(0.f, 0.f, 0.f, 0.f);
         return;
     }
+    const uint16_t* factor_b = p.b + ((size_t)a * p.N + n0) * p.rank;
+    if (threadIdx.x == 0 && n1 > n0)                  // (read in the second half; contiguous)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(factor_b), "r"((n1 - n0) * p.rank * 2) : "memory");
+
+    // ---- the groups with this adapter, in order ----------------------------------------------------------------------------------
+    {
+        constexpr int kEach = kMaxAdapterGroups / kPartThreads;
+        int of_begin[kEach], of_rows[kEach], mine = 0, mine_rows = 0;
+        bool same[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int other = threadIdx.x * kEach + i;
+            same[i] = other < p.groups && p.adapter[other] == a;
+            of_begin[i] = of_rows[i] = 0;
+            if (same[i]) cut_range(p.row_begin[other], p.row_end[other], p.rows_cap, of_begin[i], of_rows[i]);
+            mine += same[i];
+            mine_rows += of_rows[i];
+        }
+        int at = mine, at_rows = mine_rows;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, at, d), up_rows = __shfl_up_sync(0xffffffffu, at_rows, d);
+            if (lane >= d) { at += up; at_rows += up_rows; }
+        }
+        if (lane == 31) { m.warp_groups[warp] = at; m.warp_rows[warp] = at_rows; }
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) { at += m.warp_groups[w]; at_rows += m.warp_rows[w]; }
+        if (threadIdx.x == kPartThreads - 1) {
+            m.groups = at;
+            m.first[at] = min(at_rows, p.rows_cap);   // (more only where ranges overlap)
+        }
+        at -= mine;
+        at_rows -= mine_rows;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (same[i]) {
+                m.begin[at] = of_begin[i];
+                m.first[at] = min(at_rows, p.rows_cap);
+                if (threadIdx.x * kEach + i == g) m.place = at;
+                ++at;
+                at_rows += of_rows[i];
+            }
+        __syncthreads();
+    }
+    const int total = m.first[m.groups];
     const int k0 = p.K / 8 * cta / kPartCtas, k1 = p.K / 8 * (cta + 1) / kPartCtas;               // pieces of 8 of K
     const float scale = p.scale != nullptr ? p.scale[a] : 1.0f;
-    for (int r0 = 0, turn = 0; r0 < rows; r0 += kPartRows, turn ^= 1) {
-        const int live = min(kPartRows, rows - r0);
-        const uint16_t* x = p.x + (size_t)(begin + r0) * p.x_stride;
-        for (int j = warp; j < p.rank; j += kPartThreads / 32) {
-            const uint16_t* row = p.a + ((size_t)a * p.rank + j) * p.K;
-            float sum[kPartRows] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-            for (int k = k0 + lane; k < k1; k += 32) {
-                const uint4 w = ldg128(row + k * 8);
-#pragma unroll
-                for (int r = 0; r < kPartRows; ++r)
-                    if (r < live) fma8(w, ldg128(x + r * p.x_stride + k * 8), sum[r]);
+    const int tiles = (p.rank + 15) / 16, k_parts = tiles >= kPartWarps ? 1 : kPartWarps / tiles;  // warps that share 16 ranks
+    const int piece = lane & 3, row_of = lane >> 2;
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    int turn = 0;
+    for (long long c = m.place * subs + sub; c * kPartRows < total; c += m.groups * subs, turn ^= 1) {
+        auto buffer_row = [&](int i) {                // of the i-th row of this round, -1 behind the last
+            const int v = (int)(c * kPartRows) + i;
+            if (v >= total) return -1;
+            int lo = 0, hi = m.groups - 1;            // the last group whose first row is not behind v
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (m.first[mid] <= v) lo = mid; else hi = mid - 1;
             }
-#pragma unroll
-            for (int r = 0; r < kPartRows; ++r) {
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], d);
-                if (lane == 0) partial[turn][r][j] = sum[r];
+            return m.begin[lo] + v - m.first[lo];
+        };
+        // ---- u = x A^T over this CTA's part of K ---------------------------------------------------------------------------
+        const int from = buffer_row(row_of);
+        const uint16_t* x = p.x + (size_t)max(from, 0) * p.x_stride;
+        for (int tile0 = 0; tile0 < tiles; tile0 += kPartWarps / k_parts) {
+            const int tile = tile0 + warp / k_parts, k_part = warp % k_parts;
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
+            if (tile < tiles && warp / k_parts < kPartWarps / k_parts) {
+                const int j = tile * 16 + row_of;
+                const uint16_t* lo = p.a + ((size_t)a * p.rank + j) * p.K;
+                const uint16_t* hi = lo + (size_t)8 * p.K;
+                const bool in_lo = j < p.rank, in_hi = j + 8 < p.rank;
+#pragma unroll 4
+                for (int k = k0 + k_part * 4 + piece; k < k1 + piece; k += 4 * k_parts) {         // (all lanes as often: k - piece is the warp's)
+                    const bool in_k = k < k1;
+                    mma_32(d, in_k && in_lo ? ldg128(lo + k * 8) : none, in_k && in_hi ? ldg128(hi + k * 8) : none,
+                           in_k && from >= 0 ? ldg128(x + k * 8) : none);
+                }
             }
+            // ranks row_of, row_of + 8 of the tile; rows 2 piece, 2 piece + 1
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m.parts[warp * 16 + row_of + 8 * (i >> 1)][2 * piece + (i & 1)] = d[i];
+            __syncthreads();
+            for (int i = threadIdx.x; i < kPartWarps / k_parts * 16 * kPartRows; i += kPartThreads) {
+                const int r = i & (kPartRows - 1), q = i / kPartRows, of = q >> 4, j = (tile0 + of) * 16 + (q & 15);
+                float sum = 0.f;
+                for (int w = 0; w < k_parts; ++w) sum += m.parts[(of * k_parts + w) * 16 + (q & 15)][r];
+                if (j < p.rank) m.sums[turn][r][j] = sum;
+            }
+            if (tile0 + kPartWarps / k_parts < tiles) __syncthreads();
         }
         ptx::cluster_sync();
+        // ---- the CTAs' parts, in their order; u as the sum of two bf16 numbers, 2^-16 off -----------------------------------------
         for (int i = threadIdx.x; i < kPartRows * (p.rank / 4); i += kPartThreads) {
             const int r = i / (p.rank / 4), j = 4 * (i - r * (p.rank / 4));
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int c = 0; c < kPartCtas; ++c) {
-                const float4 part = ptx::ld_cluster_f4(ptx::map_rank(ptx::smem_addr(&partial[turn][r][j]), c));
+            for (int q = 0; q < kPartCtas; ++q) {
+                const float4 part = ptx::ld_cluster_f4(ptx::map_rank(ptx::smem_addr(&m.sums[turn][r][j]), q));
                 sum.x += part.x; sum.y += part.y; sum.z += part.z; sum.w += part.w;
             }
-            *reinterpret_cast<float4*>(&u[r][j]) = make_float4(sum.x * scale, sum.y * scale, sum.z * scale, sum.w * scale);
+            sum.x *= scale; sum.y *= scale; sum.z *= scale; sum.w *= scale;
+            const uint32_t h0 = pack_bf16x2(sum.x, sum.y), h1 = pack_bf16x2(sum.z, sum.w);
+            *reinterpret_cast<uint2*>(&m.u_hi[r][j]) = make_uint2(h0, h1);
+            *reinterpret_cast<uint2*>(&m.u_lo[r][j]) = make_uint2(rest_of(sum.x, sum.y, h0), rest_of(sum.z, sum.w, h1));
         }
         __syncthreads();
-        for (int f = n0 + threadIdx.x; f < n1; f += kPartThreads) {
-            const uint16_t* row = p.b + ((size_t)a * p.N + f) * p.rank;
-            float y[kPartRows] = {0.f, 0.f, 0.f, 0.f};
+        // ---- times B^T, 16 features to a warp at a time ------------------------------------------------------------------------------
+        const int to0 = buffer_row(2 * piece), to1 = buffer_row(2 * piece + 1);
+#pragma unroll 2
+        for (int f0 = warp * 16; f0 < n1 - n0; f0 += kPartWarps * 16) {
+            const uint16_t* lo = factor_b + (size_t)(f0 + row_of) * p.rank;
+            const uint16_t* hi = lo + 8 * p.rank;
+            const bool in_hi = f0 + 8 < n1 - n0;      // (features come in eights)
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-            for (int j = 0; j < p.rank; j += 8) {
-                const uint4 w = ldg128(row + j);
-                const float v[8] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y), bf16_lo(w.z), bf16_hi(w.z), bf16_lo(w.w), bf16_hi(w.w)};
-#pragma unroll
-                for (int r = 0; r < kPartRows; ++r) {
-                    const float4 lo = *reinterpret_cast<const float4*>(&u[r][j]), hi = *reinterpret_cast<const float4*>(&u[r][j + 4]);
-                    y[r] = fmaf(v[0], lo.x, y[r]); y[r] = fmaf(v[1], lo.y, y[r]); y[r] = fmaf(v[2], lo.z, y[r]); y[r] = fmaf(v[3], lo.w, y[r]);
-                    y[r] = fmaf(v[4], hi.x, y[r]); y[r] = fmaf(v[5], hi.y, y[r]); y[r] = fmaf(v[6], hi.z, y[r]); y[r] = fmaf(v[7], hi.w, y[r]);
-                }
+            for (int j0 = 0; j0 < p.rank; j0 += 32) {
+                const int j = j0 + piece * 8;
+                const bool in_j = j < p.rank;
+                const uint4 b_lo = in_j ? ldg128(lo + j) : none, b_hi = in_j && in_hi ? ldg128(hi + j) : none;
+                mma_32(d, b_lo, b_hi, in_j ? *reinterpret_cast<const uint4*>(&m.u_hi[row_of][j]) : none);
+                mma_32(d, b_lo, b_hi, in_j ? *reinterpret_cast<const uint4*>(&m.u_lo[row_of][j]) : none);
             }
-#pragma unroll
-            for (int r = 0; r < kPartRows; ++r)
-                if (r < live) addend[(size_t)(begin + r0 + r) * p.N + f] = y[r];
+            const int f = n0 + f0 + row_of;
+            if (to0 >= 0) addend[(size_t)to0 * p.N + f] = d[0];
+            if (to1 >= 0) addend[(size_t)to1 * p.N + f] = d[1];
+            if (to0 >= 0 && in_hi) addend[(size_t)to0 * p.N + f + 8] = d[2];
+            if (to1 >= 0 && in_hi) addend[(size_t)to1 * p.N + f + 8] = d[3];
         }
         __syncthreads();                              // (u is written again)
     }
@@ -146,7 +247,8 @@ extern "C" int regione_adapter_matmul(const regione_bf16* x, int64_t x_stride, c
     }
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
-    cfg.gridDim = dim3(groups * kPartCtas);
+    const int subs = std::max(1, std::min(4, (rows_cap + groups * kPartRows - 1) / (groups * kPartRows)));
+    cfg.gridDim = dim3(groups * subs * kPartCtas);
     cfg.blockDim = dim3(kPartThreads);
     cfg.stream = st;
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -156,7 +258,7 @@ extern "C" int regione_adapter_matmul(const regione_bf16* x, int64_t x_stride, c
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const cudaError_t e = launch_counted(&cfg, adapter_part_kernel, c, (float*)workspace);
+    const cudaError_t e = launch_counted(&cfg, adapter_part_kernel, c, (float*)workspace, subs);
     if (e != cudaSuccess) return launch_status(e);
     return adapters_joined(c, (const float*)workspace, st);
 }
