@@ -44,54 +44,68 @@ __device__ __forceinline__ uint32_t rest_of(float x, float y, uint32_t rounded) 
     return pack_bf16x2(isinf(a) ? 0.f : x - a, isinf(b) ? 0.f : y - b);
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 struct PartMemory {
-    float sums[2][kPartRows][kMaxRank];               // this CTA's part of u = x A^T, in turns
+    float sums[kPartRows][kMaxRank];                  // this CTA's part of u = x A^T
     float parts[kPartWarps * 16][kPartRows + 1];      // of a warp, before the warps with the same ranks are added
     uint16_t u_hi[kPartRows][kMaxRank + 8], u_lo[kPartRows][kMaxRank + 8];
+    int begin_of[kMaxAdapterGroups], rows_of[kMaxAdapterGroups], adapter_of[kMaxAdapterGroups];      // of all groups
     int begin[kMaxAdapterGroups], first[kMaxAdapterGroups + 1];      // the adapter's groups: their rows, numbered through
     int warp_rows[kPartWarps], warp_groups[kPartWarps];
     int place, groups;                                // of this cluster's group among them, how many
 };
 
-// addend[r, :] = s_a (x[r] A_a^T) B_a^T for the rows of every group, zeros without an adapter.  A cluster to a group, or `subs`; the clusters
-// of all groups with an adapter deal its rows out eight at a time, so that A and B are read once for eight rows wherever those are.
-__global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid_constant__ AdapterCall p, float* __restrict__ addend, int subs) {
+// addend[r, :] = s_a (x[r] A_a^T) B_a^T for the rows of every group, zeros without an adapter.  There are `subs` clusters to a group; those of
+// all groups with an adapter deal its rows out eight at a time, so that A and B are read once for eight rows wherever those are, and most
+// clusters have nothing to do where many groups share few adapters.  (Few clusters that go through the groups take longer, 256 groups
+// with 24 adapters 48 us instead of 37: which of them have rows is uneven.)  72 registers leave room for the product beside it.
+__global__ void __launch_bounds__(kPartThreads, 3) adapter_part_kernel(const __grid_constant__ AdapterCall p, float* __restrict__ addend, int subs) {
     __shared__ __align__(16) PartMemory m;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int cluster = blockIdx.x / kPartCtas, cta = blockIdx.x % kPartCtas, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int g = cluster / subs, sub = cluster - g * subs;
-    int begin, rows;
-    const bool in = cut_range(p.row_begin[g], p.row_end[g], p.rows_cap, begin, rows);
-    int a = p.adapter[g];
-    const bool exists = a >= -1 && a < p.n_adapters;
-    if ((!in || !exists) && cta == 0 && threadIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
-    if (!exists) a = -1;
+    const int cta = blockIdx.x % kPartCtas, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kEach = kMaxAdapterGroups / kPartThreads;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int g = threadIdx.x * kEach + i;
+        int a = -1, begin = 0, rows = 0;
+        if (g < p.groups) {
+            a = p.adapter[g];
+            const bool in = cut_range(p.row_begin[g], p.row_end[g], p.rows_cap, begin, rows);
+            const bool exists = a >= -1 && a < p.n_adapters;
+            if ((!in || !exists) && blockIdx.x == 0) record_status(p.dev_status, REGIONE_DEV_BOUNDS);
+            if (!exists) a = -1;
+        }
+        m.adapter_of[g] = a;
+        m.begin_of[g] = begin;
+        m.rows_of[g] = rows;
+    }
+    __syncthreads();
     const int n0 = p.N / 8 * cta / kPartCtas * 8, n1 = p.N / 8 * (cta + 1) / kPartCtas * 8;       // features of this CTA
+    const int k0 = p.K / 8 * cta / kPartCtas, k1 = p.K / 8 * (cta + 1) / kPartCtas;               // pieces of 8 of K
+    const int tiles = (p.rank + 15) / 16, k_parts = tiles >= kPartWarps ? 1 : kPartWarps / tiles;  // warps that share 16 ranks
+    const int piece = lane & 3, row_of = lane >> 2;
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    bool entered = false;
+    const int item = blockIdx.x / kPartCtas;
+    const int g = item / subs, sub = item - g * subs, a = m.adapter_of[g];
     if (a < 0) {                                      // (the whole cluster)
-        for (int r = sub; r < rows; r += subs)
+        for (int r = sub; r < m.rows_of[g]; r += subs)
             for (int f = n0 + threadIdx.x * 4; f < n1; f += kPartThreads * 4)
-                *reinterpret_cast<float4*>(addend + (size_t)(begin + r) * p.N + f) = make_float4(0.f, 0.f, 0.f, 0.f);
+                *reinterpret_cast<float4*>(addend + (size_t)(m.begin_of[g] + r) * p.N + f) = make_float4(0.f, 0.f, 0.f, 0.f);
         return;
     }
-    const uint16_t* factor_b = p.b + ((size_t)a * p.N + n0) * p.rank;
-    if (threadIdx.x == 0 && n1 > n0)                  // (read in the second half; contiguous)
-        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(factor_b), "r"((n1 - n0) * p.rank * 2) : "memory");
-
     // ---- the groups with this adapter, in order ----------------------------------------------------------------------------------
     {
-        constexpr int kEach = kMaxAdapterGroups / kPartThreads;
-        int of_begin[kEach], of_rows[kEach], mine = 0, mine_rows = 0;
-        bool same[kEach];
+        int mine = 0, mine_rows = 0;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int other = threadIdx.x * kEach + i;
-            same[i] = other < p.groups && p.adapter[other] == a;
-            of_begin[i] = of_rows[i] = 0;
-            if (same[i]) cut_range(p.row_begin[other], p.row_end[other], p.rows_cap, of_begin[i], of_rows[i]);
-            mine += same[i];
-            mine_rows += of_rows[i];
-        }
+        for (int i = 0; i < kEach; ++i)
+            if (m.adapter_of[threadIdx.x * kEach + i] == a) {
+                ++mine;
+                mine_rows += m.rows_of[threadIdx.x * kEach + i];
+            }
         int at = mine, at_rows = mine_rows;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -108,24 +122,25 @@ __global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid
         at -= mine;
         at_rows -= mine_rows;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            if (same[i]) {
-                m.begin[at] = of_begin[i];
+        for (int i = 0; i < kEach; ++i) {
+            const int other = threadIdx.x * kEach + i;
+            if (m.adapter_of[other] == a) {
+                m.begin[at] = m.begin_of[other];
                 m.first[at] = min(at_rows, p.rows_cap);
-                if (threadIdx.x * kEach + i == g) m.place = at;
+                if (other == g) m.place = at;
                 ++at;
-                at_rows += of_rows[i];
+                at_rows += m.rows_of[other];
             }
+        }
         __syncthreads();
     }
-    const int total = m.first[m.groups];
-    const int k0 = p.K / 8 * cta / kPartCtas, k1 = p.K / 8 * (cta + 1) / kPartCtas;               // pieces of 8 of K
+    const uint16_t* factor_b = p.b + ((size_t)a * p.N + n0) * p.rank;
     const float scale = p.scale != nullptr ? p.scale[a] : 1.0f;
-    const int tiles = (p.rank + 15) / 16, k_parts = tiles >= kPartWarps ? 1 : kPartWarps / tiles;  // warps that share 16 ranks
-    const int piece = lane & 3, row_of = lane >> 2;
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-    int turn = 0;
-    for (long long c = m.place * subs + sub; c * kPartRows < total; c += m.groups * subs, turn ^= 1) {
+    const int total = m.first[m.groups];
+    const long long first_round = m.place * subs + sub;
+    if (first_round * kPartRows < total && threadIdx.x == 0 && n1 > n0)      // (read in the second half; contiguous)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(factor_b), "r"((n1 - n0) * p.rank * 2) : "memory");
+    for (long long c = first_round; c * kPartRows < total; c += m.groups * subs) {
         auto buffer_row = [&](int i) {                // of the i-th row of this round, -1 behind the last
             const int v = (int)(c * kPartRows) + i;
             if (v >= total) return -1;
@@ -136,6 +151,7 @@ __global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid
             }
             return m.begin[lo] + v - m.first[lo];
         };
+        if (entered) cluster_wait();                  // (all have read what this CTA left in the round before)
         // ---- u = x A^T over this CTA's part of K ---------------------------------------------------------------------------
         const int from = buffer_row(row_of);
         const uint16_t* x = p.x + (size_t)max(from, 0) * p.x_stride;
@@ -147,11 +163,19 @@ __global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid
                 const uint16_t* lo = p.a + ((size_t)a * p.rank + j) * p.K;
                 const uint16_t* hi = lo + (size_t)8 * p.K;
                 const bool in_lo = j < p.rank, in_hi = j + 8 < p.rank;
-#pragma unroll 4
-                for (int k = k0 + k_part * 4 + piece; k < k1 + piece; k += 4 * k_parts) {         // (all lanes as often: k - piece is the warp's)
-                    const bool in_k = k < k1;
-                    mma_32(d, in_k && in_lo ? ldg128(lo + k * 8) : none, in_k && in_hi ? ldg128(hi + k * 8) : none,
-                           in_k && from >= 0 ? ldg128(x + k * 8) : none);
+                constexpr int kBatch = 2;             // loads of a lane, of each operand, that are on their way at one time
+                for (int k = k0 + k_part * 4; k < k1; k += kBatch * 4 * k_parts) {
+                    uint4 v_lo[kBatch], v_hi[kBatch], v_x[kBatch];        // (all loads of a batch ahead of its products)
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const int at = k + i * 4 * k_parts + piece;
+                        const bool in_k = at < k1;
+                        v_lo[i] = in_k && in_lo ? ldg128(lo + at * 8) : none;
+                        v_hi[i] = in_k && in_hi ? ldg128(hi + at * 8) : none;
+                        v_x[i] = in_k && from >= 0 ? ldg128(x + at * 8) : none;
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) mma_32(d, v_lo[i], v_hi[i], v_x[i]);
                 }
             }
             // ranks row_of, row_of + 8 of the tile; rows 2 piece, 2 piece + 1
@@ -162,18 +186,20 @@ __global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid
                 const int r = i & (kPartRows - 1), q = i / kPartRows, of = q >> 4, j = (tile0 + of) * 16 + (q & 15);
                 float sum = 0.f;
                 for (int w = 0; w < k_parts; ++w) sum += m.parts[(of * k_parts + w) * 16 + (q & 15)][r];
-                if (j < p.rank) m.sums[turn][r][j] = sum;
+                if (j < p.rank) m.sums[r][j] = sum;
             }
             if (tile0 + kPartWarps / k_parts < tiles) __syncthreads();
         }
-        ptx::cluster_sync();
+        cluster_arrive();
+        cluster_wait();
+        entered = true;
         // ---- the CTAs' parts, in their order; u as the sum of two bf16 numbers, 2^-16 off -----------------------------------------
         for (int i = threadIdx.x; i < kPartRows * (p.rank / 4); i += kPartThreads) {
             const int r = i / (p.rank / 4), j = 4 * (i - r * (p.rank / 4));
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int q = 0; q < kPartCtas; ++q) {
-                const float4 part = ptx::ld_cluster_f4(ptx::map_rank(ptx::smem_addr(&m.sums[turn][r][j]), q));
+                const float4 part = ptx::ld_cluster_f4(ptx::map_rank(ptx::smem_addr(&m.sums[r][j]), q));
                 sum.x += part.x; sum.y += part.y; sum.z += part.z; sum.w += part.w;
             }
             sum.x *= scale; sum.y *= scale; sum.z *= scale; sum.w *= scale;
@@ -181,32 +207,46 @@ __global__ void __launch_bounds__(kPartThreads) adapter_part_kernel(const __grid
             *reinterpret_cast<uint2*>(&m.u_hi[r][j]) = make_uint2(h0, h1);
             *reinterpret_cast<uint2*>(&m.u_lo[r][j]) = make_uint2(rest_of(sum.x, sum.y, h0), rest_of(sum.z, sum.w, h1));
         }
+        cluster_arrive();
         __syncthreads();
         // ---- times B^T, 16 features to a warp at a time ------------------------------------------------------------------------------
         const int to0 = buffer_row(2 * piece), to1 = buffer_row(2 * piece + 1);
-#pragma unroll 2
-        for (int f0 = warp * 16; f0 < n1 - n0; f0 += kPartWarps * 16) {
-            const uint16_t* lo = factor_b + (size_t)(f0 + row_of) * p.rank;
-            const uint16_t* hi = lo + 8 * p.rank;
-            const bool in_hi = f0 + 8 < n1 - n0;      // (features come in eights)
-            float d[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-            for (int j0 = 0; j0 < p.rank; j0 += 32) {
-                const int j = j0 + piece * 8;
-                const bool in_j = j < p.rank;
-                const uint4 b_lo = in_j ? ldg128(lo + j) : none, b_hi = in_j && in_hi ? ldg128(hi + j) : none;
-                mma_32(d, b_lo, b_hi, in_j ? *reinterpret_cast<const uint4*>(&m.u_hi[row_of][j]) : none);
-                mma_32(d, b_lo, b_hi, in_j ? *reinterpret_cast<const uint4*>(&m.u_lo[row_of][j]) : none);
+        for (int f0 = warp * 16; f0 < n1 - n0; f0 += kPartWarps * 32) {                    // two tiles of 16 features at one time
+            float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            for (int j0 = 0; j0 < p.rank; j0 += 64) {
+                uint4 v[2][2][2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int f = f0 + t * kPartWarps * 16, j = j0 + 32 * i + piece * 8;
+                        const uint16_t* at = factor_b + (size_t)(f + row_of) * p.rank + j;
+                        v[t][i][0] = j < p.rank && f < n1 - n0 ? ldg128(at) : none;
+                        v[t][i][1] = j < p.rank && f + 8 < n1 - n0 ? ldg128(at + 8 * p.rank) : none;   // (features come in eights)
+                    }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int j = j0 + 32 * i + piece * 8;
+                    const uint4 hi = j < p.rank ? *reinterpret_cast<const uint4*>(&m.u_hi[row_of][j]) : none;
+                    const uint4 lo = j < p.rank ? *reinterpret_cast<const uint4*>(&m.u_lo[row_of][j]) : none;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        mma_32(d[t], v[t][i][0], v[t][i][1], hi);
+                        mma_32(d[t], v[t][i][0], v[t][i][1], lo);
+                    }
+                }
             }
-            const int f = n0 + f0 + row_of;
-            if (to0 >= 0) addend[(size_t)to0 * p.N + f] = d[0];
-            if (to1 >= 0) addend[(size_t)to1 * p.N + f] = d[1];
-            if (to0 >= 0 && in_hi) addend[(size_t)to0 * p.N + f + 8] = d[2];
-            if (to1 >= 0 && in_hi) addend[(size_t)to1 * p.N + f + 8] = d[3];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int f = f0 + t * kPartWarps * 16 + 8 * (i >> 1), to = i & 1 ? to1 : to0;
+                    if (to >= 0 && f < n1 - n0) addend[(size_t)to * p.N + n0 + f + row_of] = d[t][i];
+                }
         }
         __syncthreads();                              // (u is written again)
     }
-    ptx::cluster_sync();                              // (no CTA leaves while another may read its sums)
+    if (entered) cluster_wait();                      // (no CTA leaves while another may read its sums)
 }
 
 // Whether the groups are of so few rows that the adapters' part is summed up apart.

@@ -1039,8 +1039,8 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
     const int* held = dev < 0 ? nullptr : grouped_pairs<FP4, VEC, OP>(dev);
     if (!held) return REGIONE_CUDA_ERROR;
     p.chunks = (p.K + kElems - 1) / kElems;
-    // (joined groups: as if all of a set were)
-    const int groups = std::min(OP == Product::kJoined ? std::min(p.groups, p.n_weights) : p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
+    // (joined groups: as if all were where there is one set, and none where the sets take turns)
+    const int groups = std::min(OP == Product::kJoined && p.n_weights == 1 ? 1 : p.groups, p.rows_cap), each = (p.rows_cap + groups - 1) / groups;
     const int f_pairs = (p.N + 2 * kFeat - 1) / (2 * kFeat), f_tiles = (p.N + kFeat - 1) / kFeat;
     // What the launch will take, in ns, if every row of the buffer is live and the groups are alike (1280 live rows in a buffer of 8704, K 2048,
     // N 6144: as long as in one of 1280; 205 in 2304 19.4 us, in 205 17.4): what a launch takes before and behind its tiles, and rounds of tiles, each the chunks of a slice times what a chunk takes (no less than 200 by latency; 105 bytes
