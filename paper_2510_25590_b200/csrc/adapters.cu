@@ -249,12 +249,15 @@ __global__ void __launch_bounds__(kPartThreads, 3) adapter_part_kernel(const __g
     if (entered) cluster_wait();                      // (no CTA leaves while another may read its sums)
 }
 
-// Whether the groups are of so few rows that the adapters' part is summed up apart.
-static bool few_rows(int rows_cap, int groups) { return (long long)rows_cap <= 16LL * groups; }
+// Whether the groups are of so few rows that the adapters' part is summed up apart: 32 on average where all have one weight set, since tiles
+// are shared then (16 groups of 16 rows, 2048 x 6144, rank 16: 25 us against 55; of 64 rows 52 and 56; 4096 x 4096, rank 64, of 64 rows 72
+// and 71), 8 where sets take turns and there are rarely rows to share (16 groups of 8 rows: 52 us against 55, of 32 rows 61 and 56).
+static bool few_rows(int rows_cap, int groups, int n_weights) { return rows_cap <= (n_weights == 1 ? 32LL : 8LL) * groups; }
 
+// For either form, and for calls of fewer rows and groups, which may be of the other one.
 static size_t adapter_workspace(int rows_cap, int groups, int N, int rank) {
-    const size_t bytes = few_rows(rows_cap, groups) ? (size_t)rows_cap * N * sizeof(float) : (size_t)rows_cap * rank * sizeof(uint16_t);
-    return (bytes + 255) & ~(size_t)255;
+    const size_t few = std::min<size_t>(rows_cap, 32 * (size_t)groups);
+    return (std::max(few * N * sizeof(float), (size_t)rows_cap * rank * sizeof(uint16_t)) + 255) & ~(size_t)255;
 }
 
 }  // namespace regione
@@ -281,7 +284,7 @@ extern "C" int regione_adapter_matmul(const regione_bf16* x, int64_t x_stride, c
     const AdapterCall c = {x, x_stride, w, bias, a, b, scale, adapter, row_begin, row_end, n_adapters, rank, rows_cap, groups, n_weights, K, N,
                            activation, out, out_stride, dev_status};
     cudaStream_t st = (cudaStream_t)stream;
-    if (!few_rows(rows_cap, groups)) {
+    if (!few_rows(rows_cap, groups, n_weights)) {
         const int into = adapters_into(c, (uint16_t*)workspace, st);
         return into == REGIONE_OK ? adapters_tail(c, (const uint16_t*)workspace, st) : into;
     }

@@ -21,6 +21,14 @@ sets, the rows' ranges on the device and the activation in its epilogue; "mxfp4"
 names how the blocks' kept K and V are stored between a full step and the region steps behind it: "bf16", or
 "mxfp4" (4 bits, widened in front of each attention).
 
+``norms`` names what normalises and modulates the rows: "torch", or "fused", one ``layer_norm`` with the scale, shift and gate of each
+stream and the residual update of the product before in the same pass.  ``positions`` (fp32 [rows of the joint sequence, axes])
+with ``rotary`` = (freq, axis) turns Q and K by the angles of coordinates instead of the tables ``cos`` and ``sin`` (which may be None
+then); V is left where its product wrote it.  ``adapters`` = (factors, of, scale) puts low-rank adapters beside the "grouped"
+products: factors[name] = (a [n, rank, K], b [n, N, rank]) for any of q<l>, k<l>, v<l>, o<l>, fc1_<l>, fc2_<l> of block l, ``of`` int32 [2] the
+adapters of text and other rows (-1: none), ``scale`` fp32 [n] or None; all on the device, where they may be exchanged
+between steps.
+
 Outside a planted mask the velocity is replaced by the straight line to the reference latent, so that
 the Adaptive Region Partition has a region to find in a stack that was never trained.  One request
 (batch 1); the block definition is stated in the oracle's counterpart of this file.
@@ -32,11 +40,18 @@ from . import binding
 
 class MMDiTScaffold:
     def __init__(self, weights, n_text, n_img, n_ref, heads, head_dim, blocks, cos, sin, ref, planted,
-                 membership=binding.ROWS_PAPER, products="torch", cache="bf16"):
+                 membership=binding.ROWS_PAPER, products="torch", cache="bf16", norms="torch", positions=None, rotary=None,
+                 adapters=None):
         import torch
         if products not in ("torch", "grouped", "mxfp4") or cache not in ("bf16", "mxfp4"):
             raise binding.RegionEError(f"no products {products!r} or cache {cache!r}")
-        self.products, self.cache = products, cache
+        if norms not in ("torch", "fused") or (positions is None) != (rotary is None):
+            raise binding.RegionEError(f"no norms {norms!r}, or positions and rotary are not given together")
+        if adapters is not None and products != "grouped":
+            raise binding.RegionEError("adapters stand beside grouped products")
+        self.products, self.cache, self.norms = products, cache, norms
+        self.positions = None if positions is None else positions.view(1, *positions.shape)
+        self.rotary, self.adapters = rotary, adapters
         self.w = weights                                   # name -> bf16 CUDA tensor
         self.n_text, self.n_img, self.n_ref = n_text, n_img, n_ref
         self.n_full = n_text + n_img + n_ref
@@ -68,8 +83,16 @@ class MMDiTScaffold:
         self._stale = True                                   # row lists / compacted caches need rebuilding
         self._nq = 0
         self.library_launches = 0
+        ints = lambda *v: torch.tensor(v, dtype=i32, device=dev)
+        self.one_each = ints(0, 1), ints(1, 2)               # the modulation's rows: one per stream
+        self.full_ranges = ints(0, self.n_text), ints(self.n_text, self.n_full)
+        self.region_begin, self.region_end = ints(0, 0), ints(0, 0)
+        self.ranges = self.full_ranges
         if products != "torch":
             self._lay_out_weights()
+        if adapters is not None:
+            need = max([binding.adapter_matmul_workspace(n, 2, a.shape[2], b.shape[1], a.shape[1]) for a, b in adapters[0].values()], default=0)
+            self.adapter_workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
 
     def bind(self, loop):
         """The loop whose partition lists (keep_idx) the region steps read."""
@@ -85,7 +108,7 @@ class MMDiTScaffold:
     def _lay_out_weights(self):
         """Both streams' weights of a product as [2, N, K] (codes and scales with 4-bit products), once."""
         import torch
-        hd, dev, i32 = self.hidden, self.ref.device, torch.int32
+        hd, dev = self.hidden, self.ref.device
         self.sets = {}
         for l in range(self.L):
             for name in (f"q{l}", f"k{l}", f"v{l}", f"o{l}", f"fc1_{l}", f"fc2_{l}", f"mod{l}"):
@@ -101,10 +124,6 @@ class MMDiTScaffold:
                     binding.mxfp4_quantize(w, codes, scales, dev_status=self.dev_status)
                     w = (codes, scales)
                 self.sets[name] = w
-        ints = lambda *v: torch.tensor(v, dtype=i32, device=dev)
-        self.one_each = ints(0, 1), ints(1, 2)               # the modulation's rows: one per stream
-        self.full_ranges = ints(0, self.n_text), ints(self.n_text, self.n_full)
-        self.region_begin, self.region_end = ints(0, 0), ints(0, 0)
 
     def _operand(self, a):
         """Rows as a product of ``products`` takes them."""
@@ -121,6 +140,12 @@ class MMDiTScaffold:
     def _product(self, operand, name, ranges, out, activation=binding.ACT_NONE):
         """out[r] = act(rows times the weight set of their range's stream)."""
         w = self.sets[name]
+        if self.adapters is not None and name in self.adapters[0]:
+            (a, b), of, scale = self.adapters[0][name], self.adapters[1], self.adapters[2]
+            binding.adapter_matmul(operand, w, a, b, of, *ranges, out, self.adapter_workspace, scale=scale, activation=activation,
+                                   dev_status=self.dev_status)
+            self.library_launches += 2
+            return out
         if isinstance(w, tuple):
             binding.mxfp4_grouped_matmul(*operand, *w, *ranges, out, activation=activation, dev_status=self.dev_status)
         else:
@@ -147,23 +172,37 @@ class MMDiTScaffold:
         c = torch.tanh(t * self.w["t_a"].float() + self.w["t_b"].float()).to(torch.bfloat16)[None]
         if self.products != "torch":
             both = torch.empty((2, 6 * self.hidden), dtype=torch.bfloat16, device=c.device)
-            m = self._product(c.expand(2, -1).contiguous(), f"mod{l}", self.one_each, both).float().split(1)
+            self._product(c.expand(2, -1).contiguous(), f"mod{l}", self.one_each, both)
         else:
-            m = [(c @ self.w[f"mod{l}_{s}"]).float() for s in (0, 1)]           # [1, 6 * hidden] per stream
+            both = torch.cat([c @ self.w[f"mod{l}_{s}"] for s in (0, 1)])       # [2, 6 * hidden]: a row per stream
+        if self.norms == "fused":
+            return both.chunk(6, dim=-1)
+        m = both.float().split(1)
         full = torch.cat([m[0].expand(n_text_rows, -1), m[1].expand(rows - n_text_rows, -1)])
         return full.chunk(6, dim=-1)
+
+    def _norm(self, h, scale=None, shift=None, update=None):
+        """Rows normalised and modulated; ``update`` = (rows, gate): h += gate * rows first, in place."""
+        import torch
+        out = torch.empty_like(h)
+        kw = {} if update is None else dict(residual=update[0], gate=update[1], x_out=h)
+        binding.layer_norm(h, scale, shift, *self.ranges, out, 1e-6, modulated=True, dev_status=self.dev_status, **kw)
+        self.library_launches += 1
+        return out
 
     def _blocks(self, h, t, positions, n_rows_dev, n_text_rows, attend, keep_kv):
         import torch
         bf = torch.bfloat16
         rows, H, D, hd = h.shape[0], self.H, self.D, self.hidden
         q_s, k_s, v_s, q_d, o_d = self.scratch              # each [1, rows, H, D]
+        fused, pending = self.norms == "fused", None         # pending: the last product, not yet added to h
         for l in range(self.L):
             sh1, sc1, g1, sh2, sc2, g2 = self._mods(t, l, n_text_rows, rows)
-            a = (self._ln(h) * (1.0 + sc1) + sh1).to(bf)
+            a = self._norm(h, sc1, sh1, pending) if fused else (self._ln(h) * (1.0 + sc1) + sh1).to(bf)
+            k_d, v_d = (self.k_full[l], self.v_full[l]) if keep_kv else (self._tmp("_ktmp", rows), self._tmp("_vtmp", rows))
             wq = lambda s: self.w[f"qkv{l}_{s}"]
             operand = None if self.products == "torch" else self._operand(a)
-            for j, dst in enumerate((q_s, k_s, v_s)):            # three projections, each into its own buffer
+            for j, dst in enumerate((q_s, k_s, v_s if self.positions is None else v_d)):   # three projections, each into its own buffer
                 out = dst.view(-1, hd)[:rows]
                 if operand is not None:
                     self._product(operand, f"{'qkv'[j]}{l}", self.ranges, out)
@@ -171,18 +210,34 @@ class MMDiTScaffold:
                 if n_text_rows:
                     torch.matmul(a[:n_text_rows], wq(0)[:, j * hd:(j + 1) * hd], out=out[:n_text_rows])
                 torch.matmul(a[n_text_rows:], wq(1)[:, j * hd:(j + 1) * hd], out=out[n_text_rows:])
-            k_d, v_d = (self.k_full[l], self.v_full[l]) if keep_kv else (self._tmp("_ktmp", rows), self._tmp("_vtmp", rows))
-            binding.fresh_qkv(q_s, k_s, v_s, positions, n_rows_dev,
-                              self.w[f"qn{l}"], self.w[f"kn{l}"], 1e-6, self.cos, self.sin, binding.ROPE_INTERLEAVED,
-                              q_d, k_d, v_d, src_compact=True, dev_status=self.dev_status)
+            if self.positions is not None:
+                binding.rotary_axes(q_s, k_s, self.positions, *self.rotary, q_d, k_d, binding.ROPE_INTERLEAVED, idx=positions,
+                                    n=n_rows_dev, q_weight=self.w[f"qn{l}"], k_weight=self.w[f"kn{l}"], eps=1e-6, src_compact=True,
+                                    dev_status=self.dev_status)
+            else:
+                binding.fresh_qkv(q_s, k_s, v_s, positions, n_rows_dev,
+                                  self.w[f"qn{l}"], self.w[f"kn{l}"], 1e-6, self.cos, self.sin, binding.ROPE_INTERLEAVED,
+                                  q_d, k_d, v_d, src_compact=True, dev_status=self.dev_status)
             self.library_launches += 1
             attend(l, q_d, k_d, v_d, o_d)
-            o = o_d.view(-1, hd)[:rows]
-            h = (h.float() + g1 * self._mm(o, f"o{l}", n_text_rows).float()).to(bf)
-            m = (self._ln(h) * (1.0 + sc2) + sh2).to(bf)
+            o = self._mm(o_d.view(-1, hd)[:rows], f"o{l}", n_text_rows)
+            if fused:
+                m = self._norm(h, sc2, sh2, (o, g1))
+            else:
+                h = (h.float() + g1 * o.float()).to(bf)
+                m = (self._ln(h) * (1.0 + sc2) + sh2).to(bf)
             u = self._mm(m, f"fc1_{l}", n_text_rows, binding.ACT_GELU_TANH)
-            h = (h.float() + g2 * self._mm(u, f"fc2_{l}", n_text_rows).float()).to(bf)
-        return h
+            y = self._mm(u, f"fc2_{l}", n_text_rows)
+            if fused:
+                pending = y, g2
+            else:
+                h = (h.float() + g2 * y.float()).to(bf)
+        return self._norm(h, update=pending) if fused else h
+
+    def _last(self, h):
+        """What the output's product takes of rows behind the blocks (``fused``: they are normalised already)."""
+        import torch
+        return h if self.norms == "fused" else self._ln(h).to(torch.bfloat16)
 
     def _tmp(self, name, rows):
         import torch
@@ -211,13 +266,12 @@ class MMDiTScaffold:
                                      workspace=self.workspace, dev_status=self.dev_status)
             self.library_launches += 2
 
-        if self.products != "torch":
-            self.ranges = self.full_ranges
+        self.ranges = self.full_ranges
         # (the scratch buffers span the whole sequence here, so no slicing copies happen)
         h = self._blocks(h, float(t), self.all_rows, self.n_all, self.n_text, attend, keep_kv=bool(store))
         if store:
             self._stale = True
-        v_net = (self._ln(h[self.n_text:self.n_text + self.n_img]).to(torch.bfloat16) @ w["w_out"])
+        v_net = self._last(h[self.n_text:self.n_text + self.n_img]) @ w["w_out"]
         return self._blend(v_net, x[0], self.ref[0], self.planted[0], float(t))[None]
 
     def _refresh_lists_and_caches(self, edit_idx, n_edit):
@@ -249,7 +303,7 @@ class MMDiTScaffold:
         if with_text:
             h = torch.cat([w["text_emb"], h])
         positions = self.query_rows[:, :nq].contiguous()
-        if self.products != "torch":                         # text rows [0, nt), the others [nt, n_query)
+        if self.products != "torch" or self.norms == "fused":   # text rows [0, nt), the others [nt, n_query)
             self.region_begin[1:].fill_(nt)
             self.region_end[:1].fill_(nt)
             self.region_end[1:].copy_(self.n_query)
@@ -266,7 +320,7 @@ class MMDiTScaffold:
             self.library_launches += 2
 
         h = self._blocks_compact(h, float(t), positions, nt, attend)
-        v_net = (self._ln(h[nt:]).to(torch.bfloat16) @ w["w_out"])
+        v_net = self._last(h[nt:]) @ w["w_out"]
         e = edit_idx[0, :ne].long()
         out = torch.zeros_like(x_e)
         out[0, :ne] = self._blend(v_net, x_e[0, :ne], self.ref[0, e], self.planted[0, e], float(t))
