@@ -84,7 +84,7 @@ def test_rotary_axes_refuses(kw):
 
 
 @pytest.mark.parametrize("kw", [dict(D=72), dict(D=272, qr=544, kr=544, qor=544, kor=544), dict(axes=5), dict(qr=132), dict(qb=516), dict(kor=132), dict(kob=516),
-                                dict(B=65536), dict(cap=(1 << 24) + 1, places=1 << 25), dict(inverse=1, norm=1), dict(Hq=65537, qr=1 << 23, qor=1 << 23)], ids=str)
+                                dict(B=65536), dict(cap=(1 << 24) + 1, places=1 << 25), dict(B=16, cap=1 << 23, places=1 << 23), dict(inverse=1, norm=1), dict(Hq=65537, qr=1 << 23, qor=1 << 23)], ids=str)
 def test_rotary_axes_does_not_support(kw):
     assert _rotary(**kw) == UNSUPPORTED
 
