@@ -104,8 +104,11 @@ FEW = [(1, [(0, 1)], 1, 64, 8, 8, 1), (1, [(0, 1)], 1, 2048, 264, 16, 3), (64, _
        (48, [(i * 16, i * 16 + n) for i, n in enumerate((16, 3, 11))], 1, 1000, 72, 40, 4), (32, _tokens(32), 2, 384, 200, 64, 5),
        (30, [(0, 7), (7, 7), (7, 20), (22, 30)], 1, 8192, 64, 128, 3), (512, _tokens(512), 1, 128, 1024, 24, 9), (300, _tokens(300), 4, 192, 2048, 256, 6),
        (8, [(4 * (i % 2) + i // 2, 4 * (i % 2) + i // 2 + 1) for i in range(8)], 2, 640, 392, 32, 4)]
+# sizes of one piece; many groups of the same few adapters, whose rows are dealt out eight at a time; one adapter for all
+FEW += [(3, _tokens(3), 1, 8, 8, 8, 2), (1000, [(2 * i, 2 * i + 2) for i in range(500)], 1, 64, 64, 8, 3), (512, _tokens(512), 1, 72, 24, 16, 1),
+        (96, [(3 * i, 3 * i + 2) for i in range(32)], 1, 136, 40, 48, 2)]
 # groups of many rows
-MANY = [(40, [(0, 40)], 1, 64, 8, 8, 1), (300, [(0, 300)], 1, 2048, 520, 16, 2), (1200, _streams(2, 77, 523, [523, 400]), 2, 512, 1544, 32, 3),
+MANY = [(70, [(0, 70)], 1, 8, 8, 8, 1), (40, [(0, 40)], 1, 64, 8, 8, 1), (300, [(0, 300)], 1, 2048, 520, 16, 2), (1200, _streams(2, 77, 523, [523, 400]), 2, 512, 1544, 32, 3),
         (2400, _streams(2, 256, 944, [901, 944]), 2, 384, 768, 64, 8), (700, [(0, 700)], 1, 8192, 136, 72, 1), (500, [(3, 50), (50, 50), (60, 490)], 3, 1000, 264, 200, 4),
         (4000, [(0, 60), (60, 70), (70, 4000)], 3, 4096, 264, 128, 2), (640, [(0, 640)], 1, 4096, 1024, 256, 1), (100, [(0, 100)], 1, 4096, 128, 8, 1),
         (2049, [(0, 2049)], 1, 256, 1000, 48, 1)]
@@ -119,7 +122,7 @@ def test_whole_numbers_are_exact(shape):
     c.check_exact(c.run(extra=16, scale=False, bias=False), scale=None, bias=None)
 
 
-@pytest.mark.parametrize("shape", [FEW[2], FEW[4], FEW[6], MANY[1], MANY[2], MANY[4], MANY[7]], ids=lambda s: f"{s[0]}x{s[3]}x{s[4]}r{s[5]}")
+@pytest.mark.parametrize("shape", [FEW[2], FEW[4], FEW[6], FEW[11], MANY[2], MANY[3], MANY[5], MANY[8]], ids=lambda s: f"{s[0]}x{s[3]}x{s[4]}r{s[5]}")
 @pytest.mark.parametrize("gelu", [False, True])
 def test_normal_numbers(shape, gelu):
     rows, ranges, sets, K, N, rank, adapters = shape
@@ -144,7 +147,7 @@ def test_normal_numbers(shape, gelu):
     assert np.sqrt((d * d).mean()) <= 2.5e-3 * np.sqrt((want[c.live] ** 2).mean())
 
 
-@pytest.mark.parametrize("shape", [FEW[2], FEW[9], MANY[2], MANY[8]], ids=["tokens", "sets", "streams", "slices"])
+@pytest.mark.parametrize("shape", [FEW[2], FEW[9], MANY[3], MANY[9]], ids=["tokens", "sets", "streams", "slices"])
 def test_without_an_adapter_it_is_the_grouped_product(shape):
     import torch
     c = Case(*shape[:6], shape[6], [-1] * len(shape[1]), whole=False)
@@ -214,7 +217,7 @@ def test_ranges_that_overlap_stay_in_bounds():
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("shape", [FEW[2], MANY[2]], ids=["few", "many"])
+@pytest.mark.parametrize("shape", [FEW[2], MANY[3]], ids=["few", "many"])
 def test_repeats_captured_two_graphs_and_another_stream(shape):
     import torch
     c = Case(*shape[:6], shape[6], _which(np.random.default_rng(0), len(shape[1]), shape[6]), whole=False)

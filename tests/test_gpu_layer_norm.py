@@ -337,3 +337,29 @@ def test_calls_repeat_bit_for_bit_captured_and_on_another_stream():
     for bufs in (again, other, captured):
         for a, b_ in zip(first[0] + first[1], bufs[0] + bufs[1]):
             assert torch.equal(a, b_)
+
+
+def test_two_calls_at_one_time():
+    """Forward and backward of two batches on two streams, a workspace each."""
+    import torch
+    cases = [Case(1800, 1032, _ragged(1800, 3), 3, residual=True, modulated=True, seed=s) for s in (1, 2)]
+    want = [(_forward(c), _backward(c, True)) for c in cases]
+    for _ in range(3):
+        held, streams = [], [torch.cuda.Stream() for _ in cases]
+        for c in cases:
+            m, s = (_dev_f32(a) for a in _stats(c))
+            held.append(dict(x=dev_bf16(c.x), w=dev_bf16(c.weight), b=dev_bf16(c.bias), r=dev_bf16(c.r), q=dev_bf16(c.gate), dy=dev_bf16(c.dy),
+                             dz=dev_bf16(c.dz), m=m, s=s, at=c.dev_ranges(), z=_old(1800, 1032), y=_old(1800, 1032), dx=_old(1800, 1032),
+                             dr=_old(1800, 1032), g=[torch.zeros((3, 1032), device="cuda") for _ in range(3)],
+                             ws=torch.empty(binding.layer_norm_backward_workspace(1800, 3, 1032), dtype=torch.uint8, device="cuda")))
+        torch.cuda.synchronize()
+        for h, st in zip(held, streams):
+            binding.layer_norm(h["x"], h["w"], h["b"], *h["at"], h["y"], EPS, modulated=True, residual=h["r"], gate=h["q"], x_out=h["z"], stream=st)
+            binding.layer_norm_backward(h["x"], h["m"], h["s"], h["dy"], h["w"], *h["at"], h["dx"], h["g"][0], h["g"][1], h["ws"], modulated=True,
+                                        dx_out=h["dz"], residual=h["r"], gate=h["q"], dresidual=h["dr"], dgate=h["g"][2], stream=st)
+        torch.cuda.synchronize()
+        for h, (f, b) in zip(held, want):
+            assert np.array_equal(host_f64(h["z"]), f[0]) and np.array_equal(host_f64(h["y"]), f[1])
+            assert np.array_equal(host_f64(h["dx"]), b[0]) and np.array_equal(host_f64(h["dr"]), b[1])
+            for i in range(3):
+                assert np.array_equal(host_f64(h["g"][i]).astype(np.float64), b[2 + i])

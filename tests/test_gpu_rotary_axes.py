@@ -109,6 +109,11 @@ def test_row_lists_and_counts(layout, compact):
     _run((16, 56, 56), 4, 200, 60, 4, 4, layout, idx=idx, n=[60, 0, 1, 37], compact=compact, extra=16)
 
 
+def test_the_same_place_twice():
+    idx = np.array([[7, 7, 0, 7, 3, 3, 49, 0, 1, 1]]).repeat(2, 0)
+    _run((16, 24, 24), 2, 50, 10, 2, 2, LAYOUTS[1], idx=idx)
+
+
 def test_indices_and_counts_outside_are_skipped():
     idx = np.arange(20)[None].repeat(2, 0)
     idx[0, 3], idx[0, 4], idx[1, 19] = -1, 50, 2 ** 31 - 1
