@@ -13,8 +13,10 @@
 // exact in two parts, whole turns taken off before anything is rounded.  The angle is off by about 2^-24 turns however far the
 // position is (one fp32 product at position 10^5 is off by 2^-8 radians, as much as the bf16 output).
 //
-// Bound by device memory: 4 bytes an element.  A warp has a row, or a part of its heads where rows are few; its lanes form the angles
-// of the D/2 pairs once and leave them in shared memory, then go through the heads, 16 bytes a lane and four loads in flight.
+// Bound by device memory, 4 bytes an element, where rows have many heads: 20 000 rows of 48 heads of 128 87 us, 0.87 of the copy rate.  A warp
+// has a row, or a part of its heads where rows are few; its lanes form the angles of the D/2 pairs once and leave them in shared memory,
+// then go through the heads, 16 bytes a lane and four loads in flight.  What a row takes before its first head (its place, its angles,
+// the factors of Q and of K) is what bounds rows of few heads: 46 352 rows of 20 heads of 64 55 us, 0.67.
 #include "f32x2.cuh"
 
 #include <algorithm>
