@@ -6,7 +6,7 @@
 // The paper names no such operator; edits of one batch that each bring an adapter of their own share everything else.
 //
 // Groups of many rows: the tensor core does all of it.  u = s_a x A_a^T first, as a grouped product whose weight set is the adapter
-// (bound by one pass over x), rounded to bf16 because the tensor core takes it as an operand: a relative 2^-9 of the adapter's part.
+// (bound by one pass over x), rounded to bf16 because the tensor core takes it as an operand: each number by 2^-8 of it at most.
 // Then the product with W, whose tiles go on behind the chunks of K with those of the rank, u against B_a into the same
 // accumulators: the adapter's part is never rounded, written or read on its own.  17408 rows, K 2048, N 8192, rank 64, GELU: 384 us, the tensor
 // core at the power limit (355 without adapters); 4 x 1101 rows, N 6144, rank 32: 91 (84).

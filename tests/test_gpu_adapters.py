@@ -261,3 +261,29 @@ def test_offsets_beyond_32_bits():
         binding.adapter_matmul(*args, scale=scale, bias=dev_bf16(c.bias))
         torch.cuda.synchronize()
         c.check_exact(host_f64(args[7]))
+
+
+@pytest.mark.parametrize("shape", [FEW[2], FEW[11], MANY[3]], ids=["few", "few_adapters", "many"])
+def test_buffers_that_are_used_again_with_other_contents(shape):
+    """The same buffers and workspace call after call, everything in them written anew on the stream: rows, ranges, adapters, bias, factors."""
+    import torch
+    rng = np.random.default_rng(1)
+    cases = [Case(*shape[:6], shape[6], _which(rng, len(shape[1]), shape[6]), seed=s) for s in range(4)]
+    for c in cases[1::2]:                                              # every second time some rows less
+        c.ranges = [(b, max(b, e - 1)) if i % 3 == 2 else (b, e) for i, (b, e) in enumerate(c.ranges)]
+        c.live = np.zeros(c.rows, bool)
+        for b, e in c.ranges:
+            c.live[b:e] = True
+    sources = [c.args()[:7] + (_f32(c.scale), dev_bf16(c.bias)) for c in cases]
+    held, (out, ws) = [t.clone() for t in sources[0]], cases[0].args()[7:9]
+    torch.cuda.synchronize()
+    got = []
+    for turn in range(12):
+        for to, t in zip(held, sources[turn % 4]):
+            to.copy_(t)
+        out.fill_(OLD)
+        binding.adapter_matmul(*held[:7], out, ws, scale=held[7], bias=held[8])
+        got.append(out.clone())
+    torch.cuda.synchronize()
+    for turn in range(12):
+        cases[turn % 4].check_exact(host_f64(got[turn]))

@@ -363,3 +363,36 @@ def test_two_calls_at_one_time():
             assert np.array_equal(host_f64(h["dx"]), b[0]) and np.array_equal(host_f64(h["dr"]), b[1])
             for i in range(3):
                 assert np.array_equal(host_f64(h["g"][i]).astype(np.float64), b[2 + i])
+
+
+def test_buffers_that_are_used_again_with_other_contents():
+    """The same buffers and workspace call after call, rows, ranges and parameters written anew on the stream."""
+    import torch
+    cases = [Case(1500, 520, _ragged(1500 - 200 * (i % 2), 4), 4, residual=True, modulated=True, seed=i) for i in range(3)]
+    for c in cases:
+        c.live = np.zeros(1500, bool)
+        for b, e in c.ranges:
+            c.live[b:e] = True
+        for a in (c.x, c.r, c.dy, c.dz):
+            a[~c.live] = np.nan
+    want = [_backward(c, True) for c in cases]
+    sources = []
+    for c in cases:
+        m, s = _stats(c)
+        sources.append([dev_bf16(a) for a in (c.x, c.dy, c.dz, c.r, c.gate, c.weight)] + [_dev_f32(m), _dev_f32(s), *c.dev_ranges()])
+    x, dy, dz, r, gate, w, m, s, begin, end = held = [t.clone() for t in sources[0]]
+    dx, dr, grads = _old(1500, 520), _old(1500, 520), [torch.zeros((4, 520), device="cuda") for _ in range(3)]
+    ws = torch.empty(binding.layer_norm_backward_workspace(1500, 4, 520), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    got = []
+    for turn in range(9):
+        for to, t in zip(held, sources[turn % 3]):
+            to.copy_(t)
+        dx.fill_(OLD); dr.fill_(OLD)
+        binding.layer_norm_backward(x, m, s, dy, w, begin, end, dx, grads[0], grads[1], ws, modulated=True, dx_out=dz, residual=r, gate=gate,
+                                    dresidual=dr, dgate=grads[2])
+        got.append([t.clone() for t in (dx, dr, *grads)])
+    torch.cuda.synchronize()
+    for turn in range(9):
+        for t, a in zip(got[turn], want[turn % 3]):
+            assert np.array_equal(host_f64(t).astype(np.float64), a)
