@@ -13,10 +13,10 @@
 // exact in two parts, whole turns taken off before anything is rounded.  The angle is off by about 2^-24 turns however far the
 // position is (one fp32 product at position 10^5 is off by 2^-8 radians, as much as the bf16 output).
 //
-// Bound by device memory, 4 bytes an element, where rows have many heads: 20 000 rows of 48 heads of 128 87 us, 0.87 of the copy rate.  A warp
+// Bound by device memory, 4 bytes an element, where rows have many heads: 20 000 rows of 48 heads of 128 86 us, 0.89 of the copy rate.  A warp
 // has a row, or a part of its heads where rows are few; its lanes form the angles of the D/2 pairs once and leave them in shared memory,
-// then go through the heads, 16 bytes a lane and four loads in flight.  What a row takes before its first head (its place, its angles,
-// the factors of Q and of K) is what bounds rows of few heads: 46 352 rows of 20 heads of 64 55 us, 0.67.
+// then go through the heads, up to eight loads of 16 bytes a lane in flight.  What a row takes before its first head (its place, its angles,
+// the factors of Q and of K) is what bounds rows of few heads: 46 352 rows of 20 heads of 64 54 us, 0.68.
 #include "f32x2.cuh"
 
 #include <algorithm>
@@ -24,7 +24,7 @@
 
 namespace regione {
 
-constexpr int kRotaryMaxD = 256, kRotaryWarps = 8, kRotaryAxes = 4, kRotaryAhead = 4;
+constexpr int kRotaryMaxD = 256, kRotaryWarps = 8, kRotaryAxes = 4;
 
 struct RotaryArgs {
     const uint16_t *q, *k;                            // rows row_stride apart, requests batch_stride apart, heads of a row side by side
@@ -44,23 +44,32 @@ struct RotaryArgs {
     uint8_t axis[kRotaryMaxD / 2];
 };
 
-__device__ __forceinline__ uint4 of_lane(const uint4& v, int lane) {
-    return make_uint4(__shfl_sync(0xffffffffu, v.x, lane), __shfl_sync(0xffffffffu, v.y, lane), __shfl_sync(0xffffffffu, v.z, lane),
-                      __shfl_sync(0xffffffffu, v.w, lane));
-}
+// A lane's pieces of 8 elements of a head, LANES lanes to a head: in the half layout a piece and the one D/2 elements further on, whose
+// elements are the partners of its own; else EACH pieces, LANES apart.  LANES is a power of two; where that is more than a head has
+// for them, lanes have nothing to do (heads of 80: 6 of 16), and EACH is 3 where that leaves none (heads of 48, 96 and 192).
+template <int LANES, int EACH, bool HALF> struct RotaryShape {
+    static constexpr int kLoads = HALF ? 2 : EACH;                     // of a pass
+    static constexpr int kAhead = EACH > 1 ? 2 : 4;                    // passes whose loads are on their way
+    static constexpr int kPairs = HALF ? LANES * 8 : LANES * EACH * 4; // of a head, at most
+    // An SM's blocks: as many as keep that in registers.  (Halves, 20 000 rows of 48 heads of 128: 84 us with two blocks and four passes, 93 with
+    // three and two; 3 x 4099 rows of 26 heads of 96 without norms: 23.8 with three pieces a lane, 26 with a quarter of the lanes idle.)
+    static constexpr int kBlocks = HALF || EACH > 1 ? 2 : 3;
+};
 
-// LANES: a power of two, at least D / 8; lane g of a head has elements 8 g .. 8 g + 7.
-template <int LANES, bool HALF, bool NORM>
-__global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const __grid_constant__ RotaryArgs p) {
-    __shared__ __align__(16) float cos_of[kRotaryWarps][LANES * 4], sin_of[kRotaryWarps][LANES * 4];
-    __shared__ float2 turns_of[LANES * 4];
-    __shared__ int axis_of[LANES * 4];
+template <int LANES, int EACH, bool HALF, bool NORM>
+__global__ void __launch_bounds__(kRotaryWarps * 32, (RotaryShape<LANES, EACH, HALF>::kBlocks))
+rotary_axes_kernel(const __grid_constant__ RotaryArgs p) {
+    using Shape = RotaryShape<LANES, EACH, HALF>;
+    constexpr int kLoads = Shape::kLoads, kAhead = Shape::kAhead;
+    __shared__ __align__(16) float cos_of[kRotaryWarps][Shape::kPairs], sin_of[kRotaryWarps][Shape::kPairs];
+    __shared__ float2 turns_of[Shape::kPairs];
+    __shared__ int axis_of[Shape::kPairs];
     constexpr int kHeads = 32 / LANES;                // of a pass of the warp
-    constexpr int kPairs = (LANES * 4 + 31) / 32;     // of a lane
+    constexpr int kPairs = (Shape::kPairs + 31) / 32; // of a lane
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pairs = p.D / 2;
     // The pairs' frequencies: from the launch's parameters once a block, since 32 addresses of them take a warp 32 turns, then a lane keeps
     // those of the pairs whose angles it forms.
-    if (threadIdx.x < LANES * 4) {
+    if (threadIdx.x < Shape::kPairs) {
         turns_of[threadIdx.x] = make_float2(p.turns_hi[threadIdx.x], p.turns_lo[threadIdx.x]);
         axis_of[threadIdx.x] = p.axis[threadIdx.x];
     }
@@ -69,17 +78,15 @@ __global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const
     int axis[kPairs];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-        const int at = min(lane + 32 * i, LANES * 4 - 1);
+        const int at = min(lane + 32 * i, Shape::kPairs - 1);
         turns[i] = turns_of[at];
         axis[i] = axis_of[at];
     }
     grid_dependency_wait();
     grid_launch_dependents();
-    const int g = lane & (LANES - 1), pieces = p.D / 8, in_pass = lane / LANES;
-    const bool on = g < pieces;
-    const bool second = HALF && 2 * g >= pieces;      // this lane's elements are the second ones of their pairs
-    const int partner = HALF ? (lane & ~(LANES - 1)) + (!on ? g : second ? g - pieces / 2 : g + pieces / 2) : 0;
-    const int partner_g = partner & (LANES - 1);
+    const int g = lane & (LANES - 1), in_pass = lane / LANES, pieces = p.D / 8, units = HALF ? pieces / 2 : pieces;
+    const bool on = EACH > 1 || g < units;
+    const int apart = 8 * (HALF ? units : LANES);     // elements from one of the lane's pieces to the next
     const float inv = 1.0f / p.D;
     const int heads = p.Hq + p.Hk, passes = (heads + kHeads - 1) / kHeads;
     const uint32_t total = ((uint32_t)p.B * p.cap) << p.parts_log;
@@ -109,16 +116,21 @@ __global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const
         uint16_t* q_out = p.q_out + b * p.q_out_batch + j * p.q_out_row + 8 * g;
         uint16_t* k_out = p.k_out + b * p.k_out_batch + j * p.k_out_row + 8 * g - (long long)p.Hq * p.D;
         const int first_pass = (passes * part) >> p.parts_log, last_pass = (passes * (part + 1)) >> p.parts_log;
-        uint4 w[kRotaryAhead];
+        uint4 w[kAhead][kLoads];
         auto fetch = [&](int i0) {
 #pragma unroll
-            for (int u = 0; u < kRotaryAhead; ++u) {
+            for (int u = 0; u < kAhead; ++u) {
+                if (i0 + u >= last_pass) break;       // (for the whole warp)
                 const int h = (i0 + u) * kHeads + in_pass;
-                w[u] = make_uint4(0u, 0u, 0u, 0u);
-                // (not through the path of read-only data: the row may be turned in place)
-                if (i0 + u < last_pass && on && h < heads)
-                    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                                 : "=r"(w[u].x), "=r"(w[u].y), "=r"(w[u].z), "=r"(w[u].w) : "l"((h < p.Hq ? q : k) + h * p.D));
+                const uint16_t* src = (h < p.Hq ? q : k) + h * p.D;
+                const bool in = on && h < heads;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    w[u][i] = make_uint4(0u, 0u, 0u, 0u);
+                    // (not through the path of read-only data: the row may be turned in place)
+                    if (in) asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                         : "=r"(w[u][i].x), "=r"(w[u][i].y), "=r"(w[u][i].z), "=r"(w[u][i].w) : "l"(src + i * apart));
+                }
             }
         };
         fetch(first_pass);
@@ -138,102 +150,133 @@ __global__ void __launch_bounds__(kRotaryWarps * 32, 3) rotary_axes_kernel(const
             }
         }
         __syncwarp();
-        // What the lane's elements are multiplied with, weights and angles in one: the same for all heads of Q, and of K.
-        //   halves: out[e] = r (x[e] own[e] + partner[e] other[e]);   pairs: (a, b) -> r (a own.x + b other.x, a own.y + b other.y)
-        uint64_t own[4], other[4];
-        const int first = !on ? 0 : HALF ? 8 * (second ? g - pieces / 2 : g) : 4 * g;
+        // What the lane's elements are multiplied with.
+        //   halves, a piece x and its partner y: cosines, sines with both signs, and the weights as they are; forming weights times angles
+        //   takes longer than the multiplications where a row has few passes, and as long where it has twelve
+        //   pairs, (a, b) -> r (a own.x + b other.x, a own.y + b other.y): weights and angles in one, the same for all heads of Q, and of K
+        uint64_t own[HALF ? 1 : kLoads][4], other[kLoads][4];
+        uint4 weight_of[2];
         auto factors = [&](const uint16_t* weight) {
-            const float *c = &cos_of[warp][first], *s = &sin_of[warp][first];
+            if constexpr (HALF && NORM) {
 #pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                if constexpr (HALF) {
-                    const float4 cs = *reinterpret_cast<const float4*>(c + 2 * e), sn = *reinterpret_cast<const float4*>(s + 2 * e);
-                    const float sign = second ? 1.f : -1.f;
-                    own[e] = pair_of(cs.x, cs.y);
-                    own[e + 1] = pair_of(cs.z, cs.w);
-                    other[e] = pair_of(sign * sn.x, sign * sn.y);
-                    other[e + 1] = pair_of(sign * sn.z, sign * sn.w);
-                } else {
-                    const float2 cs = *reinterpret_cast<const float2*>(c + e), sn = *reinterpret_cast<const float2*>(s + e);
-                    own[e] = pair_of(cs.x, sn.x);
-                    own[e + 1] = pair_of(cs.y, sn.y);
-                    other[e] = pair_of(-sn.x, cs.x);
-                    other[e + 1] = pair_of(-sn.y, cs.y);
+                for (int i = 0; i < 2; ++i) {
+                    weight_of[i] = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);     // ones
+                    if (weight != nullptr && on) weight_of[i] = ldg128(weight + 8 * g + i * apart);
                 }
-            }
-            if (NORM && weight != nullptr && on) {    // (from L1: there are no registers to keep them in)
-                uint64_t a[4], b[4];
-                if constexpr (HALF) {
-                    widen8(ldg128(weight + 8 * g), a);
-                    widen8(ldg128(weight + 8 * partner_g), b);
-                } else {
-                    const uint4 v = ldg128(weight + 8 * g);
+            } else if constexpr (!HALF) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int first = on ? 4 * (g + LANES * i) : 0;
+                    const float4 cs = *reinterpret_cast<const float4*>(&cos_of[warp][first]), sn = *reinterpret_cast<const float4*>(&sin_of[warp][first]);
+                    const float c[4] = {cs.x, cs.y, cs.z, cs.w}, s[4] = {sn.x, sn.y, sn.z, sn.w};
+                    uint4 v = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);          // ones
+                    if (NORM && weight != nullptr && on) v = ldg128(weight + 8 * g + i * apart);       // (from L1: registers are short)
                     const uint32_t of[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        a[e] = pair_of(bf16_lo(of[e]), bf16_lo(of[e]));
-                        b[e] = pair_of(bf16_hi(of[e]), bf16_hi(of[e]));
+                        own[i][e] = pair_of(c[e], s[e]);
+                        other[i][e] = pair_of(-s[e], c[e]);
+                        if constexpr (NORM) {
+                            own[i][e] = mul2(own[i][e], pair_of(bf16_lo(of[e]), bf16_lo(of[e])));
+                            other[i][e] = mul2(other[i][e], pair_of(bf16_hi(of[e]), bf16_hi(of[e])));
+                        }
                     }
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    own[e] = mul2(own[e], a[e]);
-                    other[e] = mul2(other[e], b[e]);
                 }
             }
         };
+        if constexpr (HALF) {
+            const int first = on ? 8 * g : 0;
+            const float *c = &cos_of[warp][first], *s = &sin_of[warp][first];
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const float4 cs = *reinterpret_cast<const float4*>(c + 2 * e), sn = *reinterpret_cast<const float4*>(s + 2 * e);
+                own[0][e] = pair_of(cs.x, cs.y);
+                own[0][e + 1] = pair_of(cs.z, cs.w);
+                other[0][e] = pair_of(-sn.x, -sn.y);
+                other[0][e + 1] = pair_of(-sn.z, -sn.w);
+                other[1][e] = pair_of(sn.x, sn.y);
+                other[1][e + 1] = pair_of(sn.z, sn.w);
+            }
+        }
         bool of_k = first_pass * kHeads + in_pass >= p.Hq;
         factors(of_k ? p.k_weight : p.q_weight);
 
         // ---- heads of Q, then of K: this part's share of the passes ------------------------------------------------------------
-        for (int i0 = first_pass; i0 < last_pass; i0 += kRotaryAhead) {
+        for (int i0 = first_pass; i0 < last_pass; i0 += kAhead) {
             if (i0 > first_pass) fetch(i0);
 #pragma unroll
-            for (int u = 0; u < kRotaryAhead; ++u) {
+            for (int u = 0; u < kAhead; ++u) {
                 if (i0 + u >= last_pass) break;
                 const int h = (i0 + u) * kHeads + in_pass;
                 if (NORM && !of_k && h >= p.Hq) {                    // (once a row)
                     of_k = true;
                     factors(p.k_weight);
                 }
-                uint64_t x[4], o[4];
-                widen8(w[u], x);
-                float r = 1.f;
+                uint64_t x[kLoads][4], r2 = 0;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) widen8(w[u][i], x[i]);
                 if constexpr (NORM) {
-                    float ss = sum2(fma2(x[0], x[0], fma2(x[1], x[1], fma2(x[2], x[2], mul2(x[3], x[3])))));
+                    uint64_t squares = 0;
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i)
+                        squares = fma2(x[i][0], x[i][0], fma2(x[i][1], x[i][1], fma2(x[i][2], x[i][2], fma2(x[i][3], x[i][3], squares))));
+                    float ss = sum2(squares);
 #pragma unroll
                     for (int d = LANES / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-                    r = rsqrtf(fmaf(ss, inv, p.eps));
+                    const float r = rsqrtf(fmaf(ss, inv, p.eps));
+                    r2 = pair_of(r, r);
                 }
-                if constexpr (HALF) {
-                    uint64_t y[4];
-                    widen8(of_lane(w[u], partner), y);
+                if constexpr (HALF && NORM)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[e] = fma2(y[e], other[e], mul2(x[e], own[e]));
-                } else {
-                    const uint32_t v[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+                    for (int i = 0; i < 2; ++i) {
+                        uint64_t m[4];
+                        widen8(weight_of[i], m);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float a = bf16_lo(v[e]), b = bf16_hi(v[e]);
-                        o[e] = fma2(pair_of(b, b), other[e], mul2(pair_of(a, a), own[e]));
+                        for (int e = 0; e < 4; ++e) x[i][e] = mul2(x[i][e], m[e]);
                     }
-                }
-                if constexpr (NORM)
+                const bool in = on && h < heads;
+                uint16_t* dst = (h < p.Hq ? q_out : k_out) + h * p.D;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[e] = mul2(o[e], pair_of(r, r));
-                if (!on || h >= heads) continue;
-                *reinterpret_cast<uint4*>((h < p.Hq ? q_out : k_out) + h * p.D) = round8(o);
+                for (int i = 0; i < kLoads; ++i) {
+                    uint64_t o[4];
+                    if constexpr (HALF) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = fma2(x[1 - i][e], other[i][e], mul2(x[i][e], own[0][e]));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float a, b;
+                            parts_of(x[i][e], a, b);
+                            o[e] = fma2(pair_of(b, b), other[i][e], mul2(pair_of(a, a), own[i][e]));
+                        }
+                    }
+                    if constexpr (NORM)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = mul2(o[e], r2);
+                    if (in) *reinterpret_cast<uint4*>(dst + i * apart) = round8(o);
+                }
             }
         }
     }
 }
 
-template <int LANES> static cudaError_t rotary_launch(const RotaryArgs& p, bool half, bool norm, dim3 grid, cudaStream_t st) {
+template <int LANES, int EACH, bool HALF> static cudaError_t rotary_run(RotaryArgs& p, bool norm, cudaStream_t st) {
+    // Warps to a row: what takes the fewest rounds of resident warps, an item as many turns as it has passes over heads and four more for
+    // its angles (4000 rows of 48 heads of 128: one 23.1 us, two 19.9; 20 000 rows: one).
+    constexpr int kBlocks = RotaryShape<LANES, EACH, HALF>::kBlocks;
+    const int passes = ((p.Hq + p.Hk) * LANES + 31) / 32;
+    const long long rows = (long long)p.B * p.cap, resident = (long long)kBlocks * kRotaryWarps * sm_count();
+    long long least = 0x7fffffffffffffffLL;
+    for (int log = 0; log <= 4 && (log == 0 || (1 << log) <= passes); ++log) {
+        const long long cost = (((rows << log) + resident - 1) / resident) * ((passes + (1 << log) - 1) / (1 << log) + 4);
+        if (cost >= least) continue;
+        least = cost;
+        p.parts_log = log;
+    }
+    const dim3 grid((unsigned)std::min(((rows << p.parts_log) + kRotaryWarps - 1) / kRotaryWarps, (long long)kBlocks * sm_count()));
     const dim3 block(kRotaryWarps * 32);
-    if (half) return norm ? launch_overlapped(rotary_axes_kernel<LANES, true, true>, grid, block, 0, st, p)
-                          : launch_overlapped(rotary_axes_kernel<LANES, true, false>, grid, block, 0, st, p);
-    return norm ? launch_overlapped(rotary_axes_kernel<LANES, false, true>, grid, block, 0, st, p)
-                : launch_overlapped(rotary_axes_kernel<LANES, false, false>, grid, block, 0, st, p);
+    return norm ? launch_overlapped(rotary_axes_kernel<LANES, EACH, HALF, true>, grid, block, 0, st, p)
+                : launch_overlapped(rotary_axes_kernel<LANES, EACH, HALF, false>, grid, block, 0, st, p);
 }
 
 // Rows of [B, rows, H, D] with requests and rows apart.
@@ -283,28 +326,22 @@ extern "C" int regione_rotary_axes(const regione_bf16* q, int64_t q_batch, int64
         p.turns_lo[i] = (float)(turns - (double)p.turns_hi[i]);
         p.axis[i] = (uint8_t)axis[i];
     }
-    int lanes = 2;
-    while (lanes < D / 8) lanes *= 2;
-    // Warps to a row: what takes the fewest rounds of resident warps, an item as many turns as it has passes over heads and four more for
-    // its angles (4000 rows of 48 heads of 128: one 23.1 us, two 19.9; 20 000 rows: one).
-    const int passes = ((Hq + Hk) * lanes + 31) / 32;
-    const long long rows = (long long)B * cap, resident = 3LL * kRotaryWarps * sm_count();
-    long long least = 0x7fffffffffffffffLL;
-    for (int log = 0; log <= 4 && (log == 0 || (1 << log) <= passes); ++log) {
-        const long long cost = (((rows << log) + resident - 1) / resident) * ((passes + (1 << log) - 1) / (1 << log) + 4);
-        if (cost >= least) continue;
-        least = cost;
-        p.parts_log = log;
-    }
-    const long long blocks = std::min(((rows << p.parts_log) + kRotaryWarps - 1) / kRotaryWarps, 3LL * sm_count());
-    const dim3 grid((unsigned)blocks);
-    const bool half = rope_layout == REGIONE_ROPE_HALF, norm = normalise != 0;
+    const int pieces = D / 8, units = rope_layout == REGIONE_ROPE_HALF ? pieces / 2 : pieces;
+    const bool norm = normalise != 0;
     cudaStream_t st = (cudaStream_t)stream;
-    switch (lanes) {
-        case 2: return launch_status(rotary_launch<2>(p, half, norm, grid, st));
-        case 4: return launch_status(rotary_launch<4>(p, half, norm, grid, st));
-        case 8: return launch_status(rotary_launch<8>(p, half, norm, grid, st));
-        case 16: return launch_status(rotary_launch<16>(p, half, norm, grid, st));
-        default: return launch_status(rotary_launch<32>(p, half, norm, grid, st));
+    if (rope_layout == REGIONE_ROPE_HALF) {
+        if (units <= 1) return launch_status(rotary_run<1, 1, true>(p, norm, st));
+        if (units <= 2) return launch_status(rotary_run<2, 1, true>(p, norm, st));
+        if (units <= 4) return launch_status(rotary_run<4, 1, true>(p, norm, st));
+        if (units <= 8) return launch_status(rotary_run<8, 1, true>(p, norm, st));
+        return launch_status(rotary_run<16, 1, true>(p, norm, st));
     }
+    if (units == 6) return launch_status(rotary_run<2, 3, false>(p, norm, st));
+    if (units == 12) return launch_status(rotary_run<4, 3, false>(p, norm, st));
+    if (units == 24) return launch_status(rotary_run<8, 3, false>(p, norm, st));
+    if (units <= 2) return launch_status(rotary_run<2, 1, false>(p, norm, st));
+    if (units <= 4) return launch_status(rotary_run<4, 1, false>(p, norm, st));
+    if (units <= 8) return launch_status(rotary_run<8, 1, false>(p, norm, st));
+    if (units <= 16) return launch_status(rotary_run<16, 1, false>(p, norm, st));
+    return launch_status(rotary_run<32, 1, false>(p, norm, st));
 }
