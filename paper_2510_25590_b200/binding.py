@@ -598,21 +598,24 @@ def _workspace(device, t):
 def _sets(device, C, *tensors):
     """Sets, set distance and addresses of the parameters [sets, C] that are given, which have to lie alike: (tensor, name)."""
     bf = _torch().bfloat16
-    sets, step, at = 0, C, []
+    shape, step, at = None, C, []
     for t, name in tensors:
         if t is None:
             at.append(None)
             continue
-        if not sets:
-            _ranks(**{name: (t, 2)})
-            sets = t.shape[0]
-            where, step = _rows(device, t, (sets, C), bf, name)
+        if shape is None:
+            try:
+                shape = (t.shape[0], C)
+            except (AttributeError, IndexError):
+                _ranks(**{name: (t, 2)})
+                raise
+            where, step = _rows(device, t, shape, bf, name)
         else:
-            where, apart = _rows(device, t, (sets, C), bf, name)
+            where, apart = _rows(device, t, shape, bf, name)
             if apart != step:
                 raise RegionEError(f"the sets of {name} are not as far apart as those of the other parameters")
         at.append(where)
-    return (sets or 1, step, *at)
+    return (1 if shape is None else shape[0], step, *at)
 
 
 def layer_norm(x, weight, bias, row_begin, row_end, out, eps, modulated=False, residual=None, gate=None, x_out=None, mean=None,
