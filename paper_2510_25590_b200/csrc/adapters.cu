@@ -139,11 +139,11 @@ __global__ void __launch_bounds__(kPartThreads, 3) adapter_part_kernel(const __g
     const uint16_t* factor_b = p.b + ((size_t)a * p.N + n0) * p.rank;
     const float scale = p.scale != nullptr ? p.scale[a] : 1.0f;
     const int total = m.first[m.groups];
-    const long long first_round = m.place * subs + sub;
-    if (first_round * kPartRows < total && threadIdx.x == 0 && n1 > n0)      // (read in the second half; contiguous)
+    const long long first_eight = m.place * subs + sub;
+    if (first_eight * kPartRows < total && threadIdx.x == 0 && n1 > n0)      // (read in the second half; contiguous)
         asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(factor_b), "r"((n1 - n0) * p.rank * 2) : "memory");
-    for (long long c = first_round; c * kPartRows < total; c += m.groups * subs) {
-        auto buffer_row = [&](int i) {                // of the i-th row of this round, -1 behind the last
+    for (long long c = first_eight; c * kPartRows < total; c += m.groups * subs) {
+        auto buffer_row = [&](int i) {                // of the i-th of the eight rows, -1 behind the last
             const int v = (int)(c * kPartRows) + i;
             if (v >= total) return -1;
             int lo = 0, hi = m.groups - 1;            // the last group whose first row is not behind v
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kPartThreads, 3) adapter_part_kernel(const __g
             }
             return m.begin[lo] + v - m.first[lo];
         };
-        if (entered) cluster_wait();                  // (all have read what this CTA left in the round before)
+        if (entered) cluster_wait();                  // (all have read what this CTA left for the eight before)
         // ---- u = x A^T over this CTA's part of K ---------------------------------------------------------------------------
         const int from = buffer_row(row_of);
         const uint16_t* x = p.x + (size_t)max(from, 0) * p.x_stride;
