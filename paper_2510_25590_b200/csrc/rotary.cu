@@ -307,7 +307,7 @@ extern "C" int regione_rotary_axes(const regione_bf16* q, int64_t q_batch, int64
     if (D % 16 || D > kRotaryMaxD || axes > kRotaryAxes || Hq > 65536 || Hk > 65536 || B > 65535 || cap > (1 << 24) || n_pos > (1 << 28))
         return REGIONE_UNSUPPORTED;
     for (int i = 0; i < D / 2; ++i)
-        if (axis[i] < 0 || axis[i] >= axes || !std::isfinite(freq[i])) return REGIONE_INVALID_ARG;
+        if (axis[i] < 0 || axis[i] >= axes || !(std::fabs(freq[i]) <= 1e7)) return REGIONE_INVALID_ARG;
     if (B == 0 || cap == 0) return REGIONE_OK;
     if (!positions) return REGIONE_INVALID_ARG;
     int rc;

@@ -75,7 +75,7 @@ def _rotary(q=FAKE, qb=512, qr=128, k=FAKE, kb=512, kr=128, idx=NULL, n=NULL, po
 
 @pytest.mark.parametrize("kw", [dict(q=NULL), dict(q=ODD), dict(qo=NULL), dict(qo=ODD), dict(k=ODD), dict(ko=ODD), dict(k=NULL), dict(ko=NULL), dict(Hk=0),
                                 dict(pos=NULL), dict(B=-1), dict(cap=-1), dict(places=-1), dict(Hq=0), dict(Hk=-1), dict(D=0), dict(axes=0),
-                                dict(layout=2), dict(layout=-1), dict(axis=[3]), dict(axis=[-1]), dict(freq=[float("nan")]), dict(freq=[float("inf")]),
+                                dict(layout=2), dict(layout=-1), dict(axis=[3]), dict(axis=[-1]), dict(freq=[float("nan")]), dict(freq=[float("inf")]), dict(freq=[-1.1e7]),
                                 dict(qr=120), dict(kr=120), dict(qor=120), dict(kor=120), dict(qb=-8), dict(pb=-1), dict(cap=5), dict(qob=0), dict(kob=0),
                                 dict(qw=FAKE), dict(kw=FAKE), dict(norm=1, qw=ODD), dict(norm=1, kw=ODD), dict(norm=1, eps=-1.0),
                                 dict(norm=1, eps=float("nan"))], ids=str)

@@ -1,7 +1,7 @@
 """GPU parity of the rotary positions with several axes with the oracle's turns of complex numbers in 64 bits.
 
 Bounds.  The output is off by half a bf16 step, 2^-8 of its value.  In front of that each of the two products is off by what the angle is
-off, 2 pi 2^-22, by the cosine (2^-22) and by a few fp32 operations, and the normalised element by 2^-20: less than 2^-17 of |a| + |b|."""
+off, 2 pi 2^-22, by the cosine (2^-21) and by a few fp32 operations, and the normalised element by 2^-20: less than 2^-17 of |a| + |b|."""
 import numpy as np
 import pytest
 
