@@ -51,6 +51,7 @@ struct NormGradArgs {
     float one;
     uint16_t *dx, *dr;
     long long dx_stride, dr_stride;
+    long long x_step, dy_step, dz_step, r_step, dx_step, dr_step;      // of a team, from one of its rows to the next: teams * stride
     float* sums;                                      // workspace: [slot][3][C]
     float *dweight, *dbias, *dgate;                   // [n_sets, C] or NULL
     int32_t* dev_status;
@@ -188,7 +189,7 @@ template <bool RES, int EACH, int AHEAD>
 __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(const __grid_constant__ NormGradArgs p, int width, int teams) {
     extern __shared__ __align__(16) uint8_t ring[];   // [AHEAD][x, dy, dx_out, r][piece][threads] of 16 bytes
     __shared__ RowGroups table;
-    __shared__ __align__(16) uint64_t part[2][kNormThreads / 32 + kNormMaxTeams];    // of a warp: the two sums; an even number to a team
+    __shared__ uint64_t part[2][kNormThreads / 32];   // of a warp: the two sums
     __shared__ float4 stage[kNormThreads];
     grid_dependency_wait();
     grid_launch_dependents();
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(co
     const int v1 = (int)min((long long)total, v0 + share);
     if (v0 >= v1) return;
     const int team = threadIdx.x / width, t = threadIdx.x - team * width;
-    const int warps = width >> 5, places = (warps + 1) & ~1;
+    const int warps = width >> 5, lane = threadIdx.x & 31;
     const bool from_elsewhere = p.dz != nullptr;
     const float inv = 1.0f / p.C;
     const uint64_t one = pair_of(p.one, p.one);
@@ -211,7 +212,6 @@ __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(co
         col[i] = (i * width + t) * 8;
         live[i] = col[i] < p.C;
     }
-    if ((warps & 1) && t == 0) part[0][team * places + warps] = part[1][team * places + warps] = 0;
     int g = group_of(&table, (int)v0, 0), turn = 0;
     // the rows to fetch: where their group ends, and where they lie
     int next = (int)v0 + team, next_g = g, next_end = 0;
@@ -237,10 +237,10 @@ __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(co
                 if (from_elsewhere) copy16(to + 2 * array_bytes, dz_at + i * width * 8);
                 if (RES) copy16(to + 3 * array_bytes, r_at + i * width * 8);
             }
-            x_at += teams * p.x_stride;
-            dy_at += teams * p.dy_stride;
-            if (from_elsewhere) dz_at += teams * p.dz_stride;
-            if (RES) r_at += teams * p.r_stride;
+            x_at += p.x_step;
+            dy_at += p.dy_step;
+            if (from_elsewhere) dz_at += p.dz_step;
+            if (RES) r_at += p.r_step;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         next += teams;
@@ -315,14 +315,16 @@ __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(co
                 sums = add2(sums, pair_of(__shfl_xor_sync(0xffffffffu, x, d), __shfl_xor_sync(0xffffffffu, y, d)));
             }
             if (warps > 1) {
-                const uint64_t* mine = &part[turn][team * places];
-                if ((threadIdx.x & 31) == 0) part[turn][team * places + (t >> 5)] = sums;
+                const uint64_t* mine = &part[turn][team * warps];
+                if (lane == 0) part[turn][threadIdx.x >> 5] = sums;
                 asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(width) : "memory");
-                sums = 0;
-#pragma unroll 4
-                for (int i = 0; i < places; i += 2) {
-                    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(mine + i);
-                    sums = add2(add2(sums, two.x), two.y);
+                // (each half of a warp has the sums of all warps, up to sixteen: four steps, however many there are)
+                sums = (lane & 15) < warps ? mine[lane & 15] : 0;
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1) {
+                    float x, y;
+                    parts_of(sums, x, y);
+                    sums = add2(sums, pair_of(__shfl_xor_sync(0xffffffffu, x, d), __shfl_xor_sync(0xffffffffu, y, d)));
                 }
                 turn ^= 1;                            // (a place is written again two rows on, behind the next one's barrier)
             }
@@ -356,8 +358,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(co
                     *reinterpret_cast<uint4*>(dr_at + i * width * 8) = round8(d);
                 }
             }
-            dx_at += teams * p.dx_stride;
-            if (RES) dr_at += teams * p.dr_stride;
+            dx_at += p.dx_step;
+            if (RES) dr_at += p.dr_step;
         }
         // the teams' sums, in their order, to the slot of this share and group
         float* to = p.sums + (size_t)(blockIdx.x + g) * 3 * p.C;
@@ -575,6 +577,8 @@ extern "C" int regione_layer_norm_backward(const regione_bf16* x, int64_t x_stri
     p.sums = (float*)workspace; p.dweight = dweight; p.dbias = dbias; p.dgate = dgate; p.dev_status = dev_status;
     const cudaStream_t st = (cudaStream_t)stream;
     const NormShape n = norm_shape(rows_cap, C, r != nullptr);
+    p.x_step = n.teams * p.x_stride; p.dy_step = n.teams * p.dy_stride; p.dz_step = n.teams * p.dz_stride;
+    p.r_step = n.teams * p.r_stride; p.dx_step = n.teams * p.dx_stride; p.dr_step = n.teams * p.dr_stride;
     if (!empty) {
         const cudaError_t e = n.each == 2 ? (r ? norm_grad_launch<true, 2, 3>(p, n, st) : norm_grad_launch<false, 2, 3>(p, n, st))
                                           : (r ? norm_grad_launch<true, 1, 4>(p, n, st) : norm_grad_launch<false, 1, 4>(p, n, st));
