@@ -18,7 +18,7 @@
 // Backward: a block has a contiguous share of the rows, gone through by teams, and a thread the same columns of all rows of its team, whose
 // sums it keeps in registers; two sums a row cross the team (one barrier).  Where a share passes from one group to the next the
 // teams' sums go to a slot of the workspace, and a second kernel adds the slots of a set in the order of the rows: results do
-// not depend on timing.  17408 x 2048 rows with the residual 80 us, 0.77 of the copy rate: sixteen warps an SM, which is what the sums leave
+// not depend on timing.  17408 x 2048 rows with the residual 79 us, 0.78 of the copy rate: sixteen warps an SM, which is what the sums leave
 // registers for, issue half of the time (58 us without its loads).  All arithmetic in fp32.
 #include "f32x2.cuh"
 #include "row_groups.cuh"
