@@ -19,7 +19,7 @@
 // sums it keeps in registers; two sums a row cross the team (one barrier).  Where a share passes from one group to the next the
 // teams' sums go to a slot of the workspace, and a second kernel adds the slots of a set in the order of the rows: results do
 // not depend on timing.  17408 x 2048 rows with the residual 79 us, 0.78 of the copy rate: sixteen warps an SM, which is what the sums leave
-// registers for, issue half of the time (58 us without its loads).  All arithmetic in fp32.
+// registers for, issue half of the time (a form of 86 us took 58 without its loads).  All arithmetic in fp32.
 #include "f32x2.cuh"
 #include "row_groups.cuh"
 
@@ -470,7 +470,9 @@ static cudaError_t norm_run(const NormArgs& p, cudaStream_t st) {
     if (rows < 4 * sms) return norm_launch<8>(p, rows, st);
     if (rows < 16 * sms || p.C > 2048) return norm_launch<4>(p, std::min(rows, 8 * sms), st);
     if (p.C <= 1024) return norm_launch<1>(p, std::min((rows + 7) / 8, 8 * sms), st);
-    return p.r != nullptr ? norm_launch<4>(p, std::min(rows, 64 * sms), st) : norm_launch<2>(p, std::min(rows, 16 * sms), st);
+    if (p.r != nullptr) return norm_launch<4, 2>(p, std::min(rows, 64 * sms), st);
+    const int blocks = std::min(rows, 16 * sms);
+    return p.C <= 1536 ? norm_launch<2, 3>(p, blocks, st) : norm_launch<2, 4>(p, blocks, st);
 }
 
 // Of the backward pass: threads of a team, teams of a block, blocks.
