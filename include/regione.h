@@ -340,9 +340,8 @@ int regione_mxfp4_grouped_matmul(const uint8_t* x_q, const uint8_t* x_scale, con
  *     out[r, :] = act(x[r, :] W_i^T + bias_i + s_a (x[r, :] A_a^T) B_a^T),     a = adapter[g], none where it is -1
  * a dev bf16 [n_adapters, rank, K], b dev bf16 [n_adapters, N, rank], scale dev f32 [n_adapters] or NULL (1), adapter dev int32
  * [groups]; an index outside [-1, n_adapters) is taken as -1 and REGIONE_DEV_BOUNDS recorded.  rank a multiple of 8 up to 256,
- * n_adapters <= 65536.  Sums in fp32, one rounding to bf16 at the end; where rows_cap is more than 32 rows a group (8 where
- * n_weights > 1), x A^T is rounded to bf16 in between (by 2^-8 of each of its numbers at most, which the sum over the rank averages).
- * Groups of fewer rows are fastest when those of one weight set lie side by side: they share their tiles then.
+ * n_adapters <= 65536.  Sums in fp32, one rounding to bf16 at the end; in between x A^T is a sum of bf16 numbers, 2^-15 of each of its
+ * numbers off at most.  Groups of fewer rows are fastest when those of one weight set lie side by side: they share their tiles then.
  * workspace: 16-byte aligned, regione_adapter_matmul_workspace(...) bytes, which also do for fewer rows, groups, features and ranks; two
  * calls that may run at one time need one each, so two graphs that may be replayed at one time do.  Two kernel launches; nothing is allocated.
  */

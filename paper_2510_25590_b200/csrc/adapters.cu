@@ -6,10 +6,10 @@
 // The paper names no such operator; edits of one batch that each bring an adapter of their own share everything else.
 //
 // Groups of many rows: the tensor core does all of it.  u = s_a x A_a^T first, as a grouped product whose weight set is the adapter
-// (bound by one pass over x), rounded to bf16 because the tensor core takes it as an operand: each number by 2^-8 of it at most.
-// Then the product with W, whose tiles go on behind the chunks of K with those of the rank, u against B_a into the same
-// accumulators: the adapter's part is never rounded, written or read on its own.  17408 rows, K 2048, N 8192, rank 64, GELU: 384 us, the tensor
-// core at the power limit (355 without adapters); 4 x 1101 rows, N 6144, rank 32: 91 (84).
+// (bound by one pass over x), left as two bf16 numbers that add up to it (lead_part), because the tensor core takes it as an operand and one
+// would be off by 2^-8.  Then the product with W, whose tiles go on behind the chunks of K with those of the rank, both parts of u against
+// B_a into the same accumulators: the adapter's part is never written or read on its own.  17408 rows, K 2048, N 8192, rank 64, GELU: 398 us,
+// the tensor core at the power limit (355 without adapters); 4 x 1101 rows, N 6144, rank 32: 94 (82).
 //
 // Groups of a row or two (a token each): tiles of their own would read W once per group.  The adapters' part comes first here, in
 // fp32, by this file's kernel: a cluster of eight CTAs has eight rows with the same adapter, each CTA an eighth of K for the first factor
@@ -259,7 +259,7 @@ static bool few_rows(int rows_cap, int groups, int n_weights) { return rows_cap 
 // For either form, and for calls of fewer rows and groups, which may be of the other one.
 static size_t adapter_workspace(int rows_cap, int groups, int N, int rank) {
     const size_t few = std::min<size_t>(rows_cap, 32 * (size_t)groups);
-    return (std::max(few * N * sizeof(float), (size_t)rows_cap * rank * sizeof(uint16_t)) + 255) & ~(size_t)255;
+    return (std::max(few * N * sizeof(float), (size_t)rows_cap * rank * kSumParts * sizeof(uint16_t)) + 255) & ~(size_t)255;
 }
 
 }  // namespace regione

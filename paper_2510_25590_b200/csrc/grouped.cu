@@ -64,15 +64,17 @@ struct GroupedArgs {
     int32_t* dev_status;
     // low-rank adapters (see Product)
     const int32_t* adapter;                           // [groups], -1: none
-    int n_adapters, rank, tail;                       // tail: chunks of the rank behind those of K
+    int n_adapters, rank, tail;                       // tail: chunks of the rank behind those of K, as often as a sum has parts
     const float* adapter_scale;                       // [n_adapters] or NULL
     const float* addend;                              // [rows_cap, N]
 };
 
 // What a launch multiplies.  kPlain: rows with the weight set of their group.  The others are the parts of a product with low-rank
 // adapters beside it:
-//   kInto    u = s_a x A_a^T, the adapter of the group in place of the weight set; rows of groups without one are left out
-//   kTail    rows with the weight set, and behind the chunks of K those of the rank: u with B_a, into the same accumulators
+//   kInto    u = s_a x A_a^T, the adapter of the group in place of the weight set; rows of groups without one are left out.  A sum leaves
+//            as its parts (see lead_part), each kind of them rows_cap rows behind the one before
+//   kTail    rows with the weight set, and behind the chunks of K those of the rank, once for each part: u with B_a, into the same
+//            accumulators
 //   kJoined  rows with the weight set plus an fp32 row that the adapters' sums are already in; groups of a set whose ranges touch are one
 //            range, so that many groups of a row or two share the tiles, and the weights are read once
 enum class Product { kPlain, kInto, kTail, kJoined };
@@ -83,7 +85,7 @@ struct GroupedMaps {
 };
 struct TailMaps : GroupedMaps {
     CUtensorMap b;                                    // (rank, N, n_adapters), box 128 bytes x 128 rows
-    CUtensorMap u[kMaps];                             // (rank, rows), box 128 bytes x 16 << i rows
+    CUtensorMap u[kMaps];                             // (rank, rows of all parts), box 128 bytes x 16 << i rows
 };
 template <Product OP> using MapsOf = std::conditional_t<OP == Product::kTail, TailMaps, GroupedMaps>;
 
@@ -633,7 +635,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
     constexpr int kAccs = PAIR ? 2 : 1;
     // The chunk behind the last one of a tile: the last slice takes those of the rank, where the tile's group has an adapter.
     auto chunks_end = [&](const GroupedTile& tile) {
-        return OP == Product::kTail && tile.adapter >= 0 && c_end == p.chunks ? c_end + p.tail : c_end;
+        return OP == Product::kTail && tile.adapter >= 0 && c_end == p.chunks ? c_end + kSumParts * p.tail : c_end;
     };
 
     // A cluster goes through its tiles without a stop; where slices meet, one tile at a time.
@@ -660,12 +662,12 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
                                     asm volatile("fence.proxy.async.global;" ::: "memory");
                                     waited = true;
                                 }
-                                const int j = (c - p.chunks) * kElems;
+                                const int part = (c - p.chunks) / p.tail, j = (c - p.chunks - part * p.tail) * kElems;
                                 load_w<PAIR>(dst, &maps.b, bar, j, feature, tile.adapter);
 #pragma unroll
                                 for (int box = kMaps - 1; box >= 0; --box)
                                     if (rows & (16 << box)) {
-                                        load_x<PAIR>(dst + kTileBytes + at * kChunkBytes, &maps.u[box], bar, j, row + at);
+                                        load_x<PAIR>(dst + kTileBytes + at * kChunkBytes, &maps.u[box], bar, j, part * p.rows_cap + row + at);
                                         at += 16 << box;
                                     }
                                 if (++s == stages) { s = 0; phase ^= 1; }
@@ -718,7 +720,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
                             }
                         }
                         // 32 bytes of K to an instruction; what lies behind K is zero and left out
-                        const int behind = OP == Product::kTail && c >= p.chunks ? p.rank - (c - p.chunks) * kElems : p.K - c * kElems;
+                        const int behind = OP == Product::kTail && c >= p.chunks ? p.rank - (c - p.chunks) % p.tail * kElems : p.K - c * kElems;
                         const int left = (behind + kElems / 4 - 1) / (kElems / 4);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
@@ -743,7 +745,7 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
                 while (s >= stages) { s -= stages; phase ^= 1; }
             }
         } else if (warp < kEpiWarps) {
-            constexpr int kEpiCols = 16 * (kEpiWarps / 4);
+            constexpr int kEpiCols = 16 * (kEpiWarps / 4), kOuts = OP == Product::kInto ? kSumParts : 1;
             const int sub = warp & 3, part = warp >> 2;
             const uint32_t stage = ptx::smem_addr(staging) + warp * kStagingBytes;
             for (long long t = t0; t < t_end; t += workers, ++it) {
@@ -801,36 +803,47 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
                                 y[i] = add2(y[i], pair_of(f < p.N && q < tile.live ? from[0] : 0.f, f < p.N && q + 1 < tile.live ? from[p.N] : 0.f));
                             }
                         if (p.activation == REGIONE_ACT_GELU_TANH) gelu_tanh(y);
-                        uint32_t z[8];
+                        // (one pass; a sum of kInto leaves in its parts)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float lo, hi;
-                            parts_of(y[i], lo, hi);
-                            z[i] = pack_bf16x2(lo, hi);
-                        }
-                        // row of the tile t at 64 t, its 16-byte pieces (8 features) turned by t / 2 so that eight rows meet eight banks
-                        const int row = (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1, turn = (row >> 1) & 3;
-                        if (PAIR && lane == 0) ptx::bulk_wait_read<0>();             // (the store of the step before)
-                        __syncwarp();
-                        stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), z[0], z[1], z[2], z[3]);
-                        stmatrix_x4_trans(stage + row * 64 + (((piece + 2) ^ turn) << 4), z[4], z[5], z[6], z[7]);
-                        if (PAIR && c + 16 <= tile.live) {
-                            ptx::fence_proxy_async_smem();
-                            __syncwarp();
-                            if (lane == 0 && feature < p.N) {
-                                store_out(&maps.out, stage, feature, tile.first + c);
-                                ptx::bulk_commit();
-                            }
-                        } else {
-                            __syncwarp();
+                        for (int o = 0; o < kOuts; ++o) {
+                            const int to = tile.first + c + o * p.rows_cap;
+                            uint32_t z[8];
 #pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int q = (lane >> 2) + 8 * i, j = lane & 3;
-                                const uint4 v = *reinterpret_cast<const uint4*>(staging + warp * kStagingBytes + q * 64 + ((j ^ ((q >> 1) & 3)) << 4));
-                                if (c + q < tile.live && feature + 8 * j < p.N)
-                                    *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + c + q) * p.out_stride + feature + 8 * j) = v;
+                            for (int i = 0; i < 8; ++i) {
+                                float lo, hi;
+                                parts_of(y[i], lo, hi);
+                                if constexpr (kOuts > 1) {
+                                    const float a = lead_part(lo, o + 1 == kOuts), b = lead_part(hi, o + 1 == kOuts);
+                                    y[i] = pair_of(lo, hi);
+                                    z[i] = pack_bf16x2(a, b);
+                                } else {
+                                    z[i] = pack_bf16x2(lo, hi);
+                                }
                             }
+                            // row of the tile t at 64 t, its 16-byte pieces (8 features) turned by t / 2 so that eight rows meet eight banks
+                            const int row = (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1, turn = (row >> 1) & 3;
+                            if (PAIR && lane == 0) ptx::bulk_wait_read<0>();         // (the store of the step before)
                             __syncwarp();
+                            stmatrix_x4_trans(stage + row * 64 + ((piece ^ turn) << 4), z[0], z[1], z[2], z[3]);
+                            stmatrix_x4_trans(stage + row * 64 + (((piece + 2) ^ turn) << 4), z[4], z[5], z[6], z[7]);
+                            if (PAIR && c + 16 <= tile.live) {
+                                ptx::fence_proxy_async_smem();
+                                __syncwarp();
+                                if (lane == 0 && feature < p.N) {
+                                    store_out(&maps.out, stage, feature, to);
+                                    ptx::bulk_commit();
+                                }
+                            } else {
+                                __syncwarp();
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const int q = (lane >> 2) + 8 * i, j = lane & 3;
+                                    const uint4 v = *reinterpret_cast<const uint4*>(staging + warp * kStagingBytes + q * 64 + ((j ^ ((q >> 1) & 3)) << 4));
+                                    if (c + q < tile.live && feature + 8 * j < p.N)
+                                        *reinterpret_cast<uint4*>(p.out + (size_t)(to + q) * p.out_stride + feature + 8 * j) = v;
+                                }
+                                __syncwarp();
+                            }
                         }
                     }
                 }
@@ -891,10 +904,17 @@ grouped_kernel(const __grid_constant__ MapsOf<OP> maps, const __grid_constant__ 
 #pragma unroll
                         for (int i = 0; i < 4; ++i) parts_of(z[i], y[2 * i], y[2 * i + 1]);
                     }
-                    uint4 o;
-                    o.x = pack_bf16x2(y[0], y[1]); o.y = pack_bf16x2(y[2], y[3]);
-                    o.z = pack_bf16x2(y[4], y[5]); o.w = pack_bf16x2(y[6], y[7]);
-                    *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + q) * p.out_stride + f) = o;
+                    constexpr int kOuts = OP == Product::kInto ? kSumParts : 1;
+#pragma unroll
+                    for (int i = 0; i < kOuts; ++i) {
+                        float z[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] = kOuts > 1 ? lead_part(y[e], i + 1 == kOuts) : y[e];
+                        uint4 o;
+                        o.x = pack_bf16x2(z[0], z[1]); o.y = pack_bf16x2(z[2], z[3]);
+                        o.z = pack_bf16x2(z[4], z[5]); o.w = pack_bf16x2(z[6], z[7]);
+                        *reinterpret_cast<uint4*>(p.out + (size_t)(tile.first + i * p.rows_cap + q) * p.out_stride + f) = o;
+                    }
                 }
             }
             ptx::fence_proxy_async_smem();                // (the ring's next copies write where the sums were)
@@ -1030,7 +1050,7 @@ static int grouped_launch(const MapsOf<OP>& maps, const GroupedArgs& p, int clus
     return launch_status(launch_counted(&cfg, grouped_kernel<FP4, PAIR, VEC, OP>, maps, p));
 }
 
-// `b`, `u`: the adapters' second factors [n_adapters, N, rank] and the rows' products with the first [rows_cap, rank] (kTail).
+// `b`, `u`: the adapters' second factors [n_adapters, N, rank] and the rows' products with the first [parts, rows_cap, rank] (kTail).
 template <bool FP4, bool VEC, Product OP = Product::kPlain>
 static int grouped_run(const void* x, long long x_row_bytes, const void* w, GroupedArgs p, cudaStream_t st, const void* b = nullptr,
                        const void* u = nullptr) {
@@ -1101,10 +1121,11 @@ static int grouped_run(const void* x, long long x_row_bytes, const void* w, Grou
         p.tail = (p.rank + kElems - 1) / kElems;
         ok = ok && grouped_map(&maps.b, false, 3, b, p.rank, p.N, p.n_adapters, 2LL * p.rank, 128);
         for (int i = 0; i < kMaps && ok && (pair || (16 << i) <= p.width); ++i)
-            ok = grouped_map(&maps.u[i], false, 2, u, p.rank, p.rows_cap, 1, 2LL * p.rank, 16 << i);
+            ok = grouped_map(&maps.u[i], false, 2, u, p.rank, (long long)kSumParts * p.rows_cap, 1, 2LL * p.rank, 16 << i);
     }
     if (ok && pair) {
-        const cuuint64_t dims[2] = {(cuuint64_t)p.N, (cuuint64_t)p.rows_cap}, strides[1] = {(cuuint64_t)(2 * p.out_stride)};
+        const cuuint64_t dims[2] = {(cuuint64_t)p.N, (cuuint64_t)p.rows_cap * (OP == Product::kInto ? kSumParts : 1)};
+        const cuuint64_t strides[1] = {(cuuint64_t)(2 * p.out_stride)};
         const cuuint32_t box[2] = {32u, 16u}, ones[2] = {1u, 1u};
         ok = grouped_encode_fn()(&maps.out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.out, dims, strides, box, ones,
                                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
