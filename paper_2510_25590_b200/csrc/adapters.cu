@@ -27,6 +27,7 @@ namespace regione {
 
 constexpr int kMaxRank = 256, kMaxAdapterGroups = 512;
 constexpr int kPartCtas = 8, kPartThreads = 256, kPartWarps = kPartThreads / 32, kPartRows = 8;
+constexpr int kPartSums = 3;                          // bf16 numbers that u is taken apart into: all of its 24 bits (0.2 us of 18 more than two)
 
 // D = A B + D of 16 x 16 by 16 x 8 bf16 numbers.  (Eight rows at a time: the tensor core's large tiles would stand almost empty.)
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -40,19 +41,13 @@ __device__ __forceinline__ void mma_32(float (&d)[4], const uint4& lo, const uin
     mma_16x8x16(d, lo.z, hi.z, lo.w, hi.w, b.z, b.w);
 }
 
-// What two numbers are above those that they were rounded to.  (Infinite ones: nothing.)
-__device__ __forceinline__ uint32_t rest_of(float x, float y, uint32_t rounded) {
-    const float a = bf16_lo(rounded), b = bf16_hi(rounded);
-    return pack_bf16x2(isinf(a) ? 0.f : x - a, isinf(b) ? 0.f : y - b);
-}
-
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 struct PartMemory {
     float sums[kPartRows][kMaxRank];                  // this CTA's part of u = x A^T
     float parts[kPartWarps * 16][kPartRows + 1];      // of a warp, before the warps with the same ranks are added
-    uint16_t u_hi[kPartRows][kMaxRank + 8], u_lo[kPartRows][kMaxRank + 8];
+    uint16_t u[kPartSums][kPartRows][kMaxRank + 8];
     int begin_of[kMaxAdapterGroups], rows_of[kMaxAdapterGroups], adapter_of[kMaxAdapterGroups];      // of all groups
     int begin[kMaxAdapterGroups], first[kMaxAdapterGroups + 1];      // the adapter's groups: their rows, numbered through
     int warp_rows[kPartWarps], warp_groups[kPartWarps];
@@ -195,7 +190,7 @@ __global__ void __launch_bounds__(kPartThreads, 3) adapter_part_kernel(const __g
         cluster_arrive();
         cluster_wait();
         entered = true;
-        // ---- the CTAs' parts, in their order; u as the sum of two bf16 numbers, 2^-16 off -----------------------------------------
+        // ---- the CTAs' parts, in their order; u as the sum of three bf16 numbers ---------------------------------------------------
         for (int i = threadIdx.x; i < kPartRows * (p.rank / 4); i += kPartThreads) {
             const int r = i / (p.rank / 4), j = 4 * (i - r * (p.rank / 4));
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -205,9 +200,12 @@ __global__ void __launch_bounds__(kPartThreads, 3) adapter_part_kernel(const __g
                 sum.x += part.x; sum.y += part.y; sum.z += part.z; sum.w += part.w;
             }
             sum.x *= scale; sum.y *= scale; sum.z *= scale; sum.w *= scale;
-            const uint32_t h0 = pack_bf16x2(sum.x, sum.y), h1 = pack_bf16x2(sum.z, sum.w);
-            *reinterpret_cast<uint2*>(&m.u_hi[r][j]) = make_uint2(h0, h1);
-            *reinterpret_cast<uint2*>(&m.u_lo[r][j]) = make_uint2(rest_of(sum.x, sum.y, h0), rest_of(sum.z, sum.w, h1));
+#pragma unroll
+            for (int o = 0; o < kPartSums; ++o) {
+                const bool last = o + 1 == kPartSums;
+                const float x0 = lead_part(sum.x, last), x1 = lead_part(sum.y, last), x2 = lead_part(sum.z, last), x3 = lead_part(sum.w, last);
+                *reinterpret_cast<uint2*>(&m.u[o][r][j]) = make_uint2(pack_bf16x2(x0, x1), pack_bf16x2(x2, x3));
+            }
         }
         cluster_arrive();
         __syncthreads();
@@ -229,12 +227,11 @@ __global__ void __launch_bounds__(kPartThreads, 3) adapter_part_kernel(const __g
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int j = j0 + 32 * i + piece * 8;
-                    const uint4 hi = j < p.rank ? *reinterpret_cast<const uint4*>(&m.u_hi[row_of][j]) : none;
-                    const uint4 lo = j < p.rank ? *reinterpret_cast<const uint4*>(&m.u_lo[row_of][j]) : none;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        mma_32(d[t], v[t][i][0], v[t][i][1], hi);
-                        mma_32(d[t], v[t][i][0], v[t][i][1], lo);
+                    for (int o = 0; o < kPartSums; ++o) {
+                        const uint4 u = j < p.rank ? *reinterpret_cast<const uint4*>(&m.u[o][row_of][j]) : none;
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) mma_32(d[t], v[t][i][0], v[t][i][1], u);
                     }
                 }
             }
