@@ -403,7 +403,8 @@ int regione_layer_norm_backward(const regione_bf16* x, int64_t x_stride, const f
  * q [B, rows, Hq, D], k [B, rows, Hk, D] (NULL with Hk = 0 and k_out NULL: Q alone) and the outputs [B, cap, H, D] dev bf16,
  * requests *_batch and rows *_row elements apart (multiples of 8), 16-byte aligned: parts of one projection's rows may be passed as
  * they lie.  positions dev f32 [B, n_pos, axes], requests positions_batch elements apart (0: the same for all); whole numbers are
- * exact to 2^24.  The angle is off by no more than 2^-22 turns for positions and frequencies of up to 2^22 turns.  freq host f64 [D/2],
+ * exact to 2^24.  The angle is off by no more than 2^-22 turns while it is below 2^23 turns (position times frequency, whichever of the two
+ * is the large one), and by 2^-45 of itself beyond: from 2^43 turns on it says nothing, which is not reported.  freq host f64 [D/2],
  * radians a unit of position, 0 for pairs that are not turned, no more than 1e7; axis host int32 [D/2]; both are read during the call.  q_weight,
  * k_weight dev bf16 [D] or NULL (ones).  A row may be turned in place (an output that is its source, idx NULL or src_compact);
  * otherwise sources and outputs must not overlap.  D a multiple of 16 up to 256, axes <= 4, B * cap < 2^27.  A count outside [0, cap] is clamped, a

@@ -747,7 +747,8 @@ def rotary_axes(q, k, positions, freq, axis, q_out, k_out, layout, idx=None, n=N
     normalisation where ``eps`` is given.  ``q`` [B, rows, Hq, D], ``k`` [B, rows, Hk, D] or None (requests and rows may lie apart),
     ``positions`` [B or 1, places, axes] fp32, ``freq`` and ``axis`` D / 2 numbers on the host (``rotary_frequencies``).  Output row j of
     request b, j < n[b], has place idx[b, j] (without ``idx`` place j) and is read from the row of that number, or from row j
-    (``src_compact``).  ``inverse`` turns the other way, which is the gradient of the rotation."""
+    (``src_compact``).  ``inverse`` turns the other way, which is the gradient of the rotation.  Angles are exact to 2^-22 turns while
+    position times frequency stays below 2^23 turns, and off by 2^-45 of themselves beyond."""
     torch = _torch()
     at = _here()
     bf, i32 = torch.bfloat16, torch.int32
