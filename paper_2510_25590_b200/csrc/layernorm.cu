@@ -446,10 +446,11 @@ __global__ void __launch_bounds__(kSumWarps * 32) layer_norm_sums_kernel(const _
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
+template <int W, int P, bool RES> static cudaError_t norm_launch(const NormArgs& p, int blocks, cudaStream_t st) {
+    return launch_overlapped(layer_norm_kernel<W, P, RES>, dim3(blocks), dim3(W == 1 ? 256 : W * 32), 0, st, p);
+}
 template <int W, int P> static cudaError_t norm_launch(const NormArgs& p, int blocks, cudaStream_t st) {
-    const dim3 grid(blocks), block(W == 1 ? 256 : W * 32);
-    return p.r != nullptr ? launch_overlapped(layer_norm_kernel<W, P, true>, grid, block, 0, st, p)
-                          : launch_overlapped(layer_norm_kernel<W, P, false>, grid, block, 0, st, p);
+    return p.r != nullptr ? norm_launch<W, P, true>(p, blocks, st) : norm_launch<W, P, false>(p, blocks, st);
 }
 template <int W> static cudaError_t norm_launch(const NormArgs& p, int blocks, cudaStream_t st) {
     switch ((p.C + W * 256 - 1) / (W * 256)) {
@@ -470,9 +471,9 @@ static cudaError_t norm_run(const NormArgs& p, cudaStream_t st) {
     if (rows < 4 * sms) return norm_launch<8>(p, rows, st);
     if (rows < 16 * sms || p.C > 2048) return norm_launch<4>(p, std::min(rows, 8 * sms), st);
     if (p.C <= 1024) return norm_launch<1>(p, std::min((rows + 7) / 8, 8 * sms), st);
-    if (p.r != nullptr) return norm_launch<4, 2>(p, std::min(rows, 64 * sms), st);
+    if (p.r != nullptr) return norm_launch<4, 2, true>(p, std::min(rows, 64 * sms), st);
     const int blocks = std::min(rows, 16 * sms);
-    return p.C <= 1536 ? norm_launch<2, 3>(p, blocks, st) : norm_launch<2, 4>(p, blocks, st);
+    return p.C <= 1536 ? norm_launch<2, 3, false>(p, blocks, st) : norm_launch<2, 4, false>(p, blocks, st);
 }
 
 // Of the backward pass: threads of a team, teams of a block, blocks.
