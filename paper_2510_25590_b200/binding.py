@@ -792,8 +792,8 @@ def rotary_axes(q, k, positions, freq, axis, q_out, k_out, layout, idx=None, n=N
             kw = _on(at, k_weight, bf, "k_weight")
     try:
         freq, axis = array("d", freq), array("i", axis)
-    except TypeError:
-        raise RegionEError("freq and axis must be sequences of numbers, axis of whole ones") from None
+    except (TypeError, OverflowError):
+        raise RegionEError("freq and axis must be sequences of numbers, axis of whole ones of 32 bits") from None
     if len(freq) != D // 2 or len(axis) != D // 2:
         raise RegionEError("freq and axis must have D / 2 entries")
     _check(load().regione_rotary_axes(
