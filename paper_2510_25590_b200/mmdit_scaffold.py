@@ -25,7 +25,7 @@ names how the blocks' kept K and V are stored between a full step and the region
 stream and the residual update of the product before in the same pass.  ``positions`` (fp32 [rows of the joint sequence, axes])
 with ``rotary`` = (freq, axis) turns Q and K by the angles of coordinates instead of the tables ``cos`` and ``sin`` (which may be None
 then); V is left where its product wrote it.  ``adapters`` = (factors, of, scale) puts low-rank adapters beside the "grouped"
-products: factors[name] = (a [n, rank, K], b [n, N, rank]) for any of q<l>, k<l>, v<l>, o<l>, fc1_<l>, fc2_<l> of block l, ``of`` int32 [2] the
+products: factors[name] = (a [n, rank, K], b [n, N, rank]) for any of q<l>, k<l>, v<l>, o<l>, fc1_<l>, fc2_<l>, mod<l> of block l (others are refused), ``of`` int32 [2] the
 adapters of text and other rows (-1: none), ``scale`` fp32 [n] or None; all on the device, where they may be exchanged
 between steps.
 
@@ -49,6 +49,9 @@ class MMDiTScaffold:
             raise binding.RegionEError(f"no norms {norms!r}, or positions and rotary are not given together")
         if adapters is not None and products != "grouped":
             raise binding.RegionEError("adapters stand beside grouped products")
+        names = {f"{name}{l}" for l in range(blocks) for name in ("q", "k", "v", "o", "fc1_", "fc2_", "mod")}
+        if adapters is not None and not names.issuperset(adapters[0]):
+            raise binding.RegionEError(f"no products {sorted(set(adapters[0]) - names)} to put adapters beside")
         self.products, self.cache, self.norms = products, cache, norms
         self.positions = None if positions is None else positions.view(1, *positions.shape)
         self.rotary, self.adapters = rotary, adapters
