@@ -9,13 +9,13 @@
 // (bound by one pass over x), left as two bf16 numbers that add up to it (lead_part), because the tensor core takes it as an operand and one
 // would be off by 2^-8.  Then the product with W, whose tiles go on behind the chunks of K with those of the rank, both parts of u against
 // B_a into the same accumulators: the adapter's part is never written or read on its own.  17408 rows, K 2048, N 8192, rank 64, GELU: 398 us,
-// the tensor core at the power limit (355 without adapters); 4 x 1101 rows, N 6144, rank 32: 94 (82).
+// the tensor core at the power limit (355 without adapters); 4 x 1101 rows, N 6144, rank 32: 94 (83).
 //
 // Groups of a row or two (a token each): tiles of their own would read W once per group.  The adapters' part comes first here, in
 // fp32, by this file's kernel: a cluster of eight CTAs has eight rows with the same adapter, each CTA an eighth of K for the first factor
 // (partial sums meet over distributed shared memory, added in the order of the CTAs) and an eighth of N for the second.  It is
 // bound by the latency of its steps (7 to 10 us) and by reading A and B.  The product with W, which runs beside it, takes groups that lie side by
-// side as one and adds that part in its epilogue.  64 rows, K 2048, N 6144, rank 16, 24 adapters: 17.6 us, of which the product on its own
+// side as one and adds that part in its epilogue.  64 rows, K 2048, N 6144, rank 16, 24 adapters: 17.8 us, of which the product on its own
 // takes 11.
 #include "adapters.cuh"
 #include "grouped_plan.cuh"
@@ -249,8 +249,9 @@ __global__ void __launch_bounds__(kPartThreads, 3) adapter_part_kernel(const __g
 }
 
 // Whether the groups are of so few rows that the adapters' part is summed up apart: 32 on average where all have one weight set, since tiles
-// are shared then (16 groups of 16 rows, 2048 x 6144, rank 16: 25 us against 55; of 64 rows 52 and 56; 4096 x 4096, rank 64, of 64 rows 72
-// and 71), 8 where sets take turns and there are rarely rows to share (16 groups of 8 rows: 52 us against 55, of 32 rows 61 and 56).
+// are shared then (16 groups of 16 rows, 2048 x 6144, rank 16: 26 us against 57; of 64 rows 57 and 59; 4096 x 4096, rank 64, of 64 rows 78
+// and 72; one group of 1900 rows beside 63 single ones 108 and 246, since each of those would be a tile), 8 where sets take turns and
+// there are rarely rows to share (16 groups of 8 rows: 53 us against 57, of 32 rows 62 and 58).
 static bool few_rows(int rows_cap, int groups, int n_weights) { return rows_cap <= (n_weights == 1 ? 32LL : 8LL) * groups; }
 
 // For either form, and for calls of fewer rows and groups, which may be of the other one.

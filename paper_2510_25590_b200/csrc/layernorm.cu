@@ -18,7 +18,7 @@
 // Backward: a block has a contiguous share of the rows, gone through by teams, and a thread the same columns of all rows of its team, whose
 // sums it keeps in registers; two sums a row cross the team (one barrier).  Where a share passes from one group to the next the
 // teams' sums go to a slot of the workspace, and a second kernel adds the slots of a set in the order of the rows: results do
-// not depend on timing.  17408 x 2048 rows with the residual 79 us, 0.78 of the copy rate: sixteen warps an SM, which is what the sums leave
+// not depend on timing.  17408 x 2048 rows with the residual 82 us, 0.81 of the copy rate: sixteen warps an SM, which is what the sums leave
 // registers for, issue half of the time (a form of 86 us took 58 without its loads).  All arithmetic in fp32.
 #include "f32x2.cuh"
 #include "row_groups.cuh"
@@ -482,7 +482,9 @@ struct NormShape {
 };
 // Eight columns to a thread and up to eight teams; sixteen for rows of more than 4096 columns, which need it, and for many rows without a
 // gated residual, where the sums of two pieces still fit in registers and a row's reduction costs half as much (17408 x 2048: 62 us
-// with eight, 55 with sixteen; 1101 x 1536: 10.7 and 14; with the residual, 17408 x 2048: 85 and 133, as registers are spilled).
+// with eight, 55 with sixteen; 1101 x 1536: 10.7 and 14; with the residual, 17408 x 2048: 85 and 133, as registers are spilled).  Of the
+// copy rate with the residual: 17408 x 1024 0.70, 2048 0.81, 4096 0.82; 2560, whose one team leaves 10 warps to an SM, 0.66; 8704 x 8192,
+// sixteen columns to a thread and spilled, 0.52.
 static NormShape norm_shape(int rows_cap, int C, bool residual) {
     NormShape n;
     n.each = C > 4096 || (!residual && rows_cap > 16 * sm_count()) ? 2 : 1;

@@ -17,7 +17,8 @@
 // Bound by device memory, 4 bytes an element, where rows have many heads: 20 000 rows of 48 heads of 128 86 us, 0.89 of the copy rate.  A warp
 // has a row, or a part of its heads where rows are few; its lanes form the angles of the D/2 pairs once and leave them in shared memory,
 // then go through the heads, up to eight loads of 16 bytes a lane in flight.  What a row takes before its first head (its place, its angles,
-// the factors of Q and of K) is what bounds rows of few heads: 46 352 rows of 20 heads of 64 54 us, 0.68.
+// the factors of Q and of K), which a warp waits for row by row, bounds rows of few heads: 46 352 rows of 20 heads of 64 54 us, 0.68, with
+// sixteen warps an SM, which is what the registers leave, that issue 57 % of the time.
 #include "f32x2.cuh"
 
 #include <algorithm>
